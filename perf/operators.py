@@ -264,7 +264,7 @@ def prepare(case, seed):
             s["grad_bias"] = empty((d,), g)
             s["grad_pos"] = empty((th * tw, d), g) if case["pos"] else None
             s["workspace"] = empty((tokens.patch_embed_workspace_bytes(
-                s["images"], s["grad_weight"], s["layout"]),), torch.uint8)
+                s["images"], s["grad_weight"], dt, s["layout"]),), torch.uint8)
     elif op == "embed":
         s["out"] = empty((n, d), DTYPES[case["act"]])
     elif op == "embed_grad":
