@@ -43,9 +43,18 @@ SOURCES = [
     "smol_jpeg_entropy.cpp",
     "smol_stream.hip",
     "smol_scratch.hip",
+    "smol_patch.hip",
+    "smol_patch_f32.hip",
+    "smol_patch_f16.hip",
+    "smol_patch_bf16.hip",
+    "smol_patch_grad_f32.hip",
+    "smol_patch_grad_f16.hip",
+    "smol_patch_grad_bf16.hip",
+    "smol_embed.hip",
+    "smol_norm.hip",
 ]
 HEADERS = ["smol_internal.h", "smol_device.h", "smol_rows.h", "smol_rows_rgb.h", "smol_rows_yuv.h",
-           "smol_magic.h"]
+           "smol_magic.h", "smol_tokens_device.h", "smol_patch.h", "smol_patch_kernels.h"]
 
 # -ffp-contract=off: the kernels round every multiply and add on their own, as
 # the definition does; fused multiply-adds are never formed implicitly.

@@ -1,0 +1,175 @@
+// smol_patch.h -- what the patch embedding's forward and backward kernels
+// share: where a patch's values stand in the image, and their loads.
+//
+// A patch is `runs` runs of `length` consecutive image elements (NCHW: one
+// per channel and patch row, `patch` long; NHWC: one per patch row, patch *
+// channels long), and a weight row is the same runs one after the other. The
+// kernels take runs in chunks of 16 bytes of the weight's type; a run's last
+// chunk is moved back to end with the run, and the values that it repeats
+// count as zeros ("lead" of them). So no load passes a run, whatever its
+// length, and a matrix product over chunks is one over the values.
+#ifndef SMOL_PATCH_H
+#define SMOL_PATCH_H
+
+#include <type_traits>
+
+#include "smol_magic.h"
+#include "smol_tokens.h"
+#include "smol_tokens_device.h"
+
+namespace smol {
+
+// Division by a fixed divisor (smol_magic.h).
+struct Divisor {
+    uint32_t d, m, s;
+};
+
+inline Divisor make_divisor(uint32_t d)
+{
+    Divisor v;
+    v.d = d;
+    magic_divisor(d, &v.m, &v.s);
+    return v;
+}
+
+__device__ __forceinline__ uint32_t divide(uint32_t n, const Divisor &v)
+{
+    return (uint32_t)((uint64_t)n * v.m >> v.s);
+}
+
+struct PatchArgs {
+    const void *images, *weight, *bias, *pos;
+    void *out;              // forward: rows; backward: partial products
+    const void *grad_out;
+    int64_t image_stride, row_stride;  // of out or grad_out
+    int64_t image_size;     // elements of an image
+    uint32_t rows, dim;     // n * tokens; columns
+    uint32_t values;        // of a patch: runs * length
+    uint32_t length;        // of a run
+    uint32_t chunks;        // of a patch
+    uint32_t step_y, step_x;      // elements from a patch to the next
+    uint32_t plane, pitch;        // from a channel, and a run, to the next
+    Divisor tokens, across, per_run, per_channel;  // tokens of an image and
+                            // across it; chunks of a run; runs of a channel
+    uint32_t tiles;  // of the output; tiles_n of them side by side
+    Divisor tiles_n;
+    uint32_t splits, split_rows;  // backward: parts of the rows, rows a part
+};
+
+// Where image row m's patch (m = image * tokens + token) begins.
+__device__ __forceinline__ int64_t patch_at(const PatchArgs &a, uint32_t m)
+{
+    const uint32_t i = divide(m, a.tokens), t = m - i * a.tokens.d;
+    const uint32_t ty = divide(t, a.across), tx = t - ty * a.across.d;
+    return i * a.image_size + (int64_t)ty * a.step_y + tx * a.step_x;
+}
+
+// Chunk q of a patch for elements of which C make a chunk: its place in the
+// patch, in the weight row, and how many of its first values are not its own
+// (C for a chunk past the patch).
+template <int C>
+struct Chunk {
+    uint32_t image, weight;
+    int32_t lead;
+    int32_t have;  // values from `image` on that the run has (C unless the run is shorter)
+    __device__ __forceinline__ Chunk(const PatchArgs &a, uint32_t q)
+    {
+        const bool past = q >= a.chunks;
+        q = past ? a.chunks - 1 : q;
+        const uint32_t r = divide(q, a.per_run), j = (q - r * a.per_run.d) * C;
+        const uint32_t back = a.length >= C ? a.length - C : 0;
+        const uint32_t at = j < back ? j : back;
+        const uint32_t ch = divide(r, a.per_channel);
+        image = ch * a.plane + (r - ch * a.per_channel.d) * a.pitch + at;
+        weight = r * a.length + at;
+        lead = past ? C : j - at;
+        have = a.length < C ? a.length : C;
+    }
+};
+
+// Sets a chunk's first `lead` values to zero.
+template <typename T, int C>
+__device__ __forceinline__ vec<T, C> masked(vec<T, C> v, int32_t lead)
+{
+#pragma unroll
+    for (int e = 0; e < C; ++e)
+        v[e] = e >= lead ? v[e] : (T)0.0f;
+    return v;
+}
+
+// C elements from p as type T; Short: only the first `have` exist.
+template <typename S, typename T, int C, bool Short>
+__device__ __forceinline__ vec<T, C> load_chunk(const S *p, int32_t have)
+{
+    vec<S, C> v;
+    if (Short) {
+#pragma unroll
+        for (int e = 0; e < C; ++e)
+            v[e] = e < have ? p[e] : (S)0.0f;
+    } else {
+        v = load<S, C>(p);
+    }
+    if constexpr (sizeof(S) == sizeof(T) && std::is_same<S, T>::value)
+        return v;
+    else
+        return from_f32<T, C>(to_f32<C, S>(v));
+}
+
+// The product of a lane's 16 bytes of each operand (16 rows a side, the
+// lanes' fourths of the wave holding different values of the summed index),
+// added to a 16 x 16 tile in fp32: lane l has rows 4 (l / 16) .. + 3 of the
+// first operand, column l % 16 of the second.
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ f32x4 mma(vec<f16, 8> a, vec<f16, 8> b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(vec<bf16, 8> a, vec<bf16, 8> b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(vec<float, 4> a, vec<float, 4> b, f32x4 c)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+}
+
+// Workgroup b's piece of work of `count`: workgroups are dealt out to the
+// chip's eight dies in turn, and neighbouring pieces share operands, so each
+// die takes a contiguous range of them (its L2 then holds the shared rows).
+__device__ __forceinline__ uint32_t piece_of(uint32_t b, uint32_t count)
+{
+    const uint32_t die = b & 7, each = count >> 3, more = count & 7;
+    return die * each + (die < more ? die : more) + (b >> 3);
+}
+
+// How a patch's runs meet the chunks: whole runs of whole chunks and a whole
+// number of K steps; chunks that repeat values or are past the patch; runs
+// shorter than a chunk.
+enum { kWhole, kMasked, kShort };
+
+// Calls f with the image's element type; a type of the weight takes fp32 and
+// fp16 images, and bf16 ones if it is bf16 itself.
+template <typename T, typename F>
+auto with_image(int type, F f)
+{
+    if constexpr (std::is_same<T, bf16>::value)
+        if (type == SMOL_ELEM_BF16)
+            return f(bf16{});
+    return type == SMOL_ELEM_F32 ? f(float{}) : f(f16{});
+}
+
+// Launchers, one file per type of the weight (smol_patch_<type>.hip). tile:
+// index of a tile shape. Return a hipError_t as int.
+int launch_patch_f32(const PatchArgs &a, int image_type, int mode, int tile, void *stream);
+int launch_patch_f16(const PatchArgs &a, int image_type, int mode, int tile, void *stream);
+int launch_patch_bf16(const PatchArgs &a, int image_type, int mode, int tile, void *stream);
+int launch_patch_grad_f32(const PatchArgs &a, int image_type, int mode, int tile, void *stream);
+int launch_patch_grad_f16(const PatchArgs &a, int image_type, int mode, int tile, void *stream);
+int launch_patch_grad_bf16(const PatchArgs &a, int image_type, int mode, int tile, void *stream);
+
+}  // namespace smol
+
+#endif  // SMOL_PATCH_H

@@ -1,0 +1,404 @@
+// smol_patch.hip -- patch embedding and its backward pass (smol_patch_embed,
+// smol_patch_embed_backward): argument checks, the choice of tiles, and the
+// backward pass's column sums and joins. The matrix products are in
+// smol_patch_kernels.h.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "smol.h"
+#include "smol_internal.h"
+#include "smol_patch.h"
+
+namespace smol {
+namespace {
+
+// Column sums of grad_out over the images of a part, for every token: V
+// columns a thread. sums[part][token][column].
+struct SumArgs {
+    const void *grad_out;
+    float *sums;
+    int64_t image_stride, row_stride;
+    uint32_t n, tokens, dim, part_images;
+    Divisor columns;  // groups of V columns in a row
+};
+
+template <typename T, int V>
+__global__ void __launch_bounds__(256) patch_sum_kernel(SumArgs a)
+{
+    const uint32_t e = blockIdx.x * 256 + threadIdx.x;
+    const uint32_t t = divide(e, a.columns), col = (e - t * a.columns.d) * V;
+    if (t >= a.tokens)
+        return;
+    const uint32_t at = col <= a.dim - V ? col : a.dim - V;
+    const uint32_t lo = blockIdx.y * a.part_images;
+    const uint32_t hi = a.n - lo < a.part_images ? a.n : lo + a.part_images;
+    const T *p = (const T *)a.grad_out + (int64_t)t * a.row_stride + at;
+    vec<float, V> sum = (vec<float, V>)0.0f;
+#pragma unroll 8
+    for (uint32_t i = lo; i < hi; ++i)
+        sum += to_f32<V, T>(load<T, V>(p + i * a.image_stride));
+    // columns of a group moved back are written twice, alike
+    store<float, V>(a.sums + ((int64_t)blockIdx.y * a.tokens + t) * a.dim + at, sum);
+}
+
+// Joins: the first workgroups add the splits of the weight's gradient, the
+// next the parts of the positions', the last the bias's (over parts and
+// tokens; 16 columns a workgroup, 16 threads a column).
+struct JoinArgs {
+    PatchArgs patch;
+    const float *part, *sums;
+    void *weight, *pos, *bias;
+    uint32_t tokens, parts;
+    uint32_t weight_groups, pos_groups;
+    Divisor chunks;
+    int32_t accumulate;
+};
+
+template <typename P, int C>
+__global__ void __launch_bounds__(256) patch_join_kernel(JoinArgs a)
+{
+    const uint32_t dim = a.patch.dim;
+    if (blockIdx.x < a.weight_groups) {
+        const uint32_t e = blockIdx.x * 256 + threadIdx.x;
+        const uint32_t d = divide(e, a.chunks), q = e - d * a.chunks.d;
+        if (d >= dim)
+            return;
+        const Chunk<C> c(a.patch, q);
+        const int64_t width = (int64_t)a.patch.chunks * C;
+        const float *p = a.part + d * width + q * C;
+        vec<float, C> sum = (vec<float, C>)0.0f;
+#pragma unroll 4
+        for (uint32_t s = 0; s < a.patch.splits; ++s)
+            sum += load<float, C>(p + s * dim * width);
+        P *out = (P *)a.weight + (int64_t)d * a.patch.values + c.weight;
+#pragma unroll
+        for (int k = 0; k < C; ++k)
+            if (k >= c.lead && k < c.have)
+                out[k] = (P)(a.accumulate ? (float)out[k] + sum[k] : sum[k]);
+        return;
+    }
+    if (blockIdx.x < a.weight_groups + a.pos_groups) {
+        const uint32_t e = (blockIdx.x - a.weight_groups) * 256 + threadIdx.x;
+        const uint32_t count = a.tokens * dim;
+        if (e >= count)
+            return;
+        float sum = 0.0f;
+#pragma unroll 4
+        for (uint32_t s = 0; s < a.parts; ++s)
+            sum += a.sums[(int64_t)s * count + e];
+        P *out = (P *)a.pos + e;
+        *out = (P)(a.accumulate ? (float)*out + sum : sum);
+        return;
+    }
+    __shared__ float rows[16][17];
+    const uint32_t d = (blockIdx.x - a.weight_groups - a.pos_groups) * 16 + (threadIdx.x & 15);
+    const uint32_t q = threadIdx.x >> 4;
+    float sum = 0.0f;
+    if (d < dim)
+#pragma unroll 8
+        for (uint32_t r = q; r < a.parts * a.tokens; r += 16)
+            sum += a.sums[(int64_t)r * dim + d];
+    rows[q][threadIdx.x & 15] = sum;
+    __syncthreads();
+    if (q != 0 || d >= dim)
+        return;
+    for (int k = 1; k < 16; ++k)
+        sum += rows[k][threadIdx.x];
+    P *out = (P *)a.bias + d;
+    *out = (P)(a.accumulate ? (float)*out + sum : sum);
+}
+
+// What a shape amounts to.
+struct Plan {
+    PatchArgs a;  // without pointers, strides and tiles
+    uint32_t tokens;
+    int mode;
+};
+
+int plan_of(const smol_patch_shape &s, Plan *plan)
+{
+    if (s.n < 0 || s.channels < 1 || s.height < 1 || s.width < 1 || s.patch < 1 || s.dim < 1)
+        return set_error(SMOL_ERR_INVALID_ARG, "a size of the shape is out of range");
+    if (s.layout != SMOL_LAYOUT_NCHW && s.layout != SMOL_LAYOUT_NHWC)
+        return set_error(SMOL_ERR_INVALID_ARG, "layout %d unknown", s.layout);
+    if (s.type < SMOL_ELEM_F32 || s.type > SMOL_ELEM_BF16)
+        return set_error(SMOL_ERR_INVALID_ARG, "type %d unknown", s.type);
+    if (s.image_type < SMOL_ELEM_F32 || s.image_type > SMOL_ELEM_BF16 ||
+        (s.image_type == SMOL_ELEM_BF16 && s.type != SMOL_ELEM_BF16))
+        return set_error(SMOL_ERR_INVALID_ARG, "image_type %d does not go with type %d",
+                         s.image_type, s.type);
+    for (int32_t r : s.reserved)
+        if (r)
+            return set_error(SMOL_ERR_INVALID_ARG, "reserved fields are not zero");
+    const bool sides = s.height <= SMOL_MAX_DIM && s.width <= SMOL_MAX_DIM &&
+                       s.patch <= SMOL_MAX_PATCH && s.channels <= SMOL_MAX_PATCH_VALUES &&
+                       s.dim <= SMOL_MAX_PATCH_DIM;  // no product below overflows
+    const int64_t values = sides ? (int64_t)s.channels * s.patch * s.patch : 0;
+    const int64_t image = sides ? (int64_t)s.channels * s.height * s.width : 0;
+    const int64_t th = s.height / s.patch, tw = s.width / s.patch;
+    if (!sides || values > SMOL_MAX_PATCH_VALUES || values * s.dim >= INT32_MAX ||
+        image >= INT32_MAX || th * tw * s.n > SMOL_MAX_ROWS || th * tw * s.dim >= INT32_MAX)
+        return set_error(SMOL_ERR_UNSUPPORTED,
+                         "%d images of %d x %d x %d, patches of %d, %d columns: beyond the limits",
+                         s.n, s.channels, s.height, s.width, s.patch, s.dim);
+    const bool nhwc = s.layout == SMOL_LAYOUT_NHWC;
+    const int C = 16 / elem_size(s.type);
+    PatchArgs &a = plan->a;
+    a = PatchArgs{};
+    plan->tokens = (uint32_t)(th * tw);
+    a.image_size = image;
+    a.rows = (uint32_t)(th * tw * s.n);
+    a.dim = (uint32_t)s.dim;
+    a.values = (uint32_t)values;
+    a.length = (uint32_t)(nhwc ? s.patch * s.channels : s.patch);
+    const uint32_t per_run = (a.length + C - 1) / C;
+    a.chunks = per_run * (a.values / a.length);
+    a.step_x = a.length;
+    a.pitch = (uint32_t)(nhwc ? s.width * s.channels : s.width);
+    a.step_y = (uint32_t)s.patch * a.pitch;
+    a.plane = (uint32_t)s.height * (uint32_t)s.width;
+    a.tokens = make_divisor(plan->tokens ? plan->tokens : 1);
+    a.across = make_divisor(tw ? (uint32_t)tw : 1);
+    a.per_run = make_divisor(per_run);
+    // channels-last runs belong to no channel
+    a.per_channel = make_divisor(nhwc ? SMOL_MAX_PATCH_VALUES : (uint32_t)s.patch);
+    plan->mode = a.length < (uint32_t)C           ? kShort
+                 : a.length % C || a.chunks % 8 ? kMasked
+                                                : kWhole;
+    return SMOL_OK;
+}
+
+void set_tiles(PatchArgs *a, uint32_t rows, uint32_t cols)
+{
+    a->tiles = rows * cols;
+    a->tiles_n = make_divisor(cols);
+}
+
+uint32_t ceil_div(uint32_t n, uint32_t d) { return (n + d - 1) / d; }
+
+// The backward pass's parts. A part of the rows costs its partial products a
+// write and a read, so there are only as many as fill the chip.
+struct GradPlan {
+    int tile;
+    uint32_t parts, part_images;
+    int64_t sums, bytes;  // offset of the column sums; workspace bytes
+};
+
+GradPlan grad_plan(const smol_patch_shape &s, Plan *plan)
+{
+    PatchArgs &a = plan->a;
+    const int C = 16 / elem_size(s.type), rows_a_step = C * 8;
+    const uint32_t width = a.chunks * C;
+    GradPlan g;
+    g.tile = 4;
+    set_tiles(&a, ceil_div(a.dim, 128), ceil_div(width, 128));
+    const uint32_t steps = ceil_div(a.rows, rows_a_step);
+    if (a.tiles * ceil_div(steps, 8) < 256) {
+        g.tile = 2;
+        set_tiles(&a, ceil_div(a.dim, 64), ceil_div(width, 64));
+    }
+    uint32_t splits = a.tiles < 512 ? 512 / a.tiles : 1;
+    if (splits > ceil_div(steps, 4))
+        splits = ceil_div(steps, 4);
+    a.split_rows = splits ? ceil_div(steps, splits) * rows_a_step : rows_a_step;
+    a.splits = ceil_div(a.rows, a.split_rows);
+    const uint32_t V = a.dim >= 8 ? 8 : 1, threads = plan->tokens * ceil_div(a.dim, V);
+    uint32_t parts = threads ? ceil_div(2048 * 64, threads) : 0;
+    if (parts > (uint32_t)s.n)
+        parts = (uint32_t)s.n;
+    g.part_images = parts ? ceil_div((uint32_t)s.n, parts) : 1;
+    g.parts = parts ? ceil_div((uint32_t)s.n, g.part_images) : 0;
+    g.sums = ((int64_t)a.splits * a.dim * width * 4 + 15) / 16 * 16;
+    g.bytes = g.sums + (int64_t)g.parts * plan->tokens * a.dim * 4 + 16;
+    return g;
+}
+
+int check_tensor(const char *name, const void *p, int type)
+{
+    if (!p || (uintptr_t)p % elem_size(type))
+        return set_error(SMOL_ERR_INVALID_ARG, "%s is NULL or not aligned to its elements", name);
+    return SMOL_OK;
+}
+
+// Strides of n images' rows; written rows may not overlap.
+int check_strides(const char *name, int64_t image_stride, int64_t row_stride, int64_t n,
+                  int64_t tokens, int64_t dim, bool written)
+{
+    const int64_t most = INT64_MAX / 16 / (n * tokens);
+    bool ok = image_stride >= 0 && row_stride >= 0 && image_stride <= most && row_stride <= most;
+    if (ok && written) {
+        const int64_t span_rows = (tokens - 1) * row_stride + dim;
+        const int64_t span_images = (n - 1) * image_stride + dim;
+        const bool rows_apart = tokens == 1 || row_stride >= dim;
+        const bool images_apart = n == 1 || image_stride >= dim;
+        ok = rows_apart && images_apart &&
+             (n == 1 || tokens == 1 || image_stride >= span_rows || row_stride >= span_images);
+    }
+    if (!ok)
+        return set_error(SMOL_ERR_INVALID_ARG, "%s: strides %lld, %lld out of range", name,
+                         (long long)image_stride, (long long)row_stride);
+    return SMOL_OK;
+}
+
+}  // namespace
+}  // namespace smol
+
+extern "C" int smol_patch_embed(const smol_patch_args *p, void *stream)
+{
+    using namespace smol;
+    clear_error();
+    if (!p)
+        return set_error(SMOL_ERR_INVALID_ARG, "args is NULL");
+    const smol_patch_shape &s = p->shape;
+    Plan plan;
+    int st = plan_of(s, &plan);
+    if (st != SMOL_OK)
+        return st;
+    PatchArgs &a = plan.a;
+    if (a.rows == 0)
+        return SMOL_OK;
+    if ((st = check_tensor("images", p->images, s.image_type)) != SMOL_OK ||
+        (st = check_tensor("weight", p->weight, s.type)) != SMOL_OK ||
+        (p->bias && (st = check_tensor("bias", p->bias, s.type)) != SMOL_OK) ||
+        (p->pos && (st = check_tensor("pos", p->pos, s.type)) != SMOL_OK) ||
+        (st = check_tensor("out", p->out, s.type)) != SMOL_OK ||
+        (st = check_strides("out", p->image_stride, p->row_stride, s.n, plan.tokens, s.dim,
+                            true)) != SMOL_OK)
+        return st;
+    a.images = p->images;
+    a.weight = p->weight;
+    a.bias = p->bias;
+    a.pos = p->pos;
+    a.out = p->out;
+    a.image_stride = p->image_stride;
+    a.row_stride = p->row_stride;
+    // the largest tile that leaves no compute unit without one
+    int tile = 4;
+    for (; tile > 1; tile /= 2) {
+        set_tiles(&a, ceil_div(a.rows, 32 * tile), ceil_div(a.dim, 32 * tile));
+        if (a.tiles >= 256)
+            break;
+    }
+    if (tile == 1)
+        set_tiles(&a, ceil_div(a.rows, 32), ceil_div(a.dim, 32));
+    const int e = (s.type == SMOL_ELEM_F32   ? launch_patch_f32
+                   : s.type == SMOL_ELEM_F16 ? launch_patch_f16
+                                             : launch_patch_bf16)(a, s.image_type, plan.mode, tile,
+                                                                  stream);
+    if (e != hipSuccess)
+        return set_error(SMOL_ERR_HIP, "patch embedding launch: %s",
+                         hipGetErrorString((hipError_t)e));
+    return SMOL_OK;
+}
+
+extern "C" int64_t smol_patch_workspace_bytes(const smol_patch_shape *shape)
+{
+    using namespace smol;
+    Plan plan;
+    if (!shape || plan_of(*shape, &plan) != SMOL_OK)
+        return 0;
+    return grad_plan(*shape, &plan).bytes;
+}
+
+extern "C" int smol_patch_embed_backward(const smol_patch_grad_args *p, void *stream)
+{
+    using namespace smol;
+    clear_error();
+    if (!p)
+        return set_error(SMOL_ERR_INVALID_ARG, "args is NULL");
+    const smol_patch_shape &s = p->shape;
+    Plan plan;
+    int st = plan_of(s, &plan);
+    if (st != SMOL_OK)
+        return st;
+    if (p->grad_type != SMOL_ELEM_F32 && p->grad_type != s.type)
+        return set_error(SMOL_ERR_INVALID_ARG, "grad_type %d is neither fp32 nor the type",
+                         p->grad_type);
+    if (p->accumulate != 0 && p->accumulate != 1)
+        return set_error(SMOL_ERR_INVALID_ARG, "accumulate %d is neither 0 nor 1", p->accumulate);
+    PatchArgs &a = plan.a;
+    if (a.rows > 0 &&
+        ((st = check_tensor("grad_out", p->grad_out, s.type)) != SMOL_OK ||
+         (st = check_strides("grad_out", p->image_stride, p->row_stride, s.n, plan.tokens, s.dim,
+                             false)) != SMOL_OK ||
+         (p->grad_weight && (st = check_tensor("images", p->images, s.image_type)) != SMOL_OK)))
+        return st;
+    if ((p->grad_weight &&
+         (st = check_tensor("grad_weight", p->grad_weight, p->grad_type)) != SMOL_OK) ||
+        (p->grad_bias && (st = check_tensor("grad_bias", p->grad_bias, p->grad_type)) != SMOL_OK) ||
+        (p->grad_pos && (st = check_tensor("grad_pos", p->grad_pos, p->grad_type)) != SMOL_OK))
+        return st;
+    const GradPlan g = grad_plan(s, &plan);
+    if (!p->workspace || (uintptr_t)p->workspace % 16 || p->workspace_bytes < g.bytes)
+        return set_error(SMOL_ERR_INVALID_ARG,
+                         "workspace must be 16-byte aligned and hold %lld bytes",
+                         (long long)g.bytes);
+    if (!p->grad_weight && !p->grad_bias && !p->grad_pos)
+        return SMOL_OK;
+    hipStream_t hs = (hipStream_t)stream;
+    float *part = (float *)p->workspace, *sums = (float *)((char *)p->workspace + g.sums);
+    a.images = p->images;
+    a.grad_out = p->grad_out;
+    a.out = part;
+    a.image_stride = p->image_stride;
+    a.row_stride = p->row_stride;
+    int e = hipSuccess;
+    if (p->grad_weight && a.rows > 0)
+        e = (s.type == SMOL_ELEM_F32   ? launch_patch_grad_f32
+             : s.type == SMOL_ELEM_F16 ? launch_patch_grad_f16
+                                       : launch_patch_grad_bf16)(a, s.image_type, plan.mode,
+                                                                 g.tile, stream);
+    if (e == hipSuccess && (p->grad_bias || p->grad_pos) && g.parts > 0) {
+        SumArgs b;
+        b.grad_out = p->grad_out;
+        b.sums = sums;
+        b.image_stride = p->image_stride;
+        b.row_stride = p->row_stride;
+        b.n = (uint32_t)s.n;
+        b.tokens = plan.tokens;
+        b.dim = a.dim;
+        b.part_images = g.part_images;
+        const uint32_t V = a.dim >= 8 ? 8 : 1;
+        b.columns = make_divisor(ceil_div(a.dim, V));
+        const dim3 grid(ceil_div(plan.tokens * b.columns.d, 256), g.parts);
+        with_type(s.type, [&](auto t) {
+            typedef decltype(t) T;
+            if (V == 8)
+                hipLaunchKernelGGL((patch_sum_kernel<T, 8>), grid, dim3(256), 0, hs, b);
+            else
+                hipLaunchKernelGGL((patch_sum_kernel<T, 1>), grid, dim3(256), 0, hs, b);
+        });
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess) {
+        JoinArgs j;
+        j.patch = a;
+        j.part = part;
+        j.sums = sums;
+        j.weight = p->grad_weight;
+        j.pos = p->grad_pos;
+        j.bias = p->grad_bias;
+        j.tokens = plan.tokens;
+        j.parts = g.parts;
+        j.chunks = make_divisor(a.chunks);
+        j.accumulate = p->accumulate;
+        j.weight_groups =
+            p->grad_weight ? (uint32_t)(((int64_t)a.dim * a.chunks + 255) / 256) : 0;
+        j.pos_groups = p->grad_pos ? ceil_div(plan.tokens * a.dim, 256) : 0;
+        const dim3 grid(j.weight_groups + j.pos_groups +
+                        (p->grad_bias ? ceil_div(a.dim, 16) : 0));
+        if (grid.x > 0)
+            with_type(p->grad_type, [&](auto t) {
+                typedef decltype(t) P;
+                if (elem_size(s.type) == 4)
+                    hipLaunchKernelGGL((patch_join_kernel<P, 4>), grid, dim3(256), 0, hs, j);
+                else
+                    hipLaunchKernelGGL((patch_join_kernel<P, 8>), grid, dim3(256), 0, hs, j);
+            });
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess)
+        return set_error(SMOL_ERR_HIP, "patch embedding backward launch: %s",
+                         hipGetErrorString((hipError_t)e));
+    return SMOL_OK;
+}

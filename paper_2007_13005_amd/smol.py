@@ -179,6 +179,16 @@ SIGNATURES = {
     "smol_jpeg_entropy_decode_batch": (ctypes.c_int, [_vp, ctypes.c_int64, _vp, _vp,
                                                       ctypes.c_int32, _vp, _vp, ctypes.c_int64,
                                                       _vp, ctypes.c_int32, _vp, ctypes.c_int32]),
+    "smol_patch_embed": (ctypes.c_int, [_vp, _vp]),
+    "smol_patch_embed_backward": (ctypes.c_int, [_vp, _vp]),
+    "smol_patch_workspace_bytes": (ctypes.c_int64, [_vp]),
+    "smol_embed": (ctypes.c_int, [_vp, _vp]),
+    "smol_embed_backward": (ctypes.c_int, [_vp, _vp]),
+    "smol_embed_workspace_bytes": (ctypes.c_int64, [ctypes.c_int64, ctypes.c_int64,
+                                                    ctypes.c_int32]),
+    "smol_layer_norm": (ctypes.c_int, [_vp, _vp]),
+    "smol_layer_norm_backward": (ctypes.c_int, [_vp, _vp]),
+    "smol_norm_workspace_bytes": (ctypes.c_int64, [ctypes.c_int64, ctypes.c_int32]),
     "smol_stream_probe": (ctypes.c_int, [_vp, ctypes.c_uint64, _vp, ctypes.c_uint64,
                                          ctypes.c_int32, ctypes.c_int32, _vp]),
     "smol_valu_probe": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp, _vp]),
