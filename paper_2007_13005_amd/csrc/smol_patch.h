@@ -88,28 +88,54 @@ struct Chunk {
 };
 
 // Sets a chunk's first `lead` values to zero.
-template <typename T, int C>
-__device__ __forceinline__ vec<T, C> masked(vec<T, C> v, int32_t lead)
+struct Mask {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    u32x4 keep;
+};
+template <int C>
+__device__ __forceinline__ Mask mask_of(int32_t lead)
 {
+    Mask m;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (C == 4)
+            m.keep[w] = w >= lead ? ~0u : 0u;
+        else
+            m.keep[w] = (2 * w >= lead ? 0xffffu : 0u) | (2 * w + 1 >= lead ? 0xffff0000u : 0u);
+    }
+    return m;
+}
+template <typename V>
+__device__ __forceinline__ V masked(V v, const Mask &m)
+{
+    return __builtin_bit_cast(V, __builtin_bit_cast(Mask::u32x4, v) & m.keep);
+}
+
+// C elements from p; Short: only the first `have` exist. The second form takes
+// an offset in bytes below 2^32 from a base that the wave shares.
+template <typename S, int C, bool Short>
+__device__ __forceinline__ vec<S, C> load_chunk(const S *p, int32_t have)
+{
+    if (!Short)
+        return load<S, C>(p);
+    vec<S, C> v;
 #pragma unroll
     for (int e = 0; e < C; ++e)
-        v[e] = e >= lead ? v[e] : (T)0.0f;
+        v[e] = e < have ? p[e] : (S)0.0f;
     return v;
 }
 
-// C elements from p as type T; Short: only the first `have` exist.
-template <typename S, typename T, int C, bool Short>
-__device__ __forceinline__ vec<T, C> load_chunk(const S *p, int32_t have)
+template <typename S, int C, bool Short>
+__device__ __forceinline__ vec<S, C> load_chunk(const void *base, uint32_t bytes, int32_t have)
 {
-    vec<S, C> v;
-    if (Short) {
-#pragma unroll
-        for (int e = 0; e < C; ++e)
-            v[e] = e < have ? p[e] : (S)0.0f;
-    } else {
-        v = load<S, C>(p);
-    }
-    if constexpr (sizeof(S) == sizeof(T) && std::is_same<S, T>::value)
+    return load_chunk<S, C, Short>((const S *)((const char *)base + bytes), have);
+}
+
+// To the weight's type.
+template <typename T, typename S, int C>
+__device__ __forceinline__ vec<T, C> rounded(vec<S, C> v)
+{
+    if constexpr (std::is_same<S, T>::value)
         return v;
     else
         return from_f32<T, C>(to_f32<C, S>(v));

@@ -176,6 +176,38 @@ void set_tiles(PatchArgs *a, uint32_t rows, uint32_t cols)
 
 uint32_t ceil_div(uint32_t n, uint32_t d) { return (n + d - 1) / d; }
 
+// The tile side of a forward call: the least of the times that the sides take
+// for patches of 768 values (the sides' times grow alike with the values).
+// Measured, us, for 224 x 224 images to 768 columns, sides 32 / 128 / 256:
+//   fp16, images   1: 4.9 / 12.4 / 24.0     8: 12.9 / 12.9 / 25.5
+//                 32: 39.5 / 18.9 / 27.0   64: 69.2 / 29.7 / 28.7
+//                 96: 103 / 36.0 / 30.2   128: 134 / 49.6 / 53.7
+//   fp32, images   1: 9.8 / 57.5   16: 53.3 / 61.1   64: 179 / 159
+// (32: a few tiles at once; 128: two a compute unit, one for the first 256;
+// 256: one). Rows of a large tile must lie within 2^32 bytes.
+int forward_tile(const smol_patch_shape &s, const Plan &plan)
+{
+    const PatchArgs &a = plan.a;
+    const auto tiles = [&](uint32_t side) {
+        return (double)ceil_div(a.rows, side) * ceil_div(a.dim, side);
+    };
+    const auto rounds = [](double n, double at_once) {
+        const double r = n / at_once;
+        return (double)(int64_t)r < r ? (double)(int64_t)r + 1 : r;
+    };
+    const double cus = device_cus() > 0 ? device_cus() : 256;
+    const int64_t span = (int64_t)(256 / plan.tokens + 2) * a.image_size * elem_size(s.image_type);
+    if (span > UINT32_MAX)
+        return 32;
+    if (s.type == SMOL_ELEM_F32)
+        return 5 + tiles(32) / 53 <= 4 + 53 * rounds(tiles(128), cus) ? 32 : 128;
+    const double t32 = 4 + tiles(32) / 140;
+    const double t128 = tiles(128) <= cus ? 13 : 3 + 16 * rounds(tiles(128), 2 * cus);
+    const bool large = plan.mode != kShort && elem_size(s.image_type) == 2;
+    const double t256 = large ? 1 + 25 * rounds(tiles(256), cus) : 1e30;
+    return t32 <= t128 && t32 <= t256 ? 32 : t128 <= t256 ? 128 : 256;
+}
+
 // The backward pass's parts. A part of the rows costs its partial products a
 // write and a read, so there are only as many as fill the chip.
 struct GradPlan {
@@ -272,15 +304,8 @@ extern "C" int smol_patch_embed(const smol_patch_args *p, void *stream)
     a.out = p->out;
     a.image_stride = p->image_stride;
     a.row_stride = p->row_stride;
-    // the largest tile that leaves no compute unit without one
-    int tile = 4;
-    for (; tile > 1; tile /= 2) {
-        set_tiles(&a, ceil_div(a.rows, 32 * tile), ceil_div(a.dim, 32 * tile));
-        if (a.tiles >= 256)
-            break;
-    }
-    if (tile == 1)
-        set_tiles(&a, ceil_div(a.rows, 32), ceil_div(a.dim, 32));
+    const int tile = forward_tile(s, plan);
+    set_tiles(&a, ceil_div(a.rows, tile), ceil_div(a.dim, tile));
     const int e = (s.type == SMOL_ELEM_F32   ? launch_patch_f32
                    : s.type == SMOL_ELEM_F16 ? launch_patch_f16
                                              : launch_patch_bf16)(a, s.image_type, plan.mode, tile,

@@ -354,6 +354,11 @@ PATCHES = [  # n, c, h, w, p, dim, nhwc
     (7, 3, 60, 40, 20, 33, True), (1, 5, 33, 61, 11, 129, False), (64, 3, 32, 32, 16, 4, False),
     (4, 3, 64, 100, 4, 24, True), (2, 3, 96, 96, 24, 200, False), (2, 3, 7, 7, 8, 16, False),
     (9, 3, 130, 131, 13, 300, False), (40, 3, 112, 112, 14, 384, False)]
+# enough rows for the larger tiles: whole chunks, repeated values, short runs;
+# ragged last tiles both ways
+LARGE = [(33, 3, 160, 176, 16, 1000, False), (70, 3, 140, 154, 14, 520, False),
+         (61, 3, 112, 120, 14, 776, True), (130, 2, 63, 70, 7, 264, False),
+         (97, 3, 224, 224, 16, 768, False), (260, 1, 112, 112, 8, 1030, True)]
 KINDS = [(F32, F32), (F16, F32), (F16, F16), (F32, F16), (F16, BF16), (F32, BF16), (BF16, BF16)]
 
 
@@ -393,6 +398,21 @@ def test_patch_embed(case, image, dtype):
     assert torch.equal(seq.transpose(0, 1), out)
 
 
+@pytest.mark.parametrize("case", LARGE)
+@pytest.mark.parametrize("image, dtype", KINDS)
+def test_patch_embed_large(case, image, dtype):
+    """The same bounds, from 64 bits on the device."""
+    note(f"patch {case} {image} {dtype}")
+    n, c, h, w, p, dim, nhwc = case
+    g, img, weight, t = patch_inputs(case, image, dtype, dim)
+    layout = tokens.LAYOUT_NHWC if nhwc else tokens.LAYOUT_NCHW
+    bias, pos = randn(g, dim, dtype=dtype), randn(g, t, dim, dtype=dtype)
+    args = [x.cuda() for x in (img, weight, bias, pos)]
+    out = tokens.patch_embed(*args, layout=layout)
+    want, bound = ref.patch_embed(*args, nhwc)
+    ref.close(out, want.cpu(), bound.cpu(), "patch")
+
+
 @pytest.mark.parametrize("case", PATCHES)
 @pytest.mark.parametrize("image, dtype", KINDS)
 def test_patch_gradient(case, image, dtype):
@@ -426,6 +446,22 @@ def test_patch_gradient(case, image, dtype):
         tokens.patch_embed_backward(one, dev(img), first, layout=layout)
         tokens.patch_embed_backward(one.contiguous(), dev(img), base, layout=layout)
         assert torch.equal(first, base)
+
+
+@pytest.mark.parametrize("case", LARGE)
+@pytest.mark.parametrize("image, dtype", KINDS)
+def test_patch_gradient_large(case, image, dtype):
+    note(f"patch grad {case} {image} {dtype}")
+    n, c, h, w, p, dim, nhwc = case
+    g, img, weight, t = patch_inputs(case, image, dtype, dim + 1)
+    layout = tokens.LAYOUT_NHWC if nhwc else tokens.LAYOUT_NCHW
+    dy, img = randn(g, n, t, dim, dtype=dtype).cuda(), img.cuda()
+    got = [torch.empty(s, device="cuda") for s in (weight.shape, (dim,), (t, dim))]
+    tokens.patch_embed_backward(dy, img, *got, layout=layout)
+    want, bound = ref.patch_embed_backward(dy, img, p, nhwc)
+    got[0] = got[0].view(dim, -1)
+    for a, e, b, name in zip(got, want, bound, ("weight", "bias", "pos")):
+        ref.close(a, e.cpu(), b.cpu(), f"patch grad {name}")
 
 
 def test_patch_no_images():
