@@ -141,25 +141,33 @@ __device__ __forceinline__ vec<T, C> rounded(vec<S, C> v)
         return from_f32<T, C>(to_f32<C, S>(v));
 }
 
-// The product of a lane's 16 bytes of each operand (16 rows a side, the
-// lanes' fourths of the wave holding different values of the summed index),
-// added to a 16 x 16 tile in fp32: lane l has rows 4 (l / 16) .. + 3 of the
-// first operand, column l % 16 of the second.
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ f32x4 mma(vec<f16, 8> a, vec<f16, 8> b, f32x4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mma(vec<bf16, 8> a, vec<bf16, 8> b, f32x4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mma(vec<float, 4> a, vec<float, 4> b, f32x4 c)
+
+// The products of N first operands with one second operand, or the other way
+// round (Swap), each added to a 16 x 16 tile in fp32. A lane has 16 bytes of
+// each operand, of one of its 16 rows; the four quarters of the wave hold
+// different values of the summed index. Lane l of a result has rows 4 (l / 16)
+// .. + 3 of the first operand, column l % 16 of the second.
+template <bool Swap, int N, typename V>
+__device__ __forceinline__ void multiply(f32x4 *const (&sum)[N], const V (&many)[N], const V &one)
 {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
-    return c;
+    for (int i = 0; i < N; ++i) {
+        const V a = Swap ? one : many[i], b = Swap ? many[i] : one;
+        if constexpr (std::is_same<V, vec<f16, 8>>::value)
+            *sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, *sum[i], 0, 0, 0);
+        else if constexpr (std::is_same<V, vec<bf16, 8>>::value)
+            *sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, *sum[i], 0, 0, 0);
+    }
+    if constexpr (std::is_same<V, vec<float, 4>>::value) {
+        // the N tiles in turn: an instruction does not wait for the last
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                *sum[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                    Swap ? one[e] : many[i][e], Swap ? many[i][e] : one[e], *sum[i], 0, 0, 0);
+    }
 }
 
 // Workgroup b's piece of work of `count`: workgroups are dealt out to the

@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(256) patch_sum_kernel(SumArgs a)
 
 // Joins: the first workgroups add the splits of the weight's gradient, the
 // next the parts of the positions', the last the bias's (over parts and
-// tokens; 16 columns a workgroup, 16 threads a column).
+// tokens; 8 columns a workgroup, 32 threads a column).
 struct JoinArgs {
     PatchArgs patch;
     const float *part, *sums;
@@ -83,26 +83,26 @@ __global__ void __launch_bounds__(256) patch_join_kernel(JoinArgs a)
         if (e >= count)
             return;
         float sum = 0.0f;
-#pragma unroll 4
+#pragma unroll 8
         for (uint32_t s = 0; s < a.parts; ++s)
             sum += a.sums[(int64_t)s * count + e];
         P *out = (P *)a.pos + e;
         *out = (P)(a.accumulate ? (float)*out + sum : sum);
         return;
     }
-    __shared__ float rows[16][17];
-    const uint32_t d = (blockIdx.x - a.weight_groups - a.pos_groups) * 16 + (threadIdx.x & 15);
-    const uint32_t q = threadIdx.x >> 4;
+    __shared__ float rows[32][9];
+    const uint32_t d = (blockIdx.x - a.weight_groups - a.pos_groups) * 8 + (threadIdx.x & 7);
+    const uint32_t q = threadIdx.x >> 3;
     float sum = 0.0f;
     if (d < dim)
 #pragma unroll 8
-        for (uint32_t r = q; r < a.parts * a.tokens; r += 16)
+        for (uint32_t r = q; r < a.parts * a.tokens; r += 32)
             sum += a.sums[(int64_t)r * dim + d];
-    rows[q][threadIdx.x & 15] = sum;
+    rows[q][threadIdx.x & 7] = sum;
     __syncthreads();
     if (q != 0 || d >= dim)
         return;
-    for (int k = 1; k < 16; ++k)
+    for (int k = 1; k < 32; ++k)
         sum += rows[k][threadIdx.x];
     P *out = (P *)a.bias + d;
     *out = (P)(a.accumulate ? (float)*out + sum : sum);
@@ -222,22 +222,23 @@ GradPlan grad_plan(const smol_patch_shape &s, Plan *plan)
     const int C = 16 / elem_size(s.type), rows_a_step = C * 8;
     const uint32_t width = a.chunks * C;
     GradPlan g;
-    g.tile = 4;
-    set_tiles(&a, ceil_div(a.dim, 128), ceil_div(width, 128));
     const uint32_t steps = ceil_div(a.rows, rows_a_step);
-    if (a.tiles * ceil_div(steps, 8) < 256) {
-        g.tile = 2;
-        set_tiles(&a, ceil_div(a.dim, 64), ceil_div(width, 64));
-    }
-    uint32_t splits = a.tiles < 512 ? 512 / a.tiles : 1;
+    if (s.dim < C)
+        plan->mode = kShort;
+    const bool large = plan->mode != kShort && elem_size(s.image_type) == 2 && C == 8;
+    g.tile = large ? 256 : 128;
+    const uint32_t at_once = g.tile == 256 || C == 4 ? 256 : 512;
+    set_tiles(&a, ceil_div(a.dim, g.tile), ceil_div(width, g.tile));
+    uint32_t splits = a.tiles < at_once ? at_once / a.tiles : 1;
     if (splits > ceil_div(steps, 4))
         splits = ceil_div(steps, 4);
     a.split_rows = splits ? ceil_div(steps, splits) * rows_a_step : rows_a_step;
     a.splits = ceil_div(a.rows, a.split_rows);
     const uint32_t V = a.dim >= 8 ? 8 : 1, threads = plan->tokens * ceil_div(a.dim, V);
     uint32_t parts = threads ? ceil_div(2048 * 64, threads) : 0;
-    if (parts > (uint32_t)s.n)
-        parts = (uint32_t)s.n;
+    // a part's sums are written and read again: eight images at least
+    if (parts > ceil_div((uint32_t)s.n, 8))
+        parts = ceil_div((uint32_t)s.n, 8);
     g.part_images = parts ? ceil_div((uint32_t)s.n, parts) : 1;
     g.parts = parts ? ceil_div((uint32_t)s.n, g.part_images) : 0;
     g.sums = ((int64_t)a.splits * a.dim * width * 4 + 15) / 16 * 16;
@@ -411,7 +412,7 @@ extern "C" int smol_patch_embed_backward(const smol_patch_grad_args *p, void *st
             p->grad_weight ? (uint32_t)(((int64_t)a.dim * a.chunks + 255) / 256) : 0;
         j.pos_groups = p->grad_pos ? ceil_div(plan.tokens * a.dim, 256) : 0;
         const dim3 grid(j.weight_groups + j.pos_groups +
-                        (p->grad_bias ? ceil_div(a.dim, 16) : 0));
+                        (p->grad_bias ? ceil_div(a.dim, 8) : 0));
         if (grid.x > 0)
             with_type(p->grad_type, [&](auto t) {
                 typedef decltype(t) P;

@@ -208,9 +208,11 @@ __global__ void __launch_bounds__(64 * WD * WM, 2) patch_kernel(PatchArgs a)
                 fp[g + 2] = read_p(buffer, (g + 2) / FM, (g + 2) % FM);
             if (g >= FM - FD && g < FM)
                 fw[1][g - FM + FD] = read_w(buffer, 1, g - FM + FD);
+            f32x4 *into[FD];
 #pragma unroll
             for (int i = 0; i < FD; ++i)
-                sum[i][g % FM] = mma(fw[g / FM][i], fp[g], sum[i][g % FM]);
+                into[i] = &sum[i][g % FM];
+            multiply<false>(into, fw[g / FM], fp[g]);
             if (g % kEvery == kEvery - 1) {
                 stage(buffer ^ 1, g / kEvery);
                 fetch(g / kEvery);
@@ -323,10 +325,10 @@ __global__ void __launch_bounds__(256, 2) patch_small_kernel(PatchArgs a)
                 w[k][h] = masked(w[k][h], mask);
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    sum[i][j] = mma(w[k][i], fp[j], sum[i][j]);
+            for (int j = 0; j < 2; ++j) {
+                f32x4 *const into[2] = {&sum[0][j], &sum[1][j]};
+                multiply<false>(into, w[k], fp[j]);
+            }
         }
     }
     if (wave > 0)
@@ -383,198 +385,239 @@ int launch_patch(const PatchArgs &a, int image_type, int mode, int tile, void *s
 // patch[m][chunk q, value e].
 //
 // The summed index is the row, which both operands have as their slow index.
-// A step takes 64 rows (fp32: 32) of 32 F columns of each into LDS as they
-// are; of 16-bit types the transposing LDS reads then give each lane four
-// rows' values of one column, and fp32 operands are read a value a lane. A
-// row's 16-byte chunks are moved by a swizzle of their 32-byte pairs that
-// puts the rows read at once into different banks.
-template <typename T, int F>
-struct GradTile;
-
-template <int F, typename T>
-struct GradTile16 {
-    static constexpr int kRows = 64, kCols = 32 * F, kChunks = kCols / 8;
+// A step takes kRows rows of a tile's columns into LDS as they are; of 16-bit
+// types the transposing LDS reads then give each lane four rows' values of
+// one column, and fp32 operands are read a value a lane. A row's 16-byte
+// chunks are moved by a swizzle that puts what is read, or written, at once
+// into different banks.
+template <typename T, int Cols>
+struct GradTile {  // 16-bit types
+    static constexpr int kRows = 64, kChunks = Cols / 8;
+    // Pairs of chunks are moved by three bits of the row: reads take rows r,
+    // r + 1, r + 2, r + 3 and the same + 8 of two chunks' columns, writes two
+    // neighbouring rows' four chunks.
     static __device__ __forceinline__ int slot(int row, int chunk)
     {
-        const int pairs = kChunks / 2;
-        const int turn = ((row & 7) ^ (row >> 1 & 4)) & (pairs - 1);
-        return row * kChunks + ((((chunk >> 1) ^ turn) << 1) | (chunk & 1));
+        const int turn = (row & 1) << 2 | (row & 2) | ((row >> 2 ^ row >> 3) & 1);
+        return row * kChunks + (chunk ^ turn << 1);
     }
-    // rows 32 k + 8 (lane / 16) .. + 7 of column col0 + lane % 16
-    static __device__ __forceinline__ vec<T, 8> read(const vec<T, 8> *tile, int k, int col0,
-                                                     int lane)
-    {
-        typedef short s16x4 __attribute__((ext_vector_type(4)));
-        typedef short s16x8 __attribute__((ext_vector_type(8)));
-        typedef __attribute__((address_space(3))) s16x4 Shared;
-        const int row = 32 * k + 8 * (lane >> 4) + ((lane & 15) >> 2);
-        const int col = col0 + 4 * (lane & 3);
-        s16x4 v[2];
+    // Operands of N neighbouring tiles of 16 columns from col0 (a multiple of
+    // 32) on: of tile i, rows 32 k + 8 (lane / 16) .. + 7 of its column lane %
+    // 16, in two reads of four rows. Rows four further turn the chunk pairs'
+    // lowest bit, so the second read of tile i has the place of the first of
+    // tile i ^ 1, four rows on.
+    template <int N>
+    struct Reader {
+        uint32_t at[N];
+        __device__ __forceinline__ Reader(int col0, int lane)
+        {
+            const int row = 8 * (lane >> 4) + ((lane & 15) >> 2);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const char *p = (const char *)(tile + slot(row + 4 * h, col >> 3)) + (col & 4) * 2;
-            v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)p);
+            for (int i = 0; i < N; ++i)
+                at[i] = slot(row, (col0 + 16 * i + 4 * (lane & 3)) >> 3) * 16 + (lane & 1) * 8;
         }
-        return __builtin_bit_cast(vec<T, 8>, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5,
-                                                                      6, 7));
-    }
+        __device__ __forceinline__ vec<T, 8> read(const vec<T, 8> *tile, int k, int i) const
+        {
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s16x4 Shared;
+            s16x4 v[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (Shared *)((const char *)tile + at[i ^ h] + (32 * k + 4 * h) * kChunks * 16));
+            return __builtin_bit_cast(
+                vec<T, 8>, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    };
 };
-template <int F>
-struct GradTile<f16, F> : GradTile16<F, f16> {};
-template <int F>
-struct GradTile<bf16, F> : GradTile16<F, bf16> {};
 
-template <int F>
-struct GradTile<float, F> {
-    static constexpr int kRows = 32, kCols = 32 * F, kChunks = kCols / 4;
+template <int Cols>
+struct GradTile<float, Cols> {
+    static constexpr int kRows = 32, kChunks = Cols / 4;
     // 16 lanes read 64 bytes of a row, four rows at once
     static __device__ __forceinline__ int slot(int row, int chunk)
     {
-        return row * kChunks + (chunk ^ (row << 2 & (kChunks - 1)));
+        return row * kChunks + (chunk ^ (row << 2 & 28));
     }
-    // rows 16 k + 4 e + lane / 16, e = 0 .. 3, of column col0 + lane % 16
-    static __device__ __forceinline__ vec<float, 4> read(const vec<float, 4> *tile, int k,
-                                                         int col0, int lane)
-    {
-        const int col = col0 + (lane & 15);
-        vec<float, 4> v;
+    // of tile i, rows 16 k + 4 e + lane / 16, e = 0 .. 3, of its column lane % 16
+    template <int N>
+    struct Reader {
+        int col0, lane;
+        __device__ __forceinline__ Reader(int col0, int lane) : col0(col0), lane(lane) {}
+        __device__ __forceinline__ vec<float, 4> read(const vec<float, 4> *tile, int k,
+                                                      int i) const
+        {
+            const int col = col0 + 16 * i + (lane & 15);
+            vec<float, 4> v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            v[e] = ((const float *)(tile + slot(16 * k + 4 * e + (lane >> 4), col >> 2)))[col & 3];
-        return v;
-    }
+            for (int e = 0; e < 4; ++e)
+                v[e] = ((const float *)(tile + slot(16 * k + 4 * e + (lane >> 4), col >> 2)))
+                    [col & 3];
+            return v;
+        }
+    };
 };
 
-template <typename T, typename S, int F, int Mode>
-__global__ void __launch_bounds__(256, F == 4 ? 2 : 4) patch_grad_kernel(PatchArgs a)
+// Loads, stores and products are arranged as in the forward pass: WD x WP
+// waves, tiles of 16 FD WD columns of grad_out by 16 FP WP patch values. A
+// thread loads one row of each operand a step, four chunks of it.
+template <typename T, typename S, int WD, int WP, int FD, int FP, int Mode>
+__global__ void __launch_bounds__(64 * WD * WP, 2) patch_grad_kernel(PatchArgs a)
 {
-    typedef GradTile<T, F> Tile;
-    constexpr int C = 16 / sizeof(T), kSide = 32 * F, kRows = Tile::kRows;
-    constexpr int kLoads = kRows * Tile::kChunks / 256, kStride = 256 / Tile::kChunks;
-    constexpr int kLines = kRows / 32, kSlots = Tile::kChunks / 8;
+    static_assert(FD * WD == FP * WP, "square tiles");
+    constexpr int C = 16 / sizeof(T), kWaves = WD * WP, kThreads = 64 * kWaves;
+    constexpr int kSide = 16 * FD * WD;
+    typedef GradTile<T, kSide> Tile;
+    constexpr int kRows = Tile::kRows, kChunks = Tile::kChunks;
+    constexpr int kLoads = kRows * kChunks / kThreads;  // of each operand
+    constexpr int kAcross = kThreads / kRows;           // threads of a grad_out row
+    constexpr int kBands = kRows / 16;  // waves that read 16 patches each, side by side
+    static_assert(kLoads == 4 && kWaves % kBands == 0, "one row a thread");
     typedef vec<T, C> Frag;
-    __shared__ Frag patches[2][kRows * Tile::kChunks], grads[2][kRows * Tile::kChunks];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ Frag patches[2][kRows * kChunks], grads[2][kRows * kChunks];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // the tiles of a part of the rows are neighbours: they share its rows
     const uint32_t piece = piece_of(blockIdx.x, a.tiles * a.splits);
     const uint32_t split = piece / a.tiles, tile = piece - split * a.tiles;
     const uint32_t td = divide(tile, a.tiles_n), tq = tile - td * a.tiles_n.d;
-    const uint32_t d0 = td * kSide, q0 = tq * Tile::kChunks;
+    const uint32_t d0 = td * kSide, q0 = tq * kChunks;
     const uint32_t m_lo = split * a.split_rows;
     const uint32_t m_hi = a.rows - m_lo < a.split_rows ? a.rows : m_lo + a.split_rows;
 
-    // This thread's loads: kLines patches of kSlots chunks, 32 patches side by
-    // side; kLoads rows of one chunk of grad_out, whole lines of it. A chunk
-    // that passes grad_out's columns is moved back, and what it repeats is
-    // not written at the end.
-    const uint32_t line_p = threadIdx.x & 31, slot_p = threadIdx.x >> 5;
-    uint32_t image_at[kSlots];
-    int32_t lead[kSlots], have = C;
+    // Four lanes read four chunks of a patch, 16 patches side by side;
+    // kAcross lanes read a row of grad_out. Values that a patch's chunk
+    // repeats need no zeros here: their sums are not used. A chunk that passes
+    // grad_out's columns is moved back, and what it repeats is not written.
+    const int line_p = (lane >> 2) + 16 * (wave % kBands);
+    const int line_g = threadIdx.x / kAcross;
+    uint32_t image_at[kLoads];
+    int32_t have = C;
+    // rows of grad_out shorter than a chunk are left to the kernels of short runs
+    const bool wide = Mode != kShort || a.dim >= (uint32_t)C;
+    const auto slot_p = [&](int i) {
+        return (lane & 3) + 4 * (wave / kBands + kWaves / kBands * i);
+    };
+    const auto slot_g = [&](int i) { return (int)(threadIdx.x % kAcross) + kAcross * i; };
 #pragma unroll
-    for (int k = 0; k < kSlots; ++k) {
-        const Chunk<C> c(a, q0 + slot_p + 8 * k);
-        image_at[k] = c.image;
-        lead[k] = c.lead;
+    for (int i = 0; i < kLoads; ++i) {
+        const Chunk<C> c(a, q0 + slot_p(i));
+        image_at[i] = c.image;
         have = c.have;
     }
-    const uint32_t chunk = threadIdx.x % Tile::kChunks, line = threadIdx.x / Tile::kChunks;
-    const uint32_t d = d0 + chunk * C;
-    const bool wide = a.dim >= (uint32_t)C;
-    const uint32_t d_at = !wide ? 0 : d <= a.dim - C ? d : a.dim - C;
-    vec<S, C> next_p[kLines][kSlots];
+    const auto grad_at = [&](int i) {
+        const uint32_t d = d0 + slot_g(i) * C;
+        return d <= a.dim - C ? d : a.dim - C;
+    };
+    vec<S, C> next_p[kLoads];
     Frag next_g[kLoads];
-    uint32_t fetched = 0;
-    const auto fetch = [&](uint32_t m0) {
-        fetched = m0;
-#pragma unroll
-        for (int i = 0; i < kLines; ++i) {
-            const uint32_t m = m0 + line_p + 32 * i;
-            const S *image = (const S *)a.images + patch_at(a, m < m_hi ? m : m_hi - 1);
-#pragma unroll
-            for (int k = 0; k < kSlots; ++k)
-                next_p[i][k] = load_chunk<S, C, Mode == kShort>(image + image_at[k], have);
-        }
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const uint32_t m = m0 + line + i * kStride;
-            const uint32_t at = m < m_hi ? m : m_hi - 1;
-            const uint32_t im = divide(at, a.tokens), t = at - im * a.tokens.d;
-            const T *g = (const T *)a.grad_out + im * a.image_stride + t * a.row_stride + d_at;
-            next_g[i] = wide ? load<T, C>(g) : load_chunk<T, C, true>(g, a.dim);
+    const S *image = nullptr;
+    const T *grad = nullptr;
+    // the present row's: whether the step in flight, and that being stored, have it
+    bool live_p = false, live_g = false, store_p = false, store_g = false;
+    const auto rows_of = [&](uint32_t m0) {
+        const uint32_t mp = m0 + line_p, mg = m0 + line_g;
+        live_p = mp < m_hi;
+        live_g = mg < m_hi;
+        image = (const S *)a.images + patch_at(a, live_p ? mp : m_lo);
+        const uint32_t at = live_g ? mg : m_lo;
+        const uint32_t im = divide(at, a.tokens), t = at - im * a.tokens.d;
+        grad = (const T *)a.grad_out + im * a.image_stride + t * a.row_stride;
+    };
+    const auto fetch = [&](int i) {
+        if (i < kLoads)
+            next_p[i] = load_chunk<S, C, Mode == kShort>(image + image_at[i], have);
+        else
+            next_g[i - kLoads] = wide ? load<T, C>(grad + grad_at(i - kLoads))
+                                      : load_chunk<T, C, true>(grad, a.dim);
+    };
+    const auto stage = [&](int buffer, int i) {  // rows past the part: zeros on both sides
+        if (i < kLoads) {
+            patches[buffer][Tile::slot(line_p, slot_p(i))] =
+                store_p ? rounded<T, S, C>(next_p[i]) : (Frag)(T)0.0f;
+        } else {
+            grads[buffer][Tile::slot(line_g, slot_g(i - kLoads))] =
+                store_g ? next_g[i - kLoads] : (Frag)(T)0.0f;
         }
     };
-    const auto stage = [&](int buffer) {
-        // rows past the part: zeros on both sides
+    f32x4 sum[FD][FP];  // [grad_out's columns][patch values]
 #pragma unroll
-        for (int k = 0; k < kSlots; ++k) {
-            const Mask mask = mask_of<C>(lead[k]);
+    for (int i = 0; i < FD; ++i)
 #pragma unroll
-            for (int i = 0; i < kLines; ++i) {
-                Frag p = rounded<T, S, C>(next_p[i][k]);
-                if (Mode != kWhole)
-                    p = masked(p, mask);
-                if (fetched + line_p + 32 * i >= m_hi)
-                    p = (Frag)(T)0.0f;
-                patches[buffer][Tile::slot(line_p + 32 * i, slot_p + 8 * k)] = p;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            grads[buffer][Tile::slot(line + i * kStride, chunk)] =
-                fetched + line + i * kStride < m_hi ? next_g[i] : (Frag)(T)0.0f;
-    };
-    f32x4 sum[F][F];  // [grad_out's columns][patch values]
-#pragma unroll
-    for (int i = 0; i < F; ++i)
-#pragma unroll
-        for (int j = 0; j < F; ++j)
+        for (int j = 0; j < FP; ++j)
             sum[i][j] = (f32x4)0.0f;
-    const int col_g = (wave & 1) * 16 * F, col_p = (wave >> 1) * 16 * F;
-    fetch(m_lo);
-    stage(0);
+    const int col_g = wave % WD * 16 * FD, col_p = wave / WD * 16 * FP;
+    constexpr int kPieces = 2 * kLoads, kEvery = 2 * FP / kPieces;
+    const typename Tile::template Reader<FD> reader_g(col_g, lane);
+    const typename Tile::template Reader<FP> reader_p(col_p, lane);
+    const auto products = [&](int buffer) {
+        Frag fg[2][FD], fp[2 * FP];
+#pragma unroll
+        for (int i = 0; i < FD; ++i)
+            fg[0][i] = reader_g.read(grads[buffer], 0, i);
+        fp[0] = reader_p.read(patches[buffer], 0, 0);
+#pragma unroll
+        for (int g = 0; g < 2 * FP; ++g) {
+            if (g + 1 < 2 * FP)
+                fp[g + 1] = reader_p.read(patches[buffer], (g + 1) / FP, (g + 1) % FP);
+            if (g >= FP - FD / 2 && g < FP) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    fg[1][2 * (g - FP + FD / 2) + h] =
+                        reader_g.read(grads[buffer], 1, 2 * (g - FP + FD / 2) + h);
+            }
+            f32x4 *into[FD];
+#pragma unroll
+            for (int i = 0; i < FD; ++i)
+                into[i] = &sum[i][g % FP];
+            multiply<true>(into, fg[g / FP], fp[g]);
+            if (g % kEvery == kEvery - 1) {
+                stage(buffer ^ 1, g / kEvery);
+                fetch(g / kEvery);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    rows_of(m_lo);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+        fetch(i);
+    store_p = live_p;
+    store_g = live_g;
+    rows_of(m_lo + kRows);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        stage(0, i);
+        fetch(i);
+    }
     __syncthreads();
     int buffer = 0;
     for (uint32_t m = m_lo; m < m_hi; m += kRows, buffer ^= 1) {
-        const bool more = m_hi - m > kRows;
-        if (more)
-            fetch(m + kRows);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            Frag fg[F], fp[F];
-#pragma unroll
-            for (int i = 0; i < F; ++i) {
-                fg[i] = Tile::read(grads[buffer], k, col_g + 16 * i, lane);
-                fp[i] = Tile::read(patches[buffer], k, col_p + 16 * i, lane);
-            }
-#pragma unroll
-            for (int i = 0; i < F; ++i)
-#pragma unroll
-                for (int j = 0; j < F; ++j)
-                    sum[i][j] = mma(fp[j], fg[i], sum[i][j]);
-        }
-        if (more)
-            stage(buffer ^ 1);
+        store_p = live_p;
+        store_g = live_g;
+        rows_of(m + 2 * kRows);
+        products(buffer);
         __syncthreads();
     }
-    // a lane has four patch values of one column of grad_out. Column tile
-    // chunks moved back end with the row: column col of the tile is column
-    // d0 + col of grad_out, or of its chunk counted from the row's end.
+    // A lane has four patch values of one column of grad_out: column col of
+    // the tile is column d0 + col, or of a chunk moved back, counted from the
+    // row's end.
     const uint32_t width = a.chunks * C;
     float *part = (float *)a.out + (int64_t)split * a.dim * width;
 #pragma unroll
-    for (int i = 0; i < F; ++i) {
+    for (int i = 0; i < FD; ++i) {
         const uint32_t col = col_g + 16 * i + (lane & 15);
         const uint32_t want = d0 + col / C * C;
-        uint32_t dd = d0 + col;
+        uint32_t d = d0 + col;
         if (wide && want > a.dim - C)  // in a chunk that was moved back
-            dd = want < a.dim ? a.dim - C + col % C : a.dim;
-        if (dd >= a.dim || (wide && dd < want))
+            d = want < a.dim ? a.dim - C + col % C : a.dim;
+        if (d >= a.dim || (wide && d < want))
             continue;
 #pragma unroll
-        for (int j = 0; j < F; ++j) {
+        for (int j = 0; j < FP; ++j) {
             const uint32_t k = q0 * C + col_p + 16 * j + 4 * (lane >> 4);
             if (k < width)
-                store<float, 4>(part + (int64_t)dd * width + k, sum[i][j]);
+                store<float, 4>(part + (int64_t)d * width + k, sum[i][j]);
         }
     }
 }
@@ -584,21 +627,21 @@ int launch_patch_grad(const PatchArgs &a, int image_type, int mode, int tile, vo
 {
     with_image<T>(image_type, [&](auto s) {
         typedef decltype(s) S;
-        const dim3 grid(a.tiles * a.splits), block(256);
+        const dim3 grid(a.tiles * a.splits);
         hipStream_t st = (hipStream_t)stream;
-        const auto launch = [&](auto f) {
-            constexpr int F = f.value;
-            if (mode == kWhole)
-                patch_grad_kernel<T, S, F, kWhole><<<grid, block, 0, st>>>(a);
-            else if (mode == kMasked)
-                patch_grad_kernel<T, S, F, kMasked><<<grid, block, 0, st>>>(a);
-            else
-                patch_grad_kernel<T, S, F, kShort><<<grid, block, 0, st>>>(a);
+        const auto launch = [&](auto mode) {
+            constexpr int M = mode.value;
+            if constexpr (M == kWhole && sizeof(S) == 2 && sizeof(T) == 2) {
+                if (tile == 256)
+                    patch_grad_kernel<T, S, 4, 2, 4, 8, M><<<grid, dim3(512), 0, st>>>(a);
+            }
+            if (tile == 128)
+                patch_grad_kernel<T, S, 2, 2, 4, 4, M><<<grid, dim3(256), 0, st>>>(a);
         };
-        if (tile == 4)
-            launch(std::integral_constant<int, 4>{});
+        if (mode == kShort)
+            launch(std::integral_constant<int, kShort>{});
         else
-            launch(std::integral_constant<int, 2>{});
+            launch(std::integral_constant<int, kWhole>{});
     });
     return (int)hipGetLastError();
 }
