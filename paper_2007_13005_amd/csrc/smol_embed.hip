@@ -94,26 +94,61 @@ __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a)
 
 // The gradient. The ids' keys (the id, or `vocab` for rows without a
 // gradient: they come last) are sorted stably with the rows' numbers; pieces
-// of kPiece sorted rows are summed by a wave per 64 * V columns, and sums of
-// ids that reach over pieces are joined in a second launch. Every sum runs in
-// an order that depends on the ids alone.
-constexpr int kPiece = 32;
+// of a fixed number of sorted rows are summed by a wave per 64 * V columns,
+// and sums of ids that reach over pieces are joined in a second launch. Every
+// sum runs in an order that depends on the ids alone. Zeros for the rows that
+// no id names are written by further workgroups of the sort's launches, which
+// leave most of the chip idle.
 constexpr int kBits = 9, kDigits = 1 << kBits;
-constexpr int kSortThreads = 256, kSortRounds = 4;
+constexpr int kSortThreads = 512, kSortRounds = 2;
 constexpr int kSortTile = kSortThreads * kSortRounds;
 constexpr int kSortGroups = 64;
 // Up to this many rows each row's place is counted directly, in one launch:
 // the id and the row's number fit one word for vocabularies below 2^19.
 constexpr int kRankBits = 13, kRankRows = 1 << kRankBits;
 
+// Zeros in the words lo .. hi - 1 (dense rows) or the rows lo .. hi - 1 of
+// `words` each, `stride` apart; words are 16-bit. first: the launch's first
+// workgroup that does this.
+struct Fill {
+    uint16_t *at;
+    int64_t lo, hi, words, stride;
+    uint32_t first;
+};
+
+__device__ __forceinline__ void fill(const Fill &f)
+{
+    typedef vec<uint16_t, 8> W;
+    const int64_t block = blockIdx.x - f.first, blocks = gridDim.x - f.first;
+    const int64_t count = f.words ? f.words : f.hi - f.lo;
+    const auto zero = [&](uint16_t *p, int64_t at) {  // words at .. at + 7 of p's `count`
+        if (count >= 8)
+            store<uint16_t, 8>(p + (at <= count - 8 ? at : count - 8), (W)(uint16_t)0);
+        else
+            for (int64_t k = at; k < count; ++k)
+                p[k] = 0;
+    };
+    if (!f.words) {
+        for (int64_t i = (block * blockDim.x + threadIdx.x) * 8; i < count;
+             i += blocks * blockDim.x * 8)
+            zero(f.at + f.lo, i);
+        return;
+    }
+    const int64_t waves = blockDim.x / 64;
+    for (int64_t r = f.lo + block * waves + threadIdx.x / 64; r < f.hi; r += blocks * waves)
+        for (int64_t i = (threadIdx.x & 63) * 8; i < count; i += 512)
+            zero(f.at + r * f.stride, i);
+}
+
 struct SortArgs {
     const void *ids;
     const uint32_t *key_in, *row_in;
     uint32_t *key, *row;
-    uint32_t *table;  // [digit][workgroup] counts
+    uint32_t *table;  // [workgroup][digit] counts
     int64_t vocab, padding;
     uint32_t n, per;  // keys, keys a workgroup
     int32_t shift, groups;
+    Fill fill;
 };
 
 template <typename I>
@@ -128,6 +163,10 @@ __device__ __forceinline__ uint32_t key_of(const SortArgs &a, uint32_t i)
 template <typename I>
 __global__ void __launch_bounds__(256) embed_rank_kernel(SortArgs a)
 {
+    if (blockIdx.x >= a.fill.first) {
+        fill(a.fill);
+        return;
+    }
     __shared__ uint32_t word[kRankRows];
     for (uint32_t i = threadIdx.x; i < ((a.n + 15) & ~15u); i += 256)
         word[i] = i < a.n ? key_of<I>(a, i) << kRankBits | i : 0xffffffffu;
@@ -154,9 +193,12 @@ __global__ void __launch_bounds__(256) embed_rank_kernel(SortArgs a)
 template <typename I, bool First>
 __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(SortArgs a)
 {
+    if (blockIdx.x >= a.fill.first) {
+        fill(a.fill);
+        return;
+    }
     __shared__ uint32_t count[kDigits];
-    for (int d = threadIdx.x; d < kDigits; d += kSortThreads)
-        count[d] = 0;
+    count[threadIdx.x] = 0;
     __syncthreads();
     const uint32_t lo = blockIdx.x * a.per, end = lo + a.per, hi = end < a.n ? end : a.n;
     for (uint32_t i = lo + threadIdx.x; i < hi; i += kSortThreads) {
@@ -164,34 +206,31 @@ __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(SortArgs a)
         atomicAdd(&count[key >> a.shift & (kDigits - 1)], 1u);
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < kDigits; d += kSortThreads)
-        a.table[d * kSortGroups + blockIdx.x] = count[d];
+    a.table[blockIdx.x * kDigits + threadIdx.x] = count[threadIdx.x];
 }
 
 template <typename I, bool First>
 __global__ void __launch_bounds__(kSortThreads) embed_move_kernel(SortArgs a)
 {
+    static_assert(kSortThreads == kDigits, "a digit a thread");
+    if (blockIdx.x >= a.fill.first) {
+        fill(a.fill);
+        return;
+    }
     constexpr int kWaves = kSortThreads / 64;
     __shared__ uint32_t base[kDigits];            // next place of each digit
     __shared__ uint32_t count[kWaves][kDigits];   // this tile's, wave by wave
     __shared__ uint32_t sums[kWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     // base[d]: all keys of smaller digits, and of this digit in earlier groups
-    uint32_t total[kDigits / kSortThreads], before[kDigits / kSortThreads], sum = 0;
-#pragma unroll
-    for (int k = 0; k < kDigits / kSortThreads; ++k) {
-        const int d = threadIdx.x * (kDigits / kSortThreads) + k;
-        uint32_t t = 0, b = 0;
-        for (int g = 0; g < a.groups; ++g) {
-            const uint32_t c = a.table[d * kSortGroups + g];
-            t += c;
-            b += g < (int)blockIdx.x ? c : 0;
-        }
-        total[k] = t;
-        before[k] = b;
-        sum += t;
+    uint32_t total = 0, before = 0;
+#pragma unroll 16
+    for (int g = 0; g < a.groups; ++g) {
+        const uint32_t c = a.table[g * kDigits + threadIdx.x];
+        total += c;
+        before += g < (int)blockIdx.x ? c : 0;
     }
-    uint32_t scan = sum;
+    uint32_t scan = total;
 #pragma unroll
     for (int k = 1; k < 64; k <<= 1) {
         const uint32_t up = __shfl_up(scan, k);
@@ -200,14 +239,10 @@ __global__ void __launch_bounds__(kSortThreads) embed_move_kernel(SortArgs a)
     if (lane == 63)
         sums[wave] = scan;
     __syncthreads();
-    uint32_t start = scan - sum;
+    uint32_t start = scan - total + before;
     for (int w = 0; w < wave; ++w)
         start += sums[w];
-#pragma unroll
-    for (int k = 0; k < kDigits / kSortThreads; ++k) {
-        base[threadIdx.x * (kDigits / kSortThreads) + k] = start + before[k];
-        start += total[k];
-    }
+    base[threadIdx.x] = start;
     const uint32_t lo = blockIdx.x * a.per, end = lo + a.per, hi = end < a.n ? end : a.n;
     for (uint32_t tile = lo; tile < hi; tile += kSortTile) {
         __syncthreads();
@@ -255,13 +290,11 @@ __global__ void __launch_bounds__(kSortThreads) embed_move_kernel(SortArgs a)
             a.row[to] = row[r];
         }
         __syncthreads();
-        for (int d = threadIdx.x; d < kDigits; d += kSortThreads) {
-            uint32_t c = 0;
+        uint32_t c = 0;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w)
-                c += count[w][d];
-            base[d] += c;
-        }
+        for (int w = 0; w < kWaves; ++w)
+            c += count[w][threadIdx.x];
+        base[threadIdx.x] += c;
     }
 }
 
@@ -273,6 +306,7 @@ struct GradArgs {
     void *table;
     int64_t grad_stride, table_stride;
     uint32_t n, vocab, pieces;
+    int32_t piece;  // rows of a piece, at most 64
     int32_t dim, accumulate;
     float scale;
 };
@@ -288,18 +322,24 @@ __device__ __forceinline__ void write_row(const GradArgs &a, uint32_t id, Span<V
     store_own<P, V>(p, from_f32<P, V>(sum), c.lead);
 }
 
+// A wave sums its piece, kAhead rows on their way at a time. What has arrived
+// goes through LDS (each lane's own 16 bytes, so nothing waits for other
+// waves): the loop over rows stays a loop, and its code in the instruction
+// cache, which it did not fit unrolled over registers (16384 rows and up: more
+// time went by waiting for instructions than for memory).
 template <typename G, typename P, int V>
 __global__ void __launch_bounds__(256) embed_grad_kernel(GradArgs a)
 {
     constexpr int kAhead = 8;
+    __shared__ vec<G, V> arrived[4][kAhead][64];
     const int32_t lane = threadIdx.x & 63;
-    const uint32_t piece =
-        __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t piece = blockIdx.x * 4 + wave;
     if (piece >= a.pieces)
         return;
     const Span<V> c((int32_t)(blockIdx.y * 64 + lane) * V, a.dim);
-    const uint32_t lo = piece * kPiece;
-    const uint32_t count = a.n - lo < kPiece ? a.n - lo : kPiece;
+    const uint32_t lo = piece * a.piece;
+    const uint32_t count = a.n - lo < (uint32_t)a.piece ? a.n - lo : a.piece;
     // lane p: the piece's p-th key and row; past the rows, a key of no row
     uint32_t key = a.vocab, row = 0;
     if (lane < (int32_t)count) {
@@ -307,91 +347,143 @@ __global__ void __launch_bounds__(256) embed_grad_kernel(GradArgs a)
         row = a.row[lo + lane];
     }
     const uint32_t left = lo > 0 ? a.key[lo - 1] : a.vocab;
-    const uint32_t right = lo + kPiece < a.n ? a.key[lo + kPiece] : a.vocab;
+    const uint32_t right = lo + a.piece < a.n ? a.key[lo + a.piece] : a.vocab;
     const uint32_t some = __popcll(__ballot(key != a.vocab));  // they come first
     if (some == 0)
         return;
     vec<float, V> sum = (vec<float, V>)0.0f;
     uint32_t id = __builtin_amdgcn_readlane(key, 0);
     bool first = true;
-    const auto end_of = [&](bool last) {
-        if (first && id == left)
-            store_own<float, V>(a.part + (int64_t)piece * 2 * a.dim + c.at, sum, c.lead);
-        else if (last && id == right)
-            store_own<float, V>(a.part + ((int64_t)piece * 2 + 1) * a.dim + c.at, sum, c.lead);
-        else
-            write_row<P, V>(a, id, c, sum);
-    };
-    for (uint32_t p = 0; p < some; p += kAhead) {
-        vec<G, V> x[kAhead];
+    vec<G, V> x[kAhead];
+    const auto fetch = [&](uint32_t p) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const uint32_t q = p + u < some ? p + u : some - 1;
             const int64_t r = (uint32_t)__builtin_amdgcn_readlane(row, q);
             x[u] = load<G, V>((const G *)a.grad_out + r * a.grad_stride + c.at);
         }
+        asm volatile("" ::: "memory");
+    };
+    fetch(0);
+    for (uint32_t p = 0; p < some; p += kAhead) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (p + u < some) {
-                const uint32_t k = __builtin_amdgcn_readlane(key, p + u);
-                if (k != id) {
-                    end_of(false);
-                    first = false;
-                    id = k;
-                    sum = (vec<float, V>)0.0f;
+        for (int u = 0; u < kAhead; ++u)
+            arrived[wave][u][lane] = x[u];
+        if (p + kAhead < some)
+            fetch(p + kAhead);
+        const uint32_t end = some - p < kAhead ? some : p + kAhead;
+#pragma unroll 1
+        for (uint32_t q = p; q <= end; ++q) {
+            // at the piece's end once more, for the last sum
+            const uint32_t k = q < some ? __builtin_amdgcn_readlane(key, q) : ~0u;
+            if (k != id && (q < end || end == some)) {
+                float *part = a.part + (int64_t)piece * 2 * a.dim + c.at;
+                if (first && id == left)
+                    store_own<float, V>(part, sum, c.lead);
+                else if (q == (uint32_t)a.piece && id == right)
+                    store_own<float, V>(part + a.dim, sum, c.lead);
+                else
+                    write_row<P, V>(a, id, c, sum);
+                first = false;
+                id = k;
+                sum = (vec<float, V>)0.0f;
+            }
+            if (q < end)
+                sum += to_f32<V, G>(arrived[wave][q - p][lane]);
+        }
+    }
+}
+
+// The sums of pieces from..to - 1 after `part`, added in order.
+template <int V>
+__device__ __forceinline__ vec<float, V> add_parts(const GradArgs &a, const float *part,
+                                                   uint32_t from, uint32_t to, vec<float, V> sum)
+{
+    constexpr uint32_t kAhead = 8;
+    for (uint32_t k = from; k < to; k += kAhead) {
+        vec<float, V> x[kAhead];
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u)
+            x[u] = load<float, V>(part + (int64_t)(k + u < to ? k + u : to - 1) * 2 * a.dim);
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u)
+            if (k + u < to)
+                sum += x[u];
+    }
+    return sum;
+}
+
+// An id that reaches over pieces belongs to the piece in which it begins. A
+// wave a piece adds the later pieces' sums to its own, in order; where there
+// are more than kAlone of them, the eight waves of the workgroup divide them,
+// and the waves' sums are added in order.
+template <typename P, int V>
+__global__ void __launch_bounds__(512) embed_join_kernel(GradArgs a)
+{
+    constexpr uint32_t kWaves = 8, kAlone = 16;
+    __shared__ vec<float, V> sums[kWaves][64];
+    __shared__ uint32_t counts[kWaves];
+    const uint32_t lane = threadIdx.x & 63;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Span<V> c((int32_t)(blockIdx.y * 64 + lane) * V, a.dim);
+    const auto own = [&](uint32_t piece) {
+        return load<float, V>(a.part + ((int64_t)piece * 2 + 1) * a.dim + c.at);
+    };
+    const uint32_t piece = blockIdx.x * kWaves + wave, lo = piece * a.piece, hi = lo + a.piece;
+    uint32_t count = 0, id = a.vocab;
+    if (piece + 1 < a.pieces) {
+        id = a.key[hi - 1];
+        if (id != a.vocab && a.key[hi] == id &&
+            !(lo > 0 && a.key[lo] == id && a.key[lo - 1] == id)) {
+            // how many later pieces begin with the id: 64 tried at once, then
+            // every (n / 64)th of those that are left
+            const uint32_t all = a.pieces - piece - 1;
+            uint32_t left = all, step = 1;
+            for (;;) {
+                const uint32_t at = count + (lane + 1) * step - 1;
+                const uint64_t same = __ballot(at < left && a.key[hi + at * a.piece] == id);
+                const uint32_t run = ~same ? __builtin_ctzll(~same) : 64;
+                count += run * step;
+                if (run < 64) {
+                    if (step == 1)
+                        break;
+                    left = count + step < left ? count + step : left;
                 }
-                sum += to_f32<V, G>(x[u]);
+                if (count == left)
+                    break;
+                step = left - count > 64 ? (left - count + 63) / 64 : 1;
+            }
+            if (count <= kAlone) {
+                const float *part = a.part + ((int64_t)piece + 1) * 2 * a.dim + c.at;
+                write_row<P, V>(a, id, c, add_parts<V>(a, part, 0, count, own(piece)));
             }
         }
     }
-    end_of(some == kPiece);
-}
-
-// The wave of the piece in which an id that reaches over pieces begins adds
-// the later pieces' sums to its own, in order.
-template <typename P, int V>
-__global__ void __launch_bounds__(256) embed_join_kernel(GradArgs a)
-{
-    const int32_t lane = threadIdx.x & 63;
-    const uint32_t piece =
-        __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    if (piece + 1 >= a.pieces)
-        return;
-    const uint32_t lo = piece * kPiece, hi = lo + kPiece;  // hi < n
-    const uint32_t id = a.key[hi - 1];
-    if (id == a.vocab || a.key[hi] != id)
-        return;
-    if (lo > 0 && a.key[lo] == id && a.key[lo - 1] == id)
-        return;  // begins further left
-    const Span<V> c((int32_t)(blockIdx.y * 64 + lane) * V, a.dim);
-    const float *part = a.part + c.at;
-    vec<float, V> sum = load<float, V>(part + ((int64_t)piece * 2 + 1) * a.dim);
-    for (uint32_t q = piece + 1; q < a.pieces;) {
-        // how many of the next 64 pieces begin with the id
-        const uint32_t at = q + lane;
-        const uint64_t more = __ballot(at < a.pieces && a.key[at * kPiece] == id);
-        const uint32_t run = more == ~0ull ? 64 : __builtin_ctzll(~more);
-#pragma unroll 8
-        for (uint32_t k = 0; k < run; ++k)
-            sum += load<float, V>(part + (int64_t)(q + k) * 2 * a.dim);
-        if (run < 64)
-            break;
-        q += 64;
+    if (lane == 0)
+        counts[wave] = count;
+    __syncthreads();
+    for (uint32_t k = 0; k < kWaves; ++k) {
+        const uint32_t many = __builtin_amdgcn_readfirstlane(counts[k]);
+        if (many <= kAlone)
+            continue;
+        const uint32_t at = blockIdx.x * kWaves + k, each = (many + kWaves - 1) / kWaves;
+        const uint32_t from = wave * each, to = from + each < many ? from + each : many;
+        const float *part = a.part + ((int64_t)at + 1) * 2 * a.dim + c.at;
+        vec<float, V> sum = (vec<float, V>)0.0f;
+        if (wave == 0)
+            sum = own(at);
+        sum = add_parts<V>(a, part, from, to, sum);
+        sums[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (uint32_t w = 1; w < kWaves; ++w)
+                sum += sums[w][lane];
+            write_row<P, V>(a, a.key[at * a.piece + a.piece - 1], c, sum);
+        }
+        __syncthreads();
     }
-    write_row<P, V>(a, id, c, sum);
-}
-
-// Zeros in every row.
-template <typename P, int V>
-__global__ void __launch_bounds__(256) embed_zero_kernel(GradArgs a)
-{
-    const int32_t lane = threadIdx.x & 63;
-    const uint32_t wave = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const Span<V> c((int32_t)(blockIdx.y * 64 + lane) * V, a.dim);
-    if (c.lead == V)
-        return;
-    for (uint32_t v = wave; v < a.vocab; v += gridDim.x * 4)
-        store<P, V>((P *)a.table + (int64_t)v * a.table_stride + c.at, (vec<P, V>)(P)0.0f);
 }
 
 int check_ids(int64_t n, int64_t vocab, int32_t dim, int32_t ids_type)
@@ -444,13 +536,19 @@ struct Workspace {
     int64_t keys, table, part, bytes;
 };
 
+// Rows of a piece: few where there are few rows, so that they are summed side
+// by side (777 rows: 13 us in pieces of 32); more where the pieces fill the
+// chip, so that fewer sums are written and read again.
+int piece_rows(int64_t n) { return n <= 4096 ? 8 : 32; }
+
 Workspace layout(int64_t n, int32_t dim)
 {
     Workspace w;
     w.keys = (n * 4 + 15) / 16 * 16;
     w.table = 4 * w.keys;
     w.part = w.table + kDigits * kSortGroups * 4;
-    w.bytes = w.part + (n + kPiece - 1) / kPiece * 2 * dim * 4 + 16;
+    const int piece = piece_rows(n);
+    w.bytes = w.part + (n + piece - 1) / piece * 2 * dim * 4 + 16;
     return w;
 }
 
@@ -565,36 +663,69 @@ extern "C" int smol_embed_backward(const smol_embed_grad_args *p, void *stream)
     o.n = (uint32_t)p->n;
     o.shift = 0;
     o.groups = o.per = 0;
+    const bool rank = p->n <= kRankRows && p->vocab < 1 << (32 - kRankBits);
+    int passes = 1;
+    while (p->vocab >> passes * kBits)
+        ++passes;
+    // the zeros, a share with each launch of the sort
+    const int launches = rank ? 1 : 2 * passes;
+    const int64_t words = (int64_t)p->dim * elem_size(p->grad_type) / 2;
+    const bool dense = p->vocab == 1 || p->table_stride == p->dim;
+    Fill f;
+    f.at = (uint16_t *)p->grad_table;
+    f.words = dense ? 0 : words;
+    f.stride = p->table_stride * elem_size(p->grad_type) / 2;
+    const int64_t units = dense ? (p->vocab * words + 7) / 8 : p->vocab;  // of 8 words, or rows
+    int launch = 0;
+    // The workgroups of the next launch: `sorting` that sort, and those that
+    // write zeros after them, 64 KiB each or more.
+    const auto with_fill = [&](unsigned sorting, int threads) {
+        const int64_t lo = units * launch / launches, hi = units * (launch + 1) / launches;
+        ++launch;
+        f.first = o.fill.first = sorting;
+        if (p->accumulate || lo == hi)
+            return dim3(sorting);
+        f.lo = dense ? lo * 8 : lo;
+        f.hi = dense ? (hi == units ? p->vocab * words : hi * 8) : hi;
+        o.fill = f;
+        const int64_t bytes = dense ? (hi - lo) * 16 : (hi - lo) * words * 2;
+        const int64_t want = bytes / 65536 + 1, most = 2048 * 256 / threads;
+        return dim3(sorting + (unsigned)(want < most ? want : most));
+    };
     int at = 0;  // which buffer holds the sorted keys
-    if (p->n > 0 && p->n <= kRankRows && p->vocab < 1 << (32 - kRankBits)) {
+    if (rank) {
         with_ids(p->ids_type, [&](auto i) {
-            hipLaunchKernelGGL((embed_rank_kernel<decltype(i)>),
-                               dim3((unsigned)((p->n + 15) / 16)), dim3(256), 0, s, o);
+            const dim3 grid = with_fill((unsigned)((p->n + 15) / 16), 256);
+            if (grid.x > 0)
+                hipLaunchKernelGGL((embed_rank_kernel<decltype(i)>), grid, dim3(256), 0, s, o);
         });
-    } else if (p->n > 0) {
+    } else {
         int64_t per = (p->n + kSortGroups - 1) / kSortGroups;
         per = (per + kSortTile - 1) / kSortTile * kSortTile;
         o.per = (uint32_t)per;
         o.groups = (int32_t)((p->n + per - 1) / per);
         at = 1;
-        for (int shift = 0; shift == 0 || p->vocab >> shift; shift += kBits) {
+        const dim3 block(kSortThreads);
+        const auto grid = [&] { return with_fill((unsigned)o.groups, kSortThreads); };
+        for (int pass = 0; pass < passes; ++pass) {
             at ^= 1;
-            o.shift = shift;
+            o.shift = pass * kBits;
             o.key = key[at];
             o.row = row[at];
             o.key_in = key[at ^ 1];
             o.row_in = row[at ^ 1];
-            const dim3 grid((unsigned)o.groups), block(kSortThreads);
-            if (shift == 0) {
+            if (pass == 0) {
                 with_ids(p->ids_type, [&](auto i) {
-                    hipLaunchKernelGGL((embed_count_kernel<decltype(i), true>), grid, block, 0, s,
-                                       o);
-                    hipLaunchKernelGGL((embed_move_kernel<decltype(i), true>), grid, block, 0, s,
-                                       o);
+                    dim3 g = grid();
+                    hipLaunchKernelGGL((embed_count_kernel<decltype(i), true>), g, block, 0, s, o);
+                    g = grid();
+                    hipLaunchKernelGGL((embed_move_kernel<decltype(i), true>), g, block, 0, s, o);
                 });
             } else {
-                hipLaunchKernelGGL((embed_count_kernel<int32_t, false>), grid, block, 0, s, o);
-                hipLaunchKernelGGL((embed_move_kernel<int32_t, false>), grid, block, 0, s, o);
+                dim3 g = grid();
+                hipLaunchKernelGGL((embed_count_kernel<int32_t, false>), g, block, 0, s, o);
+                g = grid();
+                hipLaunchKernelGGL((embed_move_kernel<int32_t, false>), g, block, 0, s, o);
             }
         }
     }
@@ -608,32 +739,41 @@ extern "C" int smol_embed_backward(const smol_embed_grad_args *p, void *stream)
     a.table_stride = p->table_stride;
     a.n = (uint32_t)p->n;
     a.vocab = (uint32_t)p->vocab;
-    a.pieces = (uint32_t)((p->n + kPiece - 1) / kPiece);
+    a.piece = piece_rows(p->n);
+    a.pieces = (uint32_t)((p->n + a.piece - 1) / a.piece);
     a.dim = p->dim;
     a.accumulate = p->accumulate;
     a.scale = p->scale;
-    with_width(p->dim, [&](auto v) {
-        constexpr int V = v.value;
-        const unsigned cols = (unsigned)((p->dim + 64 * V - 1) / (64 * V));
+    if (a.pieces > 0)
         with_type(p->grad_type, [&](auto t) {
             typedef decltype(t) P;
-            if (!p->accumulate) {
-                const int64_t groups = (p->vocab + 3) / 4;
-                hipLaunchKernelGGL((embed_zero_kernel<P, V>),
-                                   dim3((unsigned)(groups < 4096 ? groups : 4096), cols),
-                                   dim3(256), 0, s, a);
-            }
-            if (a.pieces == 0)
-                return;
-            const dim3 grid((a.pieces + 3) / 4, cols);
             with_type(p->out_type, [&](auto g) {
-                hipLaunchKernelGGL((embed_grad_kernel<decltype(g), P, V>), grid, dim3(256), 0, s,
-                                   a);
+                typedef decltype(g) G;
+                const auto launch = [&](auto v) {  // V columns a lane: 16 bytes of grad_out
+                    constexpr int V = v.value;
+                    const dim3 grid((a.pieces + 3) / 4,
+                                    (unsigned)((p->dim + 64 * V - 1) / (64 * V)));
+                    hipLaunchKernelGGL((embed_grad_kernel<G, P, V>), grid, dim3(256), 0, s, a);
+                };
+                constexpr int V = 16 / sizeof(G);
+                if (p->dim >= V)
+                    launch(std::integral_constant<int, V>{});
+                else
+                    launch(std::integral_constant<int, 1>{});
             });
-            if (a.pieces > 1)
-                hipLaunchKernelGGL((embed_join_kernel<P, V>), grid, dim3(256), 0, s, a);
+            if (a.pieces > 1) {
+                const auto launch = [&](auto v) {
+                    constexpr int V = v.value;
+                    const dim3 grid((a.pieces + 7) / 8,
+                                    (unsigned)((p->dim + 64 * V - 1) / (64 * V)));
+                    hipLaunchKernelGGL((embed_join_kernel<P, V>), grid, dim3(512), 0, s, a);
+                };
+                if (p->dim >= 4)
+                    launch(std::integral_constant<int, 4>{});
+                else
+                    launch(std::integral_constant<int, 1>{});
+            }
         });
-    });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return set_error(SMOL_ERR_HIP, "embedding backward launch: %s", hipGetErrorString(e));
