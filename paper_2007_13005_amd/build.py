@@ -19,6 +19,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libsmol.so")
 # the binding's native marshalling, named for this interpreter's ABI
 PYCALL = os.path.join(PKG, "_smolcall" + sysconfig.get_config_var("EXT_SUFFIX"))
+# the token operators' binding, which reads torch's tensors
+PYTOKENS = os.path.join(PKG, "_smoltokens" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 # The row-streaming kernels are split into parts (input, output type, row
 # walk, output layout) so that the compiler runs on the parts in parallel.
@@ -135,9 +137,41 @@ def build_pycall(verbose: bool = False) -> str:
     return PYCALL
 
 
+def pytokens_command() -> list:
+    """The compiler call of the token operators' binding (host code only,
+    against the headers and libraries of the installed torch)."""
+    import torch
+    base = os.path.dirname(torch.__file__)
+    libs = os.path.join(base, "lib")
+    cc = shutil.which("g++") or hipcc()
+    return [cc, "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC", "-D__HIP_PLATFORM_AMD__",
+            "-DUSE_ROCM", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            "-I", sysconfig.get_paths()["include"], "-I", INCLUDE,
+            "-isystem", os.path.join(base, "include"),
+            "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+            "-isystem", os.path.join(os.path.dirname(os.path.dirname(hipcc())), "include"),
+            os.path.join(CSRC, "smol_tokens_py.cpp"), "-L", libs, "-Wl,--no-as-needed",
+            "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10_hip", "-lc10"]
+
+
 def build(verbose: bool = False) -> str:
     cc = hipcc()
     build_pycall(verbose)
+    # beside the kernels: torch's headers take a while
+    pytokens = [*pytokens_command(), "-o", PYTOKENS + ".tmp"]
+    if verbose:
+        print(" ".join(pytokens), flush=True)
+    binding = subprocess.Popen(pytokens, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)
+    try:
+        return _build_library(cc, verbose)
+    finally:
+        _, err = binding.communicate()
+        if binding.returncode != 0:
+            raise RuntimeError(f"building _smoltokens failed ({binding.returncode}):\n{err}")
+        os.replace(PYTOKENS + ".tmp", PYTOKENS)
+
+
+def _build_library(cc: str, verbose: bool) -> str:
     tmp = LIB + ".tmp"
     with tempfile.TemporaryDirectory(prefix="smol_build_") as objdir:
         cmds = []
@@ -179,10 +213,11 @@ def build(verbose: bool = False) -> str:
 
 
 def sources_newer_than_lib() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(PYCALL):
+    if not all(os.path.exists(f) for f in (LIB, PYCALL, PYTOKENS)):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(PYCALL))
-    files = [os.path.join(CSRC, f) for f in SOURCES + HEADERS + ["smol_pycall.c"]] + [
+    t = min(os.path.getmtime(f) for f in (LIB, PYCALL, PYTOKENS))
+    files = [os.path.join(CSRC, f)
+             for f in SOURCES + HEADERS + ["smol_pycall.c", "smol_tokens_py.cpp"]] + [
         os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE) if f.endswith(".h")]
     return any(os.path.getmtime(f) > t for f in files)
 

@@ -17,27 +17,34 @@ from paper_2007_13005_amd import smol, tokens
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 AT = 0x10000
 
-# field names in the order of the C structures
+# the C structures, field by field
+SHAPE_PACK = struct.Struct("12i")
+PACKS = {"smol_patch_embed": struct.Struct("12i5Q2q"),
+         "smol_patch_embed_backward": struct.Struct("12iQ2q5Qq2i"),
+         "smol_embed": struct.Struct("3Q4q4ifi2i"),
+         "smol_embed_backward": struct.Struct("4Q6q4ifi"),
+         "smol_layer_norm": struct.Struct("8Q5q3if2i"),
+         "smol_layer_norm_backward": struct.Struct("10Q6q4i")}
 SHAPE = ["n", "channels", "height", "width", "patch", "dim", "layout", "image_type", "type",
          "r0", "r1", "r2"]
 FIELDS = {
-    "smol_patch_embed": (tokens._PATCH, SHAPE + ["images", "weight", "bias", "pos", "out",
+    "smol_patch_embed": (PACKS["smol_patch_embed"], SHAPE + ["images", "weight", "bias", "pos", "out",
                                                  "image_stride", "row_stride"]),
-    "smol_patch_embed_backward": (tokens._PATCH_GRAD, SHAPE + [
+    "smol_patch_embed_backward": (PACKS["smol_patch_embed_backward"], SHAPE + [
         "grad_out", "image_stride", "row_stride", "images", "grad_weight", "grad_bias",
         "grad_pos", "workspace", "workspace_bytes", "grad_type", "accumulate"]),
-    "smol_embed": (tokens._EMBED, ["ids", "table", "out", "n", "vocab", "table_stride",
+    "smol_embed": (PACKS["smol_embed"], ["ids", "table", "out", "n", "vocab", "table_stride",
                                    "out_stride", "dim", "ids_type", "table_type", "out_type",
                                    "scale", "keep", "r0", "r1"]),
-    "smol_embed_backward": (tokens._EMBED_GRAD, [
+    "smol_embed_backward": (PACKS["smol_embed_backward"], [
         "grad_out", "ids", "grad_table", "workspace", "workspace_bytes", "n", "vocab",
         "grad_stride", "table_stride", "padding", "dim", "ids_type", "out_type", "grad_type",
         "scale", "accumulate"]),
-    "smol_layer_norm": (tokens._NORM, ["x", "residual", "weight", "bias", "out", "sum", "mean",
+    "smol_layer_norm": (PACKS["smol_layer_norm"], ["x", "residual", "weight", "bias", "out", "sum", "mean",
                                        "rstd", "rows", "x_stride", "residual_stride",
                                        "out_stride", "sum_stride", "dim", "type", "weight_type",
                                        "eps", "r0", "r1"]),
-    "smol_layer_norm_backward": (tokens._NORM_GRAD, [
+    "smol_layer_norm_backward": (PACKS["smol_layer_norm_backward"], [
         "grad_out", "h", "grad_sum", "weight", "mean", "rstd", "grad_x", "grad_weight",
         "grad_bias", "workspace", "workspace_bytes", "rows", "grad_stride", "h_stride",
         "sum_stride", "x_stride", "dim", "type", "weight_type", "accumulate"]),
@@ -176,9 +183,9 @@ def test_workspace_sizes():
     assert lib.smol_embed_workspace_bytes(2 ** 30, 2 ** 30, 65536) > 2 ** 40
     assert lib.smol_embed_workspace_bytes(10, 0, 64) == 0
     assert lib.smol_embed_workspace_bytes(10, 100, 65537) == 0
-    shape = tokens._PATCH_SHAPE.pack(*[SHAPE_GOOD[k] for k in SHAPE])
+    shape = SHAPE_PACK.pack(*[SHAPE_GOOD[k] for k in SHAPE])
     assert lib.smol_patch_workspace_bytes(shape) > 0
-    bad = tokens._PATCH_SHAPE.pack(*[dict(SHAPE_GOOD, layout=5)[k] for k in SHAPE])
+    bad = SHAPE_PACK.pack(*[dict(SHAPE_GOOD, layout=5)[k] for k in SHAPE])
     assert lib.smol_patch_workspace_bytes(bad) == 0
     assert lib.smol_patch_workspace_bytes(None) == 0
 
@@ -279,3 +286,9 @@ def test_binding_refusals():
         tokens.patch_embed_backward(dy[:, :3], img, weight)
     with pytest.raises(ValueError):
         tokens.patch_embed_backward(dy, img, weight, workspace=torch.zeros(1, dtype=torch.uint8))
+    with pytest.raises(TypeError):
+        tokens.layer_norm(x, out=3)
+    with pytest.raises(TypeError):
+        tokens.embed([1, 2], x, out=x)
+    with pytest.raises(TypeError):
+        tokens.embed(ids, torch.zeros((5, 8)), "a")
