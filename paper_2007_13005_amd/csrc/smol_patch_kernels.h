@@ -14,12 +14,12 @@ namespace {
 // The end of a wave's tile: row m0 + 16 j + lane % 16 has columns d0 + 32 i +
 // 8 (lane / 16) .. + 7 in tiles (2 i, j) and (2 i + 1, j); bias and position
 // are added, and the result rounded and written. Where all columns exist the
-// positions of two rows are asked for together before any is used.
+// positions of three rows are asked for together before any is used.
 template <typename T, int FD, int FM>
 __device__ __forceinline__ void finish(const PatchArgs &a, uint32_t m0, uint32_t d0, int lane,
                                        f32x4 (&sum)[FD][FM])
 {
-    constexpr int N = FD / 2;
+    constexpr int N = FD / 2, kRows = FM < 3 ? FM : 3;
     const uint32_t d1 = d0 + 8 * (lane >> 4);
     const auto sums_of = [&](int j, int k) {
         return __builtin_shufflevector(sum[2 * k][j], sum[2 * k + 1][j], 0, 1, 2, 3, 4, 5, 6, 7);
@@ -31,25 +31,26 @@ __device__ __forceinline__ void finish(const PatchArgs &a, uint32_t m0, uint32_t
             for (int k = 0; k < N; ++k)
                 bias[k] = load<T, 8>((const T *)a.bias + d1 + 32 * k);
 #pragma unroll
-        for (int first = 0; first < FM; first += 2) {
-            T *out[2];
-            vec<T, 8> pos[2][N];
+        for (int first = 0; first < FM; first += kRows) {
+            vec<T, 8> pos[kRows][N];
+            if (a.pos)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                uint32_t m = m0 + 16 * (first + j) + (lane & 15);
-                m = m < a.rows ? m : a.rows - 1;
-                const uint32_t i = divide(m, a.tokens), t = m - i * a.tokens.d;
-                out[j] = (T *)a.out + i * a.image_stride + t * a.row_stride + d1;
-                if (a.pos)
+                for (int j = 0; j < kRows && first + j < FM; ++j) {
+                    uint32_t m = m0 + 16 * (first + j) + (lane & 15);
+                    m = m < a.rows ? m : a.rows - 1;
+                    const uint32_t t = m - divide(m, a.tokens) * a.tokens.d;
 #pragma unroll
                     for (int k = 0; k < N; ++k)
-                        pos[j][k] = load<T, 8>((const T *)a.pos + (int64_t)t * a.dim + d1 + 32 * k);
-            }
+                        pos[j][k] = load<T, 8>((const T *)a.pos + (t * a.dim + d1 + 32 * k));
+                }
             asm volatile("" ::: "memory");
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (m0 + 16 * (first + j) + (lane & 15) >= a.rows)
+            for (int j = 0; j < kRows && first + j < FM; ++j) {
+                const uint32_t m = m0 + 16 * (first + j) + (lane & 15);
+                if (m >= a.rows)
                     continue;
+                const uint32_t i = divide(m, a.tokens), t = m - i * a.tokens.d;
+                T *out = (T *)a.out + i * a.image_stride + t * a.row_stride + d1;
 #pragma unroll
                 for (int k = 0; k < N; ++k) {
                     vec<float, 8> v = sums_of(first + j, k);
@@ -57,7 +58,7 @@ __device__ __forceinline__ void finish(const PatchArgs &a, uint32_t m0, uint32_t
                         v += to_f32<8, T>(bias[k]);
                     if (a.pos)
                         v += to_f32<8, T>(pos[j][k]);
-                    store<T, 8>(out[j] + 32 * k, from_f32<T, 8>(v));
+                    store<T, 8>(out + 32 * k, from_f32<T, 8>(v));
                 }
             }
         }
