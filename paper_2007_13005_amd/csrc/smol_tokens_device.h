@@ -35,6 +35,14 @@ __device__ __forceinline__ void store(T *p, vec<T, N> v)
     *(Out *)p = v;
 }
 
+// The same for what is written once and not read again soon.
+template <typename T, int N>
+__device__ __forceinline__ void store_past(T *p, vec<T, N> v)
+{
+    typedef __attribute__((address_space(1))) typename Vec<T, N>::loose Out;
+    __builtin_nontemporal_store(v, (Out *)p);
+}
+
 template <int N, typename T>
 __device__ __forceinline__ vec<float, N> to_f32(vec<T, N> v)
 {
