@@ -329,9 +329,22 @@ __global__ void __launch_bounds__(256) norm_join_kernel(NormGradArgs a)
     const int32_t c = blockIdx.x * 16 + (threadIdx.x & 15), q = threadIdx.x >> 4;
     __shared__ float part[16][17];
     float s = 0.0f;
-    if (c < 2 * a.dim)
-        for (int32_t g = q; g < a.groups; g += 16)
-            s += a.part[(int64_t)g * 2 * a.dim + c];
+    if (c < 2 * a.dim) {
+        constexpr int kAhead = 8;
+        const float *p = a.part + c;
+        for (int32_t g = q; g < a.groups; g += 16 * kAhead) {
+            float x[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int32_t at = g + 16 * u;
+                x[u] = p[(int64_t)(at < a.groups ? at : q) * 2 * a.dim];
+            }
+            asm volatile("" ::: "memory");  // eight loads at once
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                s += g + 16 * u < a.groups ? x[u] : 0.0f;
+        }
+    }
     part[q][threadIdx.x & 15] = s;
     __syncthreads();
     if (q != 0 || c >= 2 * a.dim)
