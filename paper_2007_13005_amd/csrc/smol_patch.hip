@@ -178,13 +178,15 @@ uint32_t ceil_div(uint32_t n, uint32_t d) { return (n + d - 1) / d; }
 
 // The tile side of a forward call: the least of the times that the sides take
 // for patches of 768 values (the sides' times grow alike with the values).
-// Measured, us, for 224 x 224 images to 768 columns, sides 32 / 128 / 256:
-//   fp16, images   1: 4.9 / 12.4 / 24.0     8: 12.9 / 12.9 / 25.5
-//                 32: 39.5 / 18.9 / 27.0   64: 69.2 / 29.7 / 28.7
-//                 96: 103 / 36.0 / 30.2   128: 134 / 49.6 / 53.7
-//   fp32, images   1: 9.8 / 57.5   16: 53.3 / 61.1   64: 179 / 159
-// (32: a few tiles at once; 128: two a compute unit, one for the first 256;
-// 256: one). Rows of a large tile must lie within 2^32 bytes.
+// Measured, us, for 224 x 224 images to 768 columns, sides 32 / 64 / 128 / 256:
+//   fp16, images   1: 4.7 / 8.0 / 12.3 / 23.9     8: 12.5 / 10.1 / 13.0 / 25.6
+//                 16: 22.2 / 13.0 / 13.8 / 26.6  32: 38.0 / 19.2 / 18.9 / 27.1
+//                 64: 68.2 / 32.5 / 29.9 / 28.4  96: 101 / 45.3 / 35.7 / 30.5
+//                128: 133 / 60.1 / 46.4 / 53.4
+//   fp32, images   1: 10.4 / 21.5 / 57.4   4: 19.8 / 23.3 / 57.8
+//                 16: 53.4 / 48.8 / 60.1  64: 175 / 138 / 155 (128: not used)
+// (32, 64: several tiles a compute unit at once; 128: two, one for the first
+// 256; 256: one). Rows of a tile from 64 on must lie within 2^32 bytes.
 int forward_tile(const smol_patch_shape &s, const Plan &plan)
 {
     const PatchArgs &a = plan.a;
@@ -199,13 +201,18 @@ int forward_tile(const smol_patch_shape &s, const Plan &plan)
     const int64_t span = (int64_t)(256 / plan.tokens + 2) * a.image_size * elem_size(s.image_type);
     if (span > UINT32_MAX)
         return 32;
+    const auto more = [](double x, double y) { return x > y ? x : y; };
     if (s.type == SMOL_ELEM_F32)
-        return 5 + tiles(32) / 53 <= 4 + 53 * rounds(tiles(128), cus) ? 32 : 128;
-    const double t32 = 4 + tiles(32) / 140;
-    const double t128 = tiles(128) <= cus ? 13 : 3 + 16 * rounds(tiles(128), 2 * cus);
+        return 5 + tiles(32) / 53 <= more(22, 18 + tiles(64) / 19.6) ? 32 : 64;
     const bool large = plan.mode != kShort && elem_size(s.image_type) == 2;
-    const double t256 = large ? 1 + 25 * rounds(tiles(256), cus) : 1e30;
-    return t32 <= t128 && t32 <= t256 ? 32 : t128 <= t256 ? 128 : 256;
+    const double us[4] = {4 + tiles(32) / 140, more(8.2, 6.5 + tiles(64) / 88),
+                          tiles(128) <= cus ? 13 : 3 + 16 * rounds(tiles(128), 2 * cus),
+                          large ? 1 + 25 * rounds(tiles(256), cus) : 1e30};
+    int best = 0;
+    for (int k = 1; k < 4; ++k)
+        if (us[k] < us[best])
+            best = k;
+    return 32 << best;
 }
 
 // The backward pass's parts. A part of the rows costs its partial products a

@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(64 * WD * WM, 2) patch_kernel(PatchArgs a)
     };
     // A step's products: 2 FM groups of FD, each behind the next reads, with
     // a part of the next steps' stores and loads after it.
-    constexpr int kPieces = kLines + kLoads, kEvery = 2 * FM / kPieces;
+    constexpr int kPieces = kLines + kLoads, kGroups = 2 * FM;
     const auto products = [&](int buffer) {
         Frag fw[2][FD], fp[2 * FM];
 #pragma unroll
@@ -214,9 +214,10 @@ __global__ void __launch_bounds__(64 * WD * WM, 2) patch_kernel(PatchArgs a)
             for (int i = 0; i < FD; ++i)
                 into[i] = &sum[i][g % FM];
             multiply<false>(into, fw[g / FM], fp[g]);
-            if (g % kEvery == kEvery - 1) {
-                stage(buffer ^ 1, g / kEvery);
-                fetch(g / kEvery);
+#pragma unroll
+            for (int i = g * kPieces / kGroups; i < (g + 1) * kPieces / kGroups; ++i) {
+                stage(buffer ^ 1, i);
+                fetch(i);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -361,14 +362,18 @@ int launch_patch(const PatchArgs &a, int image_type, int mode, int tile, void *s
         hipStream_t st = (hipStream_t)stream;
         const auto launch = [&](auto mode) {
             constexpr int M = mode.value;
-            // no registers for the largest with short runs, wider pixels in
-            // flight, or fp32 (whose products take long enough for a smaller)
+            // no registers for the largest with short runs or wider pixels in
+            // flight; fp32 products take long enough for tiles of 64
             if constexpr (M != kShort && sizeof(S) == 2 && sizeof(T) == 2) {
                 if (tile == 256)
                     patch_kernel<T, S, 4, 2, 4, 8, M><<<grid, dim3(512), 0, st>>>(a);
             }
-            if (tile == 128)
-                patch_kernel<T, S, 2, 2, 4, 4, M><<<grid, dim3(256), 0, st>>>(a);
+            if constexpr (sizeof(T) == 2) {
+                if (tile == 128)
+                    patch_kernel<T, S, 2, 2, 4, 4, M><<<grid, dim3(256), 0, st>>>(a);
+            }
+            if (tile == 64)
+                patch_kernel<T, S, 2, 2, 2, 2, M><<<grid, dim3(256), 0, st>>>(a);
             else if (tile == 32)
                 patch_small_kernel<T, S, M><<<grid, dim3(256), 0, st>>>(a);
         };
@@ -400,7 +405,7 @@ struct GradTile {  // 16-bit types
     static __device__ __forceinline__ int slot(int row, int chunk)
     {
         const int turn = (row & 1) << 2 | (row & 2) | ((row >> 2 ^ row >> 3) & 1);
-        return row * kChunks + (chunk ^ turn << 1);
+        return row * kChunks + (chunk ^ (turn << 1 & (kChunks - 1)));
     }
     // Operands of N neighbouring tiles of 16 columns from col0 (a multiple of
     // 32) on: of tile i, rows 32 k + 8 (lane / 16) .. + 7 of its column lane %
@@ -438,7 +443,7 @@ struct GradTile<float, Cols> {
     // 16 lanes read 64 bytes of a row, four rows at once
     static __device__ __forceinline__ int slot(int row, int chunk)
     {
-        return row * kChunks + (chunk ^ (row << 2 & 28));
+        return row * kChunks + (chunk ^ (row << 2 & (kChunks - 1) & 28));
     }
     // of tile i, rows 16 k + 4 e + lane / 16, e = 0 .. 3, of its column lane % 16
     template <int N>
@@ -473,7 +478,7 @@ __global__ void __launch_bounds__(64 * WD * WP, 2) patch_grad_kernel(PatchArgs a
     constexpr int kLoads = kRows * kChunks / kThreads;  // of each operand
     constexpr int kAcross = kThreads / kRows;           // threads of a grad_out row
     constexpr int kBands = kRows / 16;  // waves that read 16 patches each, side by side
-    static_assert(kLoads == 4 && kWaves % kBands == 0, "one row a thread");
+    static_assert(kWaves % kBands == 0, "one row a thread");
     typedef vec<T, C> Frag;
     __shared__ Frag patches[2][kRows * kChunks], grads[2][kRows * kChunks];
     const int lane = threadIdx.x & 63;
@@ -548,7 +553,7 @@ __global__ void __launch_bounds__(64 * WD * WP, 2) patch_grad_kernel(PatchArgs a
         for (int j = 0; j < FP; ++j)
             sum[i][j] = (f32x4)0.0f;
     const int col_g = wave % WD * 16 * FD, col_p = wave / WD * 16 * FP;
-    constexpr int kPieces = 2 * kLoads, kEvery = 2 * FP / kPieces;
+    constexpr int kPieces = 2 * kLoads, kGroups = 2 * FP;
     const typename Tile::template Reader<FD> reader_g(col_g, lane);
     const typename Tile::template Reader<FP> reader_p(col_p, lane);
     const auto products = [&](int buffer) {
@@ -572,9 +577,10 @@ __global__ void __launch_bounds__(64 * WD * WP, 2) patch_grad_kernel(PatchArgs a
             for (int i = 0; i < FD; ++i)
                 into[i] = &sum[i][g % FP];
             multiply<true>(into, fg[g / FP], fp[g]);
-            if (g % kEvery == kEvery - 1) {
-                stage(buffer ^ 1, g / kEvery);
-                fetch(g / kEvery);
+#pragma unroll
+            for (int i = g * kPieces / kGroups; i < (g + 1) * kPieces / kGroups; ++i) {
+                stage(buffer ^ 1, i);
+                fetch(i);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
