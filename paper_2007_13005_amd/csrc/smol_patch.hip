@@ -313,6 +313,9 @@ extern "C" int smol_patch_embed(const smol_patch_args *p, void *stream)
     a.image_stride = p->image_stride;
     a.row_stride = p->row_stride;
     const int tile = forward_tile(s, plan);
+    if ((int64_t)ceil_div(a.rows, tile) * ceil_div(a.dim, tile) >= 1 << 24)
+        return set_error(SMOL_ERR_UNSUPPORTED, "%u rows of %u columns: too many for a launch",
+                         a.rows, a.dim);
     set_tiles(&a, ceil_div(a.rows, tile), ceil_div(a.dim, tile));
     const int e = (s.type == SMOL_ELEM_F32   ? launch_patch_f32
                    : s.type == SMOL_ELEM_F16 ? launch_patch_f16
