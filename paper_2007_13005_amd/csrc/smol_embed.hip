@@ -52,7 +52,10 @@ struct EmbedArgs {
     float scale;
 };
 
-// One wave takes kSpans * 64 * V columns of a row, four rows a workgroup.
+// One wave takes kSpans * 64 * V columns of a row, four rows a workgroup; it
+// moves bytes and multiplies once a value. 33001 ids (a quarter of them of no
+// token) of 1024 fp32 columns to bf16: 23 us, 4.4 TB/s; one id of 4096 fp16
+// columns 2.2 us.
 constexpr int kSpans = 2;
 
 template <typename T, typename O, typename I, int V>
@@ -160,7 +163,9 @@ __device__ __forceinline__ uint32_t key_of(const SortArgs &a, uint32_t i)
     return id >= 0 && id < a.vocab && id != a.padding ? (uint32_t)id : (uint32_t)a.vocab;
 }
 
-// Every row's place is the number of (key, row) words below its own: 16 rows
+// Every row's place is the number of (key, row) words below its own (n^2
+// comparisons, one launch: 777 rows 4.2 us with the zeros of a 6.4 MB table; the
+// four launches of a two-pass sort take about 20): 16 rows
 // a workgroup, 16 threads a row, each counting every 16th word.
 template <typename I>
 __global__ void __launch_bounds__(256) embed_rank_kernel(SortArgs a)
@@ -191,7 +196,8 @@ __global__ void __launch_bounds__(256) embed_rank_kernel(SortArgs a)
 }
 
 // One pass of the sort over digits of kBits, two launches: counts of each
-// workgroup's part, then the moves.
+// workgroup's part, then the moves. 65536 ids: 3 and 6 us, or 13 us each with
+// 66 MB of zeros beside them (5 TB/s).
 template <typename I, bool First>
 __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(SortArgs a)
 {
@@ -327,8 +333,10 @@ __device__ __forceinline__ void write_row(const GradArgs &a, uint32_t id, Span<V
 // A wave sums its piece, kAhead rows on their way at a time. What has arrived
 // goes through LDS (each lane's own 16 bytes, so nothing waits for other
 // waves): the loop over rows stays a loop, and its code in the instruction
-// cache, which it did not fit unrolled over registers (16384 rows and up: more
-// time went by waiting for instructions than for memory).
+// cache, where unrolled over registers it did not fit. 65536 rows of 1024 bf16
+// values, a vocabulary of 64000: 47 us for 101 MB read and 62 MB written; the
+// zeros written before are on their way to memory meanwhile (with none before
+// it 25 us for the same reads).
 template <typename G, typename P, int V>
 __global__ void __launch_bounds__(256) embed_grad_kernel(GradArgs a)
 {
@@ -419,7 +427,8 @@ __device__ __forceinline__ vec<float, V> add_parts(const GradArgs &a, const floa
 // An id that reaches over pieces belongs to the piece in which it begins. A
 // wave a piece adds the later pieces' sums to its own, in order; where there
 // are more than kAlone of them, the eight waves of the workgroup divide them,
-// and the waves' sums are added in order.
+// and the waves' sums are added in order. 65536 rows, the most frequent id 4000
+// times: 8 us; one id 49152 times: 18 us (187 with one wave).
 template <typename P, int V>
 __global__ void __launch_bounds__(512) embed_join_kernel(GradArgs a)
 {
