@@ -165,7 +165,7 @@ __device__ __forceinline__ uint32_t key_of(const SortArgs &a, uint32_t i)
 
 // Every row's place is the number of (key, row) words below its own (n^2
 // comparisons, one launch: 777 rows 4.2 us with the zeros of a 6.4 MB table; the
-// four launches of a two-pass sort take about 20): 16 rows
+// four launches of a two-pass sort take about 20). 16 rows
 // a workgroup, 16 threads a row, each counting every 16th word.
 template <typename I>
 __global__ void __launch_bounds__(256) embed_rank_kernel(SortArgs a)
@@ -497,6 +497,116 @@ __global__ void __launch_bounds__(512) embed_join_kernel(GradArgs a)
     }
 }
 
+// Up to kFewRows rows: everything in one launch, without a sort. A wave a row
+// looks for its id among all rows (in LDS); the first row of an id has their
+// list in order, and its wave adds them, or, where there are more than kAlone,
+// the eight waves of the workgroup a part each, joined in order. Workgroups
+// from fill.first on write zeros in the rows of the table that no id names:
+// `per` rows each, which they mark in LDS. 777 rows: 9.0 us a call, 12.2 with
+// the sort's three launches; past kFewRows an id that every row names would
+// keep eight waves too long.
+constexpr int kFewRows = 1024;
+constexpr uint32_t kFewFill = 2048;  // rows of the table a workgroup at most
+
+template <typename I, typename G, typename P, int V>
+__global__ void __launch_bounds__(512) embed_few_kernel(SortArgs o, GradArgs a, uint32_t per)
+{
+    constexpr uint32_t kWaves = 8, kAlone = 16, kAhead = 8;
+    __shared__ uint32_t keys[kFewRows];
+    __shared__ uint16_t list[kWaves][kFewRows];
+    __shared__ vec<float, V> sums[kWaves][64];
+    __shared__ uint32_t counts[kWaves], named[kFewFill / 32];
+    const uint32_t lane = threadIdx.x & 63;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (uint32_t i = threadIdx.x; i < ((a.n + 63) & ~63u); i += 512)
+        keys[i] = i < a.n ? key_of<I>(o, i) : (uint32_t)o.vocab;
+    if (blockIdx.x >= o.fill.first) {
+        if (blockIdx.y > 0)
+            return;
+        const uint32_t lo = (blockIdx.x - o.fill.first) * per;
+        const uint32_t rows = a.vocab - lo < per ? a.vocab - lo : per;
+        if (threadIdx.x < kFewFill / 32)
+            named[threadIdx.x] = 0;
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < a.n; i += 512)
+            if (keys[i] - lo < rows)
+                atomicOr(&named[(keys[i] - lo) / 32], 1u << (keys[i] - lo) % 32);
+        __syncthreads();
+        // chunks of 16 bytes; a row's last is moved back to end with it
+        const uint32_t words = a.dim * (sizeof(P) / 2), chunks = (words + 7) / 8;
+        uint16_t *table = (uint16_t *)a.table;
+        for (uint32_t e = threadIdx.x; e < rows * chunks; e += 512) {
+            const uint32_t r = e / chunks, c = (e - r * chunks) * 8;
+            if (named[r / 32] >> r % 32 & 1)
+                continue;
+            uint16_t *p = table + (int64_t)(lo + r) * a.table_stride * (sizeof(P) / 2);
+            if (words >= 8)
+                store_past<uint16_t, 8>(p + (c <= words - 8 ? c : words - 8),
+                                        (vec<uint16_t, 8>)(uint16_t)0);
+            else
+                for (uint32_t k = 0; k < words; ++k)
+                    p[k] = 0;
+        }
+        return;
+    }
+    __syncthreads();
+    const Span<V> c((int32_t)(blockIdx.y * 64 + lane) * V, a.dim);
+    const uint32_t row = blockIdx.x * kWaves + wave;
+    const uint32_t id = row < a.n ? keys[row] : a.vocab;
+    uint32_t count = 0;
+    if (id != a.vocab) {
+        for (uint32_t i = 0; i < a.n; i += 64) {
+            uint64_t same = __ballot(keys[i + lane] == id);
+            if (i < row && (same & (row - i < 64 ? (1ull << (row - i)) - 1 : ~0ull))) {
+                count = 0;  // not the first of its id
+                break;
+            }
+            if (same >> lane & 1)
+                list[wave][count + __popcll(same & ((1ull << lane) - 1))] = (uint16_t)(i + lane);
+            count += __popcll(same);
+        }
+    }
+    // rows k .. to - 1 of wave w's list, added in order
+    const auto add = [&](uint32_t w, uint32_t k, uint32_t to) {
+        vec<float, V> sum = (vec<float, V>)0.0f;
+        for (; k < to; k += kAhead) {
+            vec<G, V> x[kAhead];
+#pragma unroll
+            for (uint32_t u = 0; u < kAhead; ++u) {
+                const int64_t r = __builtin_amdgcn_readfirstlane(list[w][k + u < to ? k + u : to - 1]);
+                x[u] = load<G, V>((const G *)a.grad_out + r * a.grad_stride + c.at);
+            }
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (uint32_t u = 0; u < kAhead; ++u)
+                if (k + u < to)
+                    sum += to_f32<V, G>(x[u]);
+        }
+        return sum;
+    };
+    if (count > 0 && count <= kAlone)
+        write_row<P, V>(a, id, c, add(wave, 0, count));
+    if (lane == 0)
+        counts[wave] = count;
+    __syncthreads();
+    for (uint32_t w = 0; w < kWaves; ++w) {
+        const uint32_t many = __builtin_amdgcn_readfirstlane(counts[w]);
+        if (many <= kAlone)
+            continue;
+        const uint32_t each = (many + kWaves - 1) / kWaves, from = wave * each;
+        vec<float, V> sum = add(w, from, from + each < many ? from + each : many);
+        sums[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (uint32_t k = 1; k < kWaves; ++k)
+                sum += sums[k][lane];
+            write_row<P, V>(a, keys[blockIdx.x * kWaves + w], c, sum);
+        }
+        __syncthreads();
+    }
+}
+
 int check_ids(int64_t n, int64_t vocab, int32_t dim, int32_t ids_type)
 {
     if (n < 0 || vocab < 1 || dim < 1)
@@ -548,8 +658,8 @@ struct Workspace {
 };
 
 // Rows of a piece: few where there are few rows, so that they are summed side
-// by side (777 rows: 13 us in pieces of 32); more where the pieces fill the
-// chip, so that fewer sums are written and read again.
+// by side (777 rows took 5 us in pieces of 8, 13 in pieces of 32); more where
+// the pieces fill the chip, so that fewer sums are written and read again.
 int piece_rows(int64_t n) { return n <= 4096 ? 8 : 32; }
 
 Workspace layout(int64_t n, int32_t dim)
@@ -674,6 +784,54 @@ extern "C" int smol_embed_backward(const smol_embed_grad_args *p, void *stream)
     o.n = (uint32_t)p->n;
     o.shift = 0;
     o.groups = o.per = 0;
+    GradArgs a;
+    a.grad_out = p->grad_out;
+    a.part = (float *)(ws + w.part);
+    a.table = p->grad_table;
+    a.grad_stride = p->grad_stride;
+    a.table_stride = p->table_stride;
+    a.n = (uint32_t)p->n;
+    a.vocab = (uint32_t)p->vocab;
+    a.piece = piece_rows(p->n);
+    a.pieces = (uint32_t)((p->n + a.piece - 1) / a.piece);
+    a.dim = p->dim;
+    a.accumulate = p->accumulate;
+    a.scale = p->scale;
+    if (p->n <= kFewRows) {
+        const int64_t bytes = (int64_t)p->dim * elem_size(p->grad_type);
+        int64_t per = 65536 / bytes;  // 64 KiB of zeros a workgroup
+        per = per < 1 ? 1 : per > kFewFill ? kFewFill : per;
+        if ((p->vocab + per - 1) / per > 4096)  // of which there are not too many
+            per = (p->vocab + 4095) / 4096 < kFewFill ? (p->vocab + 4095) / 4096 : kFewFill;
+        o.fill.first = (uint32_t)((p->n + 7) / 8);
+        const unsigned zeros = p->accumulate ? 0 : (unsigned)((p->vocab + per - 1) / per);
+        with_type(p->grad_type, [&](auto t) {
+            typedef decltype(t) P;
+            with_type(p->n ? p->out_type : SMOL_ELEM_F32, [&](auto g) {
+                typedef decltype(g) G;
+                const auto launch = [&](auto v) {
+                    constexpr int V = v.value;
+                    const unsigned columns = (unsigned)((p->dim + 64 * V - 1) / (64 * V));
+                    const dim3 grid(o.fill.first + zeros, columns);
+                    with_ids(p->ids_type, [&](auto i) {
+                        hipLaunchKernelGGL((embed_few_kernel<decltype(i), G, P, V>), grid,
+                                           dim3(512), 0, s, o, a, (uint32_t)per);
+                    });
+                };
+                constexpr int V = 16 / sizeof(G);
+                if (o.fill.first + zeros == 0)
+                    return;
+                if (p->dim >= V)
+                    launch(std::integral_constant<int, V>{});
+                else
+                    launch(std::integral_constant<int, 1>{});
+            });
+        });
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return set_error(SMOL_ERR_HIP, "embedding backward launch: %s", hipGetErrorString(e));
+        return SMOL_OK;
+    }
     const bool rank = p->n <= kRankRows && p->vocab < 1 << (32 - kRankBits);
     int passes = 1;
     while (p->vocab >> passes * kBits)
@@ -707,8 +865,7 @@ extern "C" int smol_embed_backward(const smol_embed_grad_args *p, void *stream)
     if (rank) {
         with_ids(p->ids_type, [&](auto i) {
             const dim3 grid = with_fill((unsigned)((p->n + 15) / 16), 256);
-            if (grid.x > 0)
-                hipLaunchKernelGGL((embed_rank_kernel<decltype(i)>), grid, dim3(256), 0, s, o);
+            hipLaunchKernelGGL((embed_rank_kernel<decltype(i)>), grid, dim3(256), 0, s, o);
         });
     } else {
         int64_t per = (p->n + kSortGroups - 1) / kSortGroups;
@@ -740,51 +897,37 @@ extern "C" int smol_embed_backward(const smol_embed_grad_args *p, void *stream)
             }
         }
     }
-    GradArgs a;
-    a.grad_out = p->grad_out;
     a.key = key[at];
     a.row = row[at];
-    a.part = (float *)(ws + w.part);
-    a.table = p->grad_table;
-    a.grad_stride = p->grad_stride;
-    a.table_stride = p->table_stride;
-    a.n = (uint32_t)p->n;
-    a.vocab = (uint32_t)p->vocab;
-    a.piece = piece_rows(p->n);
-    a.pieces = (uint32_t)((p->n + a.piece - 1) / a.piece);
-    a.dim = p->dim;
-    a.accumulate = p->accumulate;
-    a.scale = p->scale;
-    if (a.pieces > 0)
-        with_type(p->grad_type, [&](auto t) {
-            typedef decltype(t) P;
-            with_type(p->out_type, [&](auto g) {
-                typedef decltype(g) G;
-                const auto launch = [&](auto v) {  // V columns a lane: 16 bytes of grad_out
-                    constexpr int V = v.value;
-                    const dim3 grid((a.pieces + 3) / 4,
-                                    (unsigned)((p->dim + 64 * V - 1) / (64 * V)));
-                    hipLaunchKernelGGL((embed_grad_kernel<G, P, V>), grid, dim3(256), 0, s, a);
-                };
-                constexpr int V = 16 / sizeof(G);
-                if (p->dim >= V)
-                    launch(std::integral_constant<int, V>{});
-                else
-                    launch(std::integral_constant<int, 1>{});
-            });
-            if (a.pieces > 1) {
-                const auto launch = [&](auto v) {
-                    constexpr int V = v.value;
-                    const dim3 grid((a.pieces + 7) / 8,
-                                    (unsigned)((p->dim + 64 * V - 1) / (64 * V)));
-                    hipLaunchKernelGGL((embed_join_kernel<P, V>), grid, dim3(512), 0, s, a);
-                };
-                if (p->dim >= 4)
-                    launch(std::integral_constant<int, 4>{});
-                else
-                    launch(std::integral_constant<int, 1>{});
-            }
+    with_type(p->grad_type, [&](auto t) {
+        typedef decltype(t) P;
+        with_type(p->out_type, [&](auto g) {
+            typedef decltype(g) G;
+            const auto launch = [&](auto v) {  // V columns a lane: 16 bytes of grad_out
+                constexpr int V = v.value;
+                const dim3 grid((a.pieces + 3) / 4,
+                                (unsigned)((p->dim + 64 * V - 1) / (64 * V)));
+                hipLaunchKernelGGL((embed_grad_kernel<G, P, V>), grid, dim3(256), 0, s, a);
+            };
+            constexpr int V = 16 / sizeof(G);
+            if (p->dim >= V)
+                launch(std::integral_constant<int, V>{});
+            else
+                launch(std::integral_constant<int, 1>{});
         });
+        {
+            const auto launch = [&](auto v) {
+                constexpr int V = v.value;
+                const dim3 grid((a.pieces + 7) / 8,
+                                (unsigned)((p->dim + 64 * V - 1) / (64 * V)));
+                hipLaunchKernelGGL((embed_join_kernel<P, V>), grid, dim3(512), 0, s, a);
+            };
+            if (p->dim >= 4)
+                launch(std::integral_constant<int, 4>{});
+            else
+                launch(std::integral_constant<int, 1>{});
+        }
+    });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return set_error(SMOL_ERR_HIP, "embedding backward launch: %s", hipGetErrorString(e));

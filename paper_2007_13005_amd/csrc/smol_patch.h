@@ -179,6 +179,48 @@ __device__ __forceinline__ uint32_t piece_of(uint32_t b, uint32_t count)
     return die * each + (die < more ? die : more) + (b >> 3);
 }
 
+// Column sums of grad_out over the images of a part, for every token: eight
+// columns a thread, 256 threads a workgroup. sums[part][token][column]. 256
+// images of 196 tokens, 768 bf16 columns: 15 us, 5.1 TB/s.
+struct SumArgs {
+    const void *grad_out;
+    float *sums;
+    int64_t image_stride, row_stride;
+    uint32_t n, tokens, dim, part_images;
+    Divisor columns;   // groups of columns in a row
+    Divisor per_part;  // workgroups of a part
+    uint32_t groups;   // of all parts (0: no sums wanted)
+};
+
+template <typename T, int V>
+__device__ __forceinline__ void sum_columns_of(const SumArgs &a, uint32_t group)
+{
+    const uint32_t part = divide(group, a.per_part);
+    const uint32_t e = (group - part * a.per_part.d) * 256 + threadIdx.x;
+    const uint32_t t = divide(e, a.columns), col = (e - t * a.columns.d) * V;
+    if (t >= a.tokens)
+        return;
+    const uint32_t at = col <= a.dim - V ? col : a.dim - V;
+    const uint32_t lo = part * a.part_images;
+    const uint32_t hi = a.n - lo < a.part_images ? a.n : lo + a.part_images;
+    const T *p = (const T *)a.grad_out + (int64_t)t * a.row_stride + at;
+    vec<float, V> sum = (vec<float, V>)0.0f;
+#pragma unroll 8
+    for (uint32_t i = lo; i < hi; ++i)
+        sum += to_f32<V, T>(load<T, V>(p + i * a.image_stride));
+    // columns of a group moved back are written twice, alike
+    store<float, V>(a.sums + ((int64_t)part * a.tokens + t) * a.dim + at, sum);
+}
+
+template <typename T>
+__device__ __forceinline__ void sum_columns(const SumArgs &a, uint32_t group)
+{
+    if (a.dim >= 8)
+        sum_columns_of<T, 8>(a, group);
+    else
+        sum_columns_of<T, 1>(a, group);
+}
+
 // How a patch's runs meet the chunks: whole runs of whole chunks and a whole
 // number of K steps; chunks that repeat values or are past the patch; runs
 // shorter than a chunk.
@@ -200,9 +242,12 @@ auto with_image(int type, F f)
 int launch_patch_f32(const PatchArgs &a, int image_type, int mode, int tile, void *stream);
 int launch_patch_f16(const PatchArgs &a, int image_type, int mode, int tile, void *stream);
 int launch_patch_bf16(const PatchArgs &a, int image_type, int mode, int tile, void *stream);
-int launch_patch_grad_f32(const PatchArgs &a, int image_type, int mode, int tile, void *stream);
-int launch_patch_grad_f16(const PatchArgs &a, int image_type, int mode, int tile, void *stream);
-int launch_patch_grad_bf16(const PatchArgs &a, int image_type, int mode, int tile, void *stream);
+int launch_patch_grad_f32(const PatchArgs &a, const SumArgs &b, int image_type, int mode, int tile,
+                          void *stream);
+int launch_patch_grad_f16(const PatchArgs &a, const SumArgs &b, int image_type, int mode, int tile,
+                          void *stream);
+int launch_patch_grad_bf16(const PatchArgs &a, const SumArgs &b, int image_type, int mode, int tile,
+                          void *stream);
 
 }  // namespace smol
 

@@ -12,34 +12,12 @@
 namespace smol {
 namespace {
 
-// Column sums of grad_out over the images of a part, for every token: V
-// columns a thread. sums[part][token][column]. 256 images of 196 tokens, 768
-// bf16 columns: 15 us, 5.1 TB/s.
-struct SumArgs {
-    const void *grad_out;
-    float *sums;
-    int64_t image_stride, row_stride;
-    uint32_t n, tokens, dim, part_images;
-    Divisor columns;  // groups of V columns in a row
-};
-
-template <typename T, int V>
+// Column sums alone, beside products of 256-wide tiles (whose workgroups leave
+// no room for others).
+template <typename T>
 __global__ void __launch_bounds__(256) patch_sum_kernel(SumArgs a)
 {
-    const uint32_t e = blockIdx.x * 256 + threadIdx.x;
-    const uint32_t t = divide(e, a.columns), col = (e - t * a.columns.d) * V;
-    if (t >= a.tokens)
-        return;
-    const uint32_t at = col <= a.dim - V ? col : a.dim - V;
-    const uint32_t lo = blockIdx.y * a.part_images;
-    const uint32_t hi = a.n - lo < a.part_images ? a.n : lo + a.part_images;
-    const T *p = (const T *)a.grad_out + (int64_t)t * a.row_stride + at;
-    vec<float, V> sum = (vec<float, V>)0.0f;
-#pragma unroll 8
-    for (uint32_t i = lo; i < hi; ++i)
-        sum += to_f32<V, T>(load<T, V>(p + i * a.image_stride));
-    // columns of a group moved back are written twice, alike
-    store<float, V>(a.sums + ((int64_t)blockIdx.y * a.tokens + t) * a.dim + at, sum);
+    sum_columns<T>(a, blockIdx.x);
 }
 
 // Joins: the first workgroups add the splits of the weight's gradient, the
@@ -380,14 +358,8 @@ extern "C" int smol_patch_embed_backward(const smol_patch_grad_args *p, void *st
     a.out = part;
     a.image_stride = p->image_stride;
     a.row_stride = p->row_stride;
-    int e = hipSuccess;
-    if (p->grad_weight && a.rows > 0)
-        e = (s.type == SMOL_ELEM_F32   ? launch_patch_grad_f32
-             : s.type == SMOL_ELEM_F16 ? launch_patch_grad_f16
-                                       : launch_patch_grad_bf16)(a, s.image_type, plan.mode,
-                                                                 g.tile, stream);
-    if (e == hipSuccess && (p->grad_bias || p->grad_pos) && g.parts > 0) {
-        SumArgs b;
+    SumArgs b = {};
+    if ((p->grad_bias || p->grad_pos) && g.parts > 0) {
         b.grad_out = p->grad_out;
         b.sums = sums;
         b.image_stride = p->image_stride;
@@ -396,15 +368,22 @@ extern "C" int smol_patch_embed_backward(const smol_patch_grad_args *p, void *st
         b.tokens = plan.tokens;
         b.dim = a.dim;
         b.part_images = g.part_images;
-        const uint32_t V = a.dim >= 8 ? 8 : 1;
-        b.columns = make_divisor(ceil_div(a.dim, V));
-        const dim3 grid(ceil_div(plan.tokens * b.columns.d, 256), g.parts);
+        b.columns = make_divisor(ceil_div(a.dim, a.dim >= 8 ? 8 : 1));
+        b.per_part = make_divisor(ceil_div(plan.tokens * b.columns.d, 256));
+        b.groups = b.per_part.d * g.parts;
+    }
+    const bool beside = p->grad_weight && g.tile == 128;
+    int e = hipSuccess;
+    if (p->grad_weight && a.rows > 0)
+        e = (s.type == SMOL_ELEM_F32   ? launch_patch_grad_f32
+             : s.type == SMOL_ELEM_F16 ? launch_patch_grad_f16
+                                       : launch_patch_grad_bf16)(a, beside ? b : SumArgs{},
+                                                                 s.image_type, plan.mode, g.tile,
+                                                                 stream);
+    if (e == hipSuccess && b.groups > 0 && !beside) {
         with_type(s.type, [&](auto t) {
-            typedef decltype(t) T;
-            if (V == 8)
-                hipLaunchKernelGGL((patch_sum_kernel<T, 8>), grid, dim3(256), 0, hs, b);
-            else
-                hipLaunchKernelGGL((patch_sum_kernel<T, 1>), grid, dim3(256), 0, hs, b);
+            hipLaunchKernelGGL((patch_sum_kernel<decltype(t)>), dim3(b.groups), dim3(256), 0, hs,
+                               b);
         });
         e = hipGetLastError();
     }

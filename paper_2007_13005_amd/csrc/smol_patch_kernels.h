@@ -484,8 +484,16 @@ struct GradTile<float, Cols> {
 // images of 203 x 331, patches of 20, 380 columns: 33 us; the matrix units are
 // busy for 41 of 67 thousand cycles.
 template <typename T, typename S, int WD, int WP, int FD, int FP, int Mode>
-__global__ void __launch_bounds__(64 * WD * WP, 2) patch_grad_kernel(PatchArgs a)
+__global__ void __launch_bounds__(64 * WD * WP, 2) patch_grad_kernel(PatchArgs a, SumArgs b)
 {
+    if constexpr (WD * WP == 4) {
+        // further workgroups, beside these, for the sums of grad_out's columns
+        const uint32_t products = a.tiles * a.splits;
+        if (blockIdx.x >= products) {
+            sum_columns<T>(b, blockIdx.x - products);
+            return;
+        }
+    }
     static_assert(FD * WD == FP * WP, "square tiles");
     constexpr int C = 16 / sizeof(T), kWaves = WD * WP, kThreads = 64 * kWaves;
     constexpr int kSide = 16 * FD * WD;
@@ -646,20 +654,21 @@ __global__ void __launch_bounds__(64 * WD * WP, 2) patch_grad_kernel(PatchArgs a
 }
 
 template <typename T>
-int launch_patch_grad(const PatchArgs &a, int image_type, int mode, int tile, void *stream)
+int launch_patch_grad(const PatchArgs &a, const SumArgs &b, int image_type, int mode, int tile,
+                      void *stream)
 {
     with_image<T>(image_type, [&](auto s) {
         typedef decltype(s) S;
-        const dim3 grid(a.tiles * a.splits);
+        const dim3 grid(a.tiles * a.splits + b.groups);
         hipStream_t st = (hipStream_t)stream;
         const auto launch = [&](auto mode) {
             constexpr int M = mode.value;
             if constexpr (M == kWhole && sizeof(S) == 2 && sizeof(T) == 2) {
                 if (tile == 256)
-                    patch_grad_kernel<T, S, 4, 2, 4, 8, M><<<grid, dim3(512), 0, st>>>(a);
+                    patch_grad_kernel<T, S, 4, 2, 4, 8, M><<<grid, dim3(512), 0, st>>>(a, b);
             }
             if (tile == 128)
-                patch_grad_kernel<T, S, 2, 2, 4, 4, M><<<grid, dim3(256), 0, st>>>(a);
+                patch_grad_kernel<T, S, 2, 2, 4, 4, M><<<grid, dim3(256), 0, st>>>(a, b);
         };
         if (mode == kShort)
             launch(std::integral_constant<int, kShort>{});

@@ -278,6 +278,8 @@ def test_embed_widths(dim, kinds):
     (33, 1, 700, True), (64, 2, 12, True), (65, 7, 40, True), (777, 5003, 321, True),
     (1000, 4, 100, False), (4097, 300, 72, True), (8192, 1000, 16, True),
     (8193, 1000, 16, True), (20000, 511, 24, True), (20000, 512, 24, True),
+    (1023, 3, 40, True), (1024, 900, 520, True), (1025, 900, 520, True), (700, 5000, 3, True),
+    (1000, 1, 300, True), (40, 300000, 33, False), (5, 9000, 4100, False), (1024, 2, 8, False),
     (70001, 262143, 8, True), (70001, 262144, 8, True), (9000, 600000, 8, False),
     (3000, 600000, 8, False), (150000, 40, 4, False)])
 @pytest.mark.parametrize("kinds", [(F32, F32), (BF16, F32), (F16, F16)])
