@@ -213,7 +213,13 @@ GradPlan grad_plan(const smol_patch_shape &s, Plan *plan)
     if (s.dim < C)
         plan->mode = kShort;
     const bool large = plan->mode != kShort && elem_size(s.image_type) == 2 && C == 8;
-    g.tile = large ? 256 : 128;
+    // Large tiles where each compute unit has 20 of their steps or more: us of
+    // fp16 images of 224 x 224 in patches of 16 to 768 bf16 columns, sides 128 /
+    // 256: 1 image 15 / 26, 16: 26 / 36, 64: 40 / 49, 128: 72 / 72, 160: 83 / 80,
+    // 256: 117 / 106; to 256 columns, 512 images: 90 / 96.
+    const uint64_t large_steps =
+        (uint64_t)ceil_div(a.dim, 256) * ceil_div(width, 256) * ceil_div(a.rows, 64);
+    g.tile = large && large_steps >= 20 * 256 ? 256 : 128;
     const uint32_t at_once = g.tile == 256 || C == 4 ? 256 : 512;
     set_tiles(&a, ceil_div(a.dim, g.tile), ceil_div(width, g.tile));
     uint32_t splits = a.tiles < at_once ? at_once / a.tiles : 1;

@@ -361,7 +361,8 @@ PATCHES = [  # n, c, h, w, p, dim, nhwc
 LARGE = [(33, 3, 160, 176, 16, 1000, False), (70, 3, 140, 154, 14, 520, False),
          (61, 3, 112, 120, 14, 776, True), (130, 2, 63, 70, 7, 264, False),
          (97, 3, 224, 224, 16, 768, False), (260, 1, 112, 112, 8, 1030, True),
-         (11, 3, 224, 224, 16, 770, False), (9, 3, 210, 196, 14, 760, False)]
+         (11, 3, 224, 224, 16, 770, False), (9, 3, 210, 196, 14, 760, False),
+         (201, 3, 224, 224, 16, 780, False), (150, 3, 210, 224, 14, 1000, True)]
 KINDS = [(F32, F32), (F16, F32), (F16, F16), (F32, F16), (F16, BF16), (F32, BF16), (BF16, BF16)]
 
 
