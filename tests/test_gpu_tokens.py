@@ -607,10 +607,12 @@ def test_sequence_on_another_stream():
     assert torch.equal(got, want)
 
 
-def test_sequence_in_a_graph():
+@pytest.mark.parametrize("text", [40, 300, 2500])
+def test_sequence_in_a_graph(text):
     """Captured once, replayed with new inputs between eager work: every
-    replay gives the eager bits."""
-    s, eager = sequence_state(3), sequence_state(3)
+    replay gives the eager bits (the ids' gradient without a sort, with one by
+    counting and with one by digits)."""
+    s, eager = sequence_state(3, text=text), sequence_state(3, text=text)
     st = torch.cuda.Stream()
     st.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(st):
@@ -620,7 +622,7 @@ def test_sequence_in_a_graph():
     with torch.cuda.graph(graph):
         sequence_step(s)
     for turn in range(4):
-        new = sequence_state(10 + turn)
+        new = sequence_state(10 + turn, text=text)
         for k in ("ids", "images", "table", "top"):
             s[k].copy_(new[k])
             eager[k].copy_(new[k])
