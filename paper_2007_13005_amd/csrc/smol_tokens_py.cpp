@@ -87,8 +87,10 @@ int elem(const at::Tensor &t, const char *name)
     }
 }
 
+// What is read, and what is written: only the latter gives a lazily cloned
+// tensor memory of its own, which its source then does not share.
 const void *ptr(const at::Tensor *t) { return t ? t->const_data_ptr() : nullptr; }
-void *out_ptr(const at::Tensor *t) { return t ? const_cast<void *>(t->const_data_ptr()) : nullptr; }
+void *out_ptr(const at::Tensor *t) { return t ? t->mutable_data_ptr() : nullptr; }
 
 // Rows of `dim` dense elements a constant stride apart; rows < 0: any number.
 int64_t rows_of(const at::Tensor &t, int64_t dim, const char *name, int64_t rows, int64_t *stride)
@@ -161,7 +163,6 @@ int32_t small(int64_t v)  // past 32 bits: a size that the library refuses
 template <typename F>
 PyObject *launch(PyObject *stream, const Tensors &t, F f)
 {
-    t.check_device();
     void *s = stream == Py_None
                   ? (void *)c10::hip::getCurrentHIPStream((c10::DeviceIndex)t.device).stream()
                   : PyLong_AsVoidPtr(stream);
@@ -251,6 +252,7 @@ PyObject *patch_embed(PyObject *const *o)
     strides_of(out, a.shape, "out", &a.image_stride, &a.row_stride);
     vector(bias, a.shape.dim, weight.scalar_type(), "bias");
     vector(pos, tokens_of(a.shape) * a.shape.dim, weight.scalar_type(), "pos");
+    all.check_device();
     a.images = ptr(&images);
     a.weight = ptr(&weight);
     a.bias = ptr(bias);
@@ -277,6 +279,7 @@ PyObject *patch_embed_backward(PyObject *const *o)
     vector(pos, tokens_of(a.shape) * a.shape.dim, weight.scalar_type(), "grad_pos");
     const at::Tensor &room = *all.take(o[7], "workspace");
     workspace(room, lib.patch_bytes(&a.shape));
+    all.check_device();
     a.grad_out = ptr(&grad_out);
     a.images = ptr(&images);
     a.grad_weight = out_ptr(&weight);
@@ -313,6 +316,7 @@ PyObject *embed(PyObject *const *o)
     a.out_type = elem(out, "out");
     a.scale = (float)number(o[2]);
     a.keep = (int32_t)integer(o[4]);
+    all.check_device();
     a.ids = ptr(&ids);
     a.table = ptr(&table);
     a.out = out_ptr(&out);
@@ -340,6 +344,7 @@ PyObject *embed_backward(PyObject *const *o)
     a.accumulate = (int32_t)integer(o[5]);
     const at::Tensor &room = *all.take(o[6], "workspace");
     workspace(room, lib.embed_bytes(a.n, a.vocab, a.dim));
+    all.check_device();
     a.grad_out = ptr(&grad_out);
     a.ids = ptr(&ids);
     a.grad_table = out_ptr(&table);
@@ -391,14 +396,15 @@ PyObject *layer_norm(PyObject *const *o)
     a.weight_type = w == at::kFloat ? SMOL_ELEM_F32 : w == at::kHalf ? SMOL_ELEM_F16
                                                                      : SMOL_ELEM_BF16;
     a.eps = (float)number(o[3]);
+    all.check_device();
+    a.out = out_ptr(&out);  // first: x and residual may be these
+    a.sum = out_ptr(sum);
+    a.mean = (float *)out_ptr(mean);
+    a.rstd = (float *)out_ptr(rstd);
     a.x = ptr(&x);
     a.residual = ptr(residual);
     a.weight = ptr(weight);
     a.bias = ptr(bias);
-    a.out = out_ptr(&out);
-    a.sum = out_ptr(sum);
-    a.mean = (float *)out_ptr(mean);
-    a.rstd = (float *)out_ptr(rstd);
     return launch(o[9], all, [&](void *s) { return lib.norm(&a, s); });
 }
 
@@ -438,16 +444,17 @@ PyObject *layer_norm_backward(PyObject *const *o)
     a.accumulate = (int32_t)integer(o[9]);
     const at::Tensor &room = *all.take(o[10], "workspace");
     workspace(room, lib.norm_bytes(a.rows, a.dim));
+    all.check_device();
+    a.grad_x = out_ptr(&grad_x);  // first: an input may be it
+    a.grad_weight = out_ptr(grad_weight);
+    a.grad_bias = out_ptr(grad_bias);
+    a.workspace = out_ptr(&room);
     a.grad_out = ptr(&grad_out);
     a.h = ptr(&h);
     a.grad_sum = ptr(grad_sum);
     a.weight = ptr(weight);
     a.mean = (const float *)ptr(mean);
     a.rstd = (const float *)ptr(rstd);
-    a.grad_x = out_ptr(&grad_x);
-    a.grad_weight = out_ptr(grad_weight);
-    a.grad_bias = out_ptr(grad_bias);
-    a.workspace = out_ptr(&room);
     a.workspace_bytes = room.numel();
     return launch(o[11], all, [&](void *s) { return lib.norm_backward(&a, s); });
 }

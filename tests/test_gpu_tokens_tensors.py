@@ -1,0 +1,88 @@
+"""What the token operators do with torch's tensors beside their values:
+memory that another tensor shares lazily, autograd's record of writes."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2007_13005_amd import tokens
+
+pytestmark = pytest.mark.gpu
+
+F32 = torch.float32
+
+
+def calls():
+    """name -> (function, keyword arguments, names of those that are written)."""
+    g = torch.Generator().manual_seed(0)
+
+    def new(*shape):
+        return torch.randn(shape, generator=g).cuda()
+
+    def room(n):
+        return torch.zeros(n, dtype=torch.uint8, device="cuda")
+
+    rows, dim, vocab = 40, 72, 50
+    x, w = new(rows, dim), new(dim)
+    mean, rstd = x.mean(1), 1 / x.std(1)
+    ids = torch.randint(0, vocab, (rows,), generator=g).cuda()
+    img, proj, dy = new(2, 3, 32, 32), new(24, 3, 16, 16), new(2, 4, 24)
+    return {
+        "layer_norm": (tokens.layer_norm, dict(
+            x=x, weight=w, residual=x.clone(), out=new(rows, dim), sum_out=new(rows, dim),
+            mean=new(rows), rstd=new(rows)), ("out", "sum_out", "mean", "rstd")),
+        "layer_norm_backward": (tokens.layer_norm_backward, dict(
+            grad_out=new(rows, dim), h=x, weight=w, mean=mean, rstd=rstd, grad_x=new(rows, dim),
+            grad_weight=new(dim), grad_bias=new(dim), accumulate=True,
+            workspace=room(tokens.layer_norm_workspace_bytes(rows, dim))),
+            ("grad_x", "grad_weight", "grad_bias", "workspace")),
+        "embed": (tokens.embed, dict(ids=ids, table=new(vocab, dim), out=new(rows, dim)),
+                  ("out",)),
+        "embed_backward": (tokens.embed_backward, dict(
+            grad_out=new(1100, dim), ids=torch.randint(0, vocab, (1100,), generator=g).cuda(),
+            grad_table=new(vocab, dim), accumulate=True,
+            workspace=room(tokens.embed_workspace_bytes(1100, vocab, dim))),
+            ("grad_table", "workspace")),
+        "patch_embed": (tokens.patch_embed, dict(images=img, weight=proj, out=new(2, 4, 24)),
+                        ("out",)),
+        "patch_embed_backward": (tokens.patch_embed_backward, dict(
+            grad_out=dy, images=img, grad_weight=new(24, 3, 16, 16), grad_bias=new(24),
+            grad_pos=new(4, 24), accumulate=True,
+            workspace=room(tokens.patch_embed_workspace_bytes(img, proj, F32))),
+            ("grad_weight", "grad_bias", "grad_pos", "workspace")),
+    }
+
+
+NAMES = ["layer_norm", "layer_norm_backward", "embed", "embed_backward", "patch_embed",
+         "patch_embed_backward"]
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_lazy_clones_are_separated(name):
+    """What is written of a lazily cloned tensor does not reach its source."""
+    function, args, written = calls()[name]
+    before = {k: args[k].clone() for k in written}
+    sources = {k: args[k] for k in written}
+    lazy = {k: torch._lazy_clone(v) for k, v in sources.items()}
+    function(**dict(args, **lazy))
+    for k in written:
+        assert torch.equal(sources[k], before[k]), k
+    function(**args)
+    for k in written:
+        if k != "workspace":
+            assert torch.equal(lazy[k], args[k]), k
+            assert not torch.equal(args[k], before[k]), k
+
+
+def test_lazy_clones_in_place():
+    """An input that is the output, lazily cloned: the result has memory of its own."""
+    x = torch.randn((40, 72), device="cuda")
+    before, lazy = x.clone(), torch._lazy_clone(x)
+    y = tokens.layer_norm(lazy, out=lazy)[0]
+    assert y is lazy and torch.equal(x, before)
+    assert torch.equal(y, tokens.layer_norm(x)[0])
+    mean, rstd = x.mean(1), 1 / x.std(1)
+    want = tokens.layer_norm_backward(x, x, None, mean, rstd)[0]
+    lazy = torch._lazy_clone(x)
+    assert tokens.layer_norm_backward(lazy, lazy, None, mean, rstd, lazy)[0] is lazy
+    assert torch.equal(x, before) and torch.equal(lazy, want)
