@@ -19,6 +19,7 @@
 #include <cstdio>
 #include <exception>
 
+#include "smol.h"
 #include "smol_tokens.h"
 
 namespace {
@@ -75,6 +76,29 @@ struct Tensors {
         if (device < 0 || device != c10::hip::current_device())
             wrong("tensors must be on the current device");
     }
+    // The address of a tensor that the call writes (or null). Asked for as
+    // such it gives a lazily cloned tensor memory of its own, which its source
+    // then does not share.
+    void *write(const at::Tensor *t)
+    {
+        if (!t)
+            return nullptr;
+        written[writes++] = t;
+        return t->mutable_data_ptr();
+    }
+    // After the call: autograd counts the writes, and refuses a backward pass
+    // that needs what was overwritten. (Inference tensors have no count, and
+    // autograd saves none.)
+    void count_writes() const
+    {
+        for (int k = 0; k < writes; ++k)
+            if (!written[k]->is_inference())
+                written[k]->unsafeGetTensorImpl()->bump_version();
+    }
+
+private:
+    const at::Tensor *written[4];  // no call writes more
+    int writes = 0;
 };
 
 int elem(const at::Tensor &t, const char *name)
@@ -87,10 +111,7 @@ int elem(const at::Tensor &t, const char *name)
     }
 }
 
-// What is read, and what is written: only the latter gives a lazily cloned
-// tensor memory of its own, which its source then does not share.
 const void *ptr(const at::Tensor *t) { return t ? t->const_data_ptr() : nullptr; }
-void *out_ptr(const at::Tensor *t) { return t ? t->mutable_data_ptr() : nullptr; }
 
 // Rows of `dim` dense elements a constant stride apart; rows < 0: any number.
 int64_t rows_of(const at::Tensor &t, int64_t dim, const char *name, int64_t rows, int64_t *stride)
@@ -172,6 +193,8 @@ PyObject *launch(PyObject *stream, const Tensors &t, F f)
     Py_BEGIN_ALLOW_THREADS
     status = f(s);
     Py_END_ALLOW_THREADS
+    if (status == SMOL_OK || status == SMOL_ERR_HIP)  // else nothing was enqueued
+        t.count_writes();
     return PyLong_FromLong(status);
 }
 
@@ -257,7 +280,7 @@ PyObject *patch_embed(PyObject *const *o)
     a.weight = ptr(&weight);
     a.bias = ptr(bias);
     a.pos = ptr(pos);
-    a.out = out_ptr(&out);
+    a.out = all.write(&out);
     return launch(o[6], all, [&](void *s) { return lib.patch(&a, s); });
 }
 
@@ -282,10 +305,10 @@ PyObject *patch_embed_backward(PyObject *const *o)
     all.check_device();
     a.grad_out = ptr(&grad_out);
     a.images = ptr(&images);
-    a.grad_weight = out_ptr(&weight);
-    a.grad_bias = out_ptr(bias);
-    a.grad_pos = out_ptr(pos);
-    a.workspace = out_ptr(&room);
+    a.grad_weight = all.write(&weight);
+    a.grad_bias = all.write(bias);
+    a.grad_pos = all.write(pos);
+    a.workspace = all.write(&room);
     a.workspace_bytes = room.numel();
     return launch(o[8], all, [&](void *s) { return lib.patch_backward(&a, s); });
 }
@@ -319,7 +342,7 @@ PyObject *embed(PyObject *const *o)
     all.check_device();
     a.ids = ptr(&ids);
     a.table = ptr(&table);
-    a.out = out_ptr(&out);
+    a.out = all.write(&out);
     return launch(o[5], all, [&](void *s) { return lib.embed(&a, s); });
 }
 
@@ -347,8 +370,8 @@ PyObject *embed_backward(PyObject *const *o)
     all.check_device();
     a.grad_out = ptr(&grad_out);
     a.ids = ptr(&ids);
-    a.grad_table = out_ptr(&table);
-    a.workspace = out_ptr(&room);
+    a.grad_table = all.write(&table);
+    a.workspace = all.write(&room);
     a.workspace_bytes = room.numel();
     return launch(o[7], all, [&](void *s) { return lib.embed_backward(&a, s); });
 }
@@ -397,10 +420,10 @@ PyObject *layer_norm(PyObject *const *o)
                                                                      : SMOL_ELEM_BF16;
     a.eps = (float)number(o[3]);
     all.check_device();
-    a.out = out_ptr(&out);  // first: x and residual may be these
-    a.sum = out_ptr(sum);
-    a.mean = (float *)out_ptr(mean);
-    a.rstd = (float *)out_ptr(rstd);
+    a.out = all.write(&out);  // first: x and residual may be these
+    a.sum = all.write(sum);
+    a.mean = (float *)all.write(mean);
+    a.rstd = (float *)all.write(rstd);
     a.x = ptr(&x);
     a.residual = ptr(residual);
     a.weight = ptr(weight);
@@ -445,10 +468,10 @@ PyObject *layer_norm_backward(PyObject *const *o)
     const at::Tensor &room = *all.take(o[10], "workspace");
     workspace(room, lib.norm_bytes(a.rows, a.dim));
     all.check_device();
-    a.grad_x = out_ptr(&grad_x);  // first: an input may be it
-    a.grad_weight = out_ptr(grad_weight);
-    a.grad_bias = out_ptr(grad_bias);
-    a.workspace = out_ptr(&room);
+    a.grad_x = all.write(&grad_x);  // first: an input may be it
+    a.grad_weight = all.write(grad_weight);
+    a.grad_bias = all.write(grad_bias);
+    a.workspace = all.write(&room);
     a.grad_out = ptr(&grad_out);
     a.h = ptr(&h);
     a.grad_sum = ptr(grad_sum);

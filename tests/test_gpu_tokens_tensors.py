@@ -86,3 +86,38 @@ def test_lazy_clones_in_place():
     lazy = torch._lazy_clone(x)
     assert tokens.layer_norm_backward(lazy, lazy, None, mean, rstd, lazy)[0] is lazy
     assert torch.equal(x, before) and torch.equal(lazy, want)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_writes_are_counted(name):
+    """A buffer that autograd saved and a call wrote since is not used as if it
+    had not been: backward raises, as after torch's own writes in place."""
+    function, args, written = calls()[name]
+    for k in written:
+        if k == "workspace":
+            continue
+        factor = torch.ones_like(args[k], requires_grad=True)
+        loss = (args[k] * factor).sum()  # saves args[k]
+        function(**args)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    counts = {k: v._version for k, v in args.items() if torch.is_tensor(v)}
+    function(**args)
+    for k, v in counts.items():
+        assert (args[k]._version > v) == (k in written), k
+
+
+def test_refused_calls_count_no_write():
+    x, out = torch.randn((4, 72), device="cuda"), torch.zeros((4, 72), device="cuda")
+    with pytest.raises(ValueError):
+        tokens.layer_norm(x, out=out, weight=torch.zeros(3, device="cuda"))
+    with pytest.raises(tokens.SmolError):
+        tokens.layer_norm(x, out=out, eps=-1.0)
+    assert out._version == 0
+
+
+def test_inference_tensors_are_written():
+    with torch.inference_mode():
+        x, out = torch.randn((4, 72), device="cuda"), torch.zeros((4, 72), device="cuda")
+    y = tokens.layer_norm(x, out=out)[0]
+    assert y is out and torch.equal(y, tokens.layer_norm(x.clone())[0])
