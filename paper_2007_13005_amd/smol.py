@@ -440,6 +440,15 @@ def _out_tensor(out, n: int, params: Params, device, layout: int = LAYOUT_NCHW):
     return out
 
 
+def _count_writes(*given) -> None:
+    """After a call: autograd counts the writes to the buffers that the caller
+    gave (None: made by the call), and refuses a backward pass that needs what
+    was overwritten."""
+    for t in given:
+        if t is not None:
+            _torch.autograd.graph.increment_version(t)
+
+
 def _rois(rois, n: int):
     if rois is None:
         return None
@@ -469,6 +478,7 @@ def preprocess_batch(src, offsets, widths, heights, params: Params, pitches=None
         raise ValueError("table lengths differ")
     r = _rois(rois, n)
     _struct_types(params, options)
+    given = out
     out = _out_tensor(out, n, params, src.device, options.layout if options else LAYOUT_NCHW)
     if r is None and options is None:
         _call("smol_preprocess_batch", src.data_ptr(), src.numel(), off, w, h, pt, n, params,
@@ -476,6 +486,7 @@ def preprocess_batch(src, offsets, widths, heights, params: Params, pitches=None
     else:
         _call("smol_preprocess_batch_ex", src.data_ptr(), src.numel(), off, w, h, pt, r, n,
               params, options, out.data_ptr(), _launch_stream(stream, src, out))
+    _count_writes(given)
     return out
 
 
@@ -496,6 +507,7 @@ def yuv420_preprocess_batch(src, y_offsets, cb_offsets, cr_offsets, widths, heig
         raise ValueError("table lengths differ")
     r = _rois(rois, n)
     _struct_types(params, options)
+    given = out
     out = _out_tensor(out, n, params, src.device, options.layout if options else LAYOUT_NCHW)
     if r is None and options is None:
         _call("smol_yuv420_preprocess_batch", src.data_ptr(), src.numel(), yo, bo, ro, w, h, n,
@@ -503,6 +515,7 @@ def yuv420_preprocess_batch(src, y_offsets, cb_offsets, cr_offsets, widths, heig
     else:
         _call("smol_yuv420_preprocess_batch_ex", src.data_ptr(), src.numel(), yo, bo, ro, w, h,
               r, n, params, options, out.data_ptr(), _launch_stream(stream, src, out))
+    _count_writes(given)
     return out
 
 
@@ -536,11 +549,13 @@ def lowres_preprocess_batch(src, offsets, widths, heights, params: Params, low_r
     if not (len(w) == len(h) == n and (pt is None or len(pt) == n)):
         raise ValueError("table lengths differ")
     _struct_types(params, None)
+    given = out
     out = _out_tensor(out, n, params, src.device)
     ws = _workspace(workspace, n, low_res, src.device)
     _call("smol_lowres_preprocess_batch", src.data_ptr(), src.numel(), off, w, h, pt, n,
           operator.index(low_res), params, ws.data_ptr(), ws.numel(), out.data_ptr(),
           _launch_stream(stream, src, out, ws))
+    _count_writes(given, workspace)
     return out
 
 
@@ -559,11 +574,13 @@ def yuv420_lowres_preprocess_batch(src, y_offsets, cb_offsets, cr_offsets, width
     if not (len(bo) == len(ro) == len(w) == len(h) == n):
         raise ValueError("table lengths differ")
     _struct_types(params, None)
+    given = out
     out = _out_tensor(out, n, params, src.device)
     ws = _workspace(workspace, n, low_res, src.device)
     _call("smol_yuv420_lowres_preprocess_batch", src.data_ptr(), src.numel(), yo, bo, ro, w, h,
           n, operator.index(low_res), params, ws.data_ptr(), ws.numel(), out.data_ptr(),
           _launch_stream(stream, src, out, ws))
+    _count_writes(given, workspace)
     return out
 
 
@@ -617,6 +634,7 @@ def jpeg_decode_i420(coef, coef_offsets, qtables, widths, heights, out, y_offset
     _call("smol_jpeg_decode_i420", coef.data_ptr(), coef.numel(), co, q, nq, w, h, r, n,
           operator.index(coef_layout), out.data_ptr(), out.numel(), yo, bo, ro,
           _launch_stream(stream, coef, out))
+    _count_writes(out)
 
 
 def jpeg_workspace_bytes(widths, heights) -> int:
@@ -636,6 +654,7 @@ def jpeg_roi_preprocess_batch(coef, coef_offsets, qtables, widths, heights, para
     w, h = _table(widths, np.int32), _table(heights, np.int32)
     n = len(co)
     q, nq = _qtables(qtables, n)
+    given = out, workspace
     need = jpeg_workspace_bytes(w, h)
     if workspace is None:
         workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=coef.device)
@@ -644,6 +663,7 @@ def jpeg_roi_preprocess_batch(coef, coef_offsets, qtables, widths, heights, para
     _call("smol_jpeg_roi_preprocess_batch", coef.data_ptr(), coef.numel(), co, q, nq, w, h, n,
           operator.index(coef_layout), params, options, workspace.data_ptr(), workspace.numel(),
           out.data_ptr(), _launch_stream(stream, coef, out, workspace))
+    _count_writes(*given)
     return out
 
 
