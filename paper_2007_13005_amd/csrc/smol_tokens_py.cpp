@@ -64,6 +64,9 @@ struct Tensors {
             throw Raised();
         }
         const at::Tensor &t = THPVariable_Unpack(o);
+        // a lazy negation is not in the memory that the kernels read and write
+        if (t.is_neg())
+            wrong("%s is a lazily negated view: pass its resolve_neg()", name);
         const int at = t.is_cuda() ? t.get_device() : -1;
         if (device == -2)
             device = at;

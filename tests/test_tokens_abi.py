@@ -292,3 +292,24 @@ def test_binding_refusals():
         tokens.embed([1, 2], x, out=x)
     with pytest.raises(TypeError):
         tokens.embed(ids, torch.zeros((5, 8)), "a")
+
+
+def test_binding_refuses_lazily_negated_views():
+    """Their memory holds the values' negatives, which the kernels would take."""
+    x = torch.zeros((4, 8))
+    negated = torch.zeros((4, 8), dtype=torch.complex64).conj().imag[:, :4]
+    assert negated.is_neg()
+    ids = torch.zeros(4, dtype=torch.int64)
+    img, weight = torch.zeros((1, 3, 16, 16)), torch.zeros((8, 3, 16, 16))
+    for function, args in ((tokens.layer_norm, (torch._neg_view(x),)),
+                           (tokens.layer_norm, (negated,)),
+                           (tokens.embed, (ids, torch._neg_view(x))),
+                           (tokens.embed_backward, (torch._neg_view(x), ids, x)),
+                           (tokens.patch_embed, (torch._neg_view(img), weight)),
+                           (tokens.patch_embed, (img, weight, torch._neg_view(x)[0])),
+                           (tokens.patch_embed_backward,
+                            (torch.zeros((1, 1, 8)), img, torch._neg_view(weight)))):
+        with pytest.raises(ValueError, match="resolve_neg"):
+            function(*args)
+    with pytest.raises(ValueError, match="resolve_neg"):
+        tokens.layer_norm(x, out=torch._neg_view(x.clone()))
