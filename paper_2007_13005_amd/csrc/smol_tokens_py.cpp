@@ -11,6 +11,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -18,6 +19,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <exception>
+#include <initializer_list>
 
 #include "smol.h"
 #include "smol_tokens.h"
@@ -201,6 +203,24 @@ PyObject *launch(PyObject *stream, const Tensors &t, F f)
     return PyLong_FromLong(status);
 }
 
+// The forward calls record nothing for autograd: a result that a graph was
+// asked for comes with a warning, not in silence.
+void warn_no_graph(const char *call, std::initializer_list<const at::Tensor *> inputs)
+{
+    if (!c10::GradMode::is_enabled())
+        return;
+    for (const at::Tensor *t : inputs)
+        if (t && t->requires_grad()) {
+            if (PyErr_WarnFormat(PyExc_UserWarning, 2,
+                                 "%s: an input requires grad, and the result has no graph; "
+                                 "%s_backward gives the gradients (call under torch.no_grad() or "
+                                 "in an autograd function's forward)",
+                                 call, call) < 0)
+                throw Raised();
+            return;
+        }
+}
+
 // An entry: the number of arguments checked, exceptions turned into Python's.
 template <int N, PyObject *(*F)(PyObject *const *)>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t count)
@@ -284,6 +304,7 @@ PyObject *patch_embed(PyObject *const *o)
     a.bias = ptr(bias);
     a.pos = ptr(pos);
     a.out = all.write(&out);
+    warn_no_graph("patch_embed", {&images, &weight, bias, pos});
     return launch(o[6], all, [&](void *s) { return lib.patch(&a, s); });
 }
 
@@ -346,6 +367,7 @@ PyObject *embed(PyObject *const *o)
     a.ids = ptr(&ids);
     a.table = ptr(&table);
     a.out = all.write(&out);
+    warn_no_graph("embed", {&table});
     return launch(o[5], all, [&](void *s) { return lib.embed(&a, s); });
 }
 
@@ -431,6 +453,7 @@ PyObject *layer_norm(PyObject *const *o)
     a.residual = ptr(residual);
     a.weight = ptr(weight);
     a.bias = ptr(bias);
+    warn_no_graph("layer_norm", {&x, residual, weight, bias});
     return launch(o[9], all, [&](void *s) { return lib.norm(&a, s); });
 }
 

@@ -8,8 +8,11 @@ last dimension is dense; leading dimensions count as rows, and the rows must
 lie a constant stride apart. Outputs and workspaces are allocated where they
 are not given; a loop keeps its own. Wrong shapes, types and devices raise
 ValueError before anything is called (the checks are the native module's,
-``csrc/smol_tokens_py.cpp``). The backward functions are plain calls, not
-autograd nodes.
+``csrc/smol_tokens_py.cpp``). All are plain calls, not
+autograd nodes: a forward call with an input that requires grad warns (unless
+grad mode is off, as it is in an autograd function's ``forward``), and the
+backward functions give the gradients. Autograd does count the writes to given
+buffers, as it does those of torch's own operations.
 """
 from __future__ import annotations
 

@@ -2,6 +2,8 @@
 memory that another tensor shares lazily, autograd's record of writes."""
 from __future__ import annotations
 
+import warnings
+
 import pytest
 import torch
 
@@ -121,3 +123,51 @@ def test_inference_tensors_are_written():
         x, out = torch.randn((4, 72), device="cuda"), torch.zeros((4, 72), device="cuda")
     y = tokens.layer_norm(x, out=out)[0]
     assert y is out and torch.equal(y, tokens.layer_norm(x.clone())[0])
+
+
+@pytest.mark.parametrize("name, inputs", [("layer_norm", ("x", "weight", "residual")),
+                                          ("embed", ("table",)),
+                                          ("patch_embed", ("images", "weight"))])
+def test_results_without_a_graph_warn(name, inputs):
+    function, args, _ = calls()[name]
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        function(**args)
+        for k in inputs:
+            asked = dict(args, **{k: args[k].clone().requires_grad_()})
+            with torch.no_grad():
+                function(**asked)
+            with pytest.raises(UserWarning, match=f"no graph; {name}_backward"):
+                function(**asked)
+    with pytest.warns(UserWarning) as seen:
+        function(**asked)
+    assert seen[0].filename == __file__  # the caller's line
+
+
+class Norm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias):
+        y, _, mean, rstd = tokens.layer_norm(x, weight, bias)
+        ctx.save_for_backward(x, weight, mean, rstd)
+        return y
+
+    @staticmethod
+    def backward(ctx, grad):
+        x, weight, mean, rstd = ctx.saved_tensors
+        return tokens.layer_norm_backward(grad, x, weight, mean, rstd, None,
+                                          torch.empty_like(weight), torch.empty_like(weight))
+
+
+def test_calls_in_an_autograd_function():
+    g = torch.Generator().manual_seed(1)
+    args = [torch.randn(s, generator=g).cuda().requires_grad_() for s in ((40, 72), (72,), (72,))]
+    top = torch.randn((40, 72), generator=g).cuda()
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        Norm.apply(*args).backward(top)
+    _, _, mean, rstd = tokens.layer_norm(args[0].detach())
+    want = tokens.layer_norm_backward(top, args[0].detach(), args[1].detach(), mean, rstd, None,
+                                      torch.empty(72, device="cuda"),
+                                      torch.empty(72, device="cuda"))
+    for a, w in zip(args, want):
+        assert torch.equal(a.grad, w)
