@@ -357,6 +357,17 @@ extern "C" int smol_patch_embed_backward(const smol_patch_grad_args *p, void *st
                          (long long)g.bytes);
     if (!p->grad_weight && !p->grad_bias && !p->grad_pos)
         return SMOL_OK;
+    // The join's workgroups; of 256 threads a launch takes less than 2^24. (Of
+    // the products' tiles and the sums' parts the limits allow fewer.)
+    const uint32_t weight_groups =
+        p->grad_weight ? (uint32_t)(((int64_t)a.dim * a.chunks + 255) / 256) : 0;
+    const uint32_t pos_groups = p->grad_pos ? ceil_div(plan.tokens * a.dim, 256) : 0;
+    const uint32_t join_groups =
+        weight_groups + pos_groups + (p->grad_bias ? ceil_div(a.dim, 8) : 0);
+    if (join_groups >= 1 << 24)
+        return set_error(SMOL_ERR_UNSUPPORTED,
+                         "gradients of %lld and %lld values: too many for a launch",
+                         (long long)a.dim * a.values, (long long)plan.tokens * a.dim);
     hipStream_t hs = (hipStream_t)stream;
     float *part = (float *)p->workspace, *sums = (float *)((char *)p->workspace + g.sums);
     a.images = p->images;
@@ -405,11 +416,9 @@ extern "C" int smol_patch_embed_backward(const smol_patch_grad_args *p, void *st
         j.parts = g.parts;
         j.chunks = make_divisor(a.chunks);
         j.accumulate = p->accumulate;
-        j.weight_groups =
-            p->grad_weight ? (uint32_t)(((int64_t)a.dim * a.chunks + 255) / 256) : 0;
-        j.pos_groups = p->grad_pos ? ceil_div(plan.tokens * a.dim, 256) : 0;
-        const dim3 grid(j.weight_groups + j.pos_groups +
-                        (p->grad_bias ? ceil_div(a.dim, 8) : 0));
+        j.weight_groups = weight_groups;
+        j.pos_groups = pos_groups;
+        const dim3 grid(join_groups);
         if (grid.x > 0)
             with_type(p->grad_type, [&](auto t) {
                 typedef decltype(t) P;

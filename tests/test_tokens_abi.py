@@ -313,3 +313,12 @@ def test_binding_refuses_lazily_negated_views():
             function(*args)
     with pytest.raises(ValueError, match="resolve_neg"):
         tokens.layer_norm(x, out=torch._neg_view(x.clone()))
+
+
+def test_patch_gradients_past_a_launch():
+    """Every size within its limit, and more joins than one launch takes:
+    refused before anything is enqueued, not by the last of the launches."""
+    large = dict(n=1, channels=32767, height=181, width=181, patch=1, dim=65536, image_stride=0,
+                 row_stride=0)
+    assert call("smol_patch_embed_backward", **large) == UNSUPPORTED
+    assert b"too many for a launch" in smol.lib().smol_last_error()
