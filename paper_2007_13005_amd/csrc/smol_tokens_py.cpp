@@ -240,30 +240,56 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t count)
     return nullptr;
 }
 
-smol_patch_shape shape_of(const at::Tensor &images, const at::Tensor &weight, int64_t layout,
+// The type of the weights among those given (float32 where none is).
+at::ScalarType weight_type(const at::Tensor *a, const at::Tensor *b, const at::Tensor *c,
+                           const char *name = "weight")
+{
+    const at::Tensor *t = a ? a : b ? b : c;
+    if (!t)
+        return at::kFloat;
+    elem(*t, name);
+    return t->scalar_type();
+}
+
+int elem_of(at::ScalarType type)  // one of the three
+{
+    return type == at::kFloat ? SMOL_ELEM_F32 : type == at::kHalf ? SMOL_ELEM_F16 : SMOL_ELEM_BF16;
+}
+
+smol_patch_shape shape_of(const at::Tensor &images, int64_t patch, int64_t dim, int64_t layout,
                           int type)
 {
     if (layout != 0 && layout != 1)
         wrong("layout %lld unknown", (long long)layout);
-    if (images.dim() != 4 || weight.dim() != 4 || !images.is_contiguous() ||
-        !weight.is_contiguous())
-        wrong("weight and images must be contiguous tensors of four dimensions");
+    if (images.dim() != 4 || !images.is_contiguous())
+        wrong("images must be a contiguous tensor of four dimensions");
     const bool nhwc = layout == 1;
-    const auto w = weight.sizes(), i = images.sizes();
-    const int64_t ch = nhwc ? w[3] : w[1], p = nhwc ? w[1] : w[2], q = nhwc ? w[2] : w[3];
-    if (p != q || ch != (nhwc ? i[3] : i[1]))
-        wrong("weight does not fit the images");
+    const auto i = images.sizes();
     smol_patch_shape s = {};
     s.n = small(i[0]);
-    s.channels = small(ch);
+    s.channels = small(nhwc ? i[3] : i[1]);
     s.height = small(nhwc ? i[1] : i[2]);
     s.width = small(nhwc ? i[2] : i[3]);
-    s.patch = small(p);
-    s.dim = small(w[0]);
+    s.patch = small(patch);
+    s.dim = small(dim);
     s.layout = (int32_t)layout;
     s.image_type = elem(images, "images");
     s.type = type;
     if (s.patch < 1)
+        wrong("a patch's side must be 1 or more");
+    return s;
+}
+
+smol_patch_shape shape_of(const at::Tensor &images, const at::Tensor &weight, int64_t layout,
+                          int type)
+{
+    if (weight.dim() != 4 || !weight.is_contiguous())
+        wrong("weight must be a contiguous tensor of four dimensions");
+    const bool nhwc = layout == 1;
+    const auto w = weight.sizes();
+    const int64_t p = nhwc ? w[1] : w[2], q = nhwc ? w[2] : w[3];
+    const smol_patch_shape s = shape_of(images, p, w[0], layout, type);
+    if (p != q || (nhwc ? w[3] : w[1]) != images.size(nhwc ? 3 : 1))
         wrong("weight does not fit the images");
     return s;
 }
@@ -309,27 +335,37 @@ PyObject *patch_embed(PyObject *const *o)
 }
 
 // grad_out, images, grad_weight, grad_bias, grad_pos, layout, accumulate,
-// workspace, stream
+// workspace, stream, patch
 PyObject *patch_embed_backward(PyObject *const *o)
 {
     Tensors all;
     const at::Tensor &grad_out = *all.take(o[0], "grad_out"), &images = *all.take(o[1], "images");
-    const at::Tensor &weight = *all.take(o[2], "grad_weight");
+    const at::Tensor *weight = all.take(o[2], "grad_weight", true);
     const at::Tensor *bias = all.take(o[3], "grad_bias", true);
     const at::Tensor *pos = all.take(o[4], "grad_pos", true);
     smol_patch_grad_args a = {};
-    a.shape = shape_of(images, weight, integer(o[5]), elem(grad_out, "grad_out"));
-    a.grad_type = elem(weight, "grad_weight");
+    const int type = elem(grad_out, "grad_out");
+    if (!weight && o[9] == Py_None)
+        wrong("without grad_weight the patch's side must be given");
+    if (!weight)
+        a.shape = shape_of(images, integer(o[9]), grad_out.dim() ? grad_out.size(-1) : 0,
+                           integer(o[5]), type);
+    else
+        a.shape = shape_of(images, *weight, integer(o[5]), type);
+    if (o[9] != Py_None && integer(o[9]) != a.shape.patch)
+        wrong("patch does not fit grad_weight");
+    const at::ScalarType g = weight_type(weight, bias, pos, "a gradient");
+    a.grad_type = elem_of(g);
     a.accumulate = (int32_t)integer(o[6]);
     strides_of(grad_out, a.shape, "grad_out", &a.image_stride, &a.row_stride);
-    vector(bias, a.shape.dim, weight.scalar_type(), "grad_bias");
-    vector(pos, tokens_of(a.shape) * a.shape.dim, weight.scalar_type(), "grad_pos");
+    vector(bias, a.shape.dim, g, "grad_bias");
+    vector(pos, tokens_of(a.shape) * a.shape.dim, g, "grad_pos");
     const at::Tensor &room = *all.take(o[7], "workspace");
     workspace(room, lib.patch_bytes(&a.shape));
     all.check_device();
     a.grad_out = ptr(&grad_out);
     a.images = ptr(&images);
-    a.grad_weight = all.write(&weight);
+    a.grad_weight = all.write(weight);
     a.grad_bias = all.write(bias);
     a.grad_pos = all.write(pos);
     a.workspace = all.write(&room);
@@ -401,16 +437,6 @@ PyObject *embed_backward(PyObject *const *o)
     return launch(o[7], all, [&](void *s) { return lib.embed_backward(&a, s); });
 }
 
-// The type of the weights among those given (float32 where none is).
-at::ScalarType weight_type(const at::Tensor *a, const at::Tensor *b, const at::Tensor *c)
-{
-    const at::Tensor *t = a ? a : b ? b : c;
-    if (!t)
-        return at::kFloat;
-    elem(*t, "weight");
-    return t->scalar_type();
-}
-
 // x, weight, bias, eps, residual, out, sum_out, mean, rstd, stream
 PyObject *layer_norm(PyObject *const *o)
 {
@@ -441,8 +467,7 @@ PyObject *layer_norm(PyObject *const *o)
     vector(bias, dim, w, "bias");
     vector(mean, a.rows, at::kFloat, "mean");
     vector(rstd, a.rows, at::kFloat, "rstd");
-    a.weight_type = w == at::kFloat ? SMOL_ELEM_F32 : w == at::kHalf ? SMOL_ELEM_F16
-                                                                     : SMOL_ELEM_BF16;
+    a.weight_type = elem_of(w);
     a.eps = (float)number(o[3]);
     all.check_device();
     a.out = all.write(&out);  // first: x and residual may be these
@@ -488,8 +513,7 @@ PyObject *layer_norm_backward(PyObject *const *o)
     vector(grad_bias, dim, w, "grad_bias");
     vector(mean, a.rows, at::kFloat, "mean");
     vector(rstd, a.rows, at::kFloat, "rstd");
-    a.weight_type = w == at::kFloat ? SMOL_ELEM_F32 : w == at::kHalf ? SMOL_ELEM_F16
-                                                                     : SMOL_ELEM_BF16;
+    a.weight_type = elem_of(w);
     a.accumulate = (int32_t)integer(o[9]);
     const at::Tensor &room = *all.take(o[10], "workspace");
     workspace(room, lib.norm_bytes(a.rows, a.dim));
@@ -524,7 +548,7 @@ PyObject *bind(PyObject *const *o)
     {#name, (PyCFunction)(void (*)(void))entry<count, name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SMOL_METHOD(bind, 9),
                          SMOL_METHOD(patch_embed, 7),
-                         SMOL_METHOD(patch_embed_backward, 9),
+                         SMOL_METHOD(patch_embed_backward, 10),
                          SMOL_METHOD(embed, 6),
                          SMOL_METHOD(embed_backward, 8),
                          SMOL_METHOD(layer_norm, 10),

@@ -105,36 +105,50 @@ def patch_embed(images, weight, bias=None, pos=None, layout: int = LAYOUT_NCHW, 
     return out
 
 
-def patch_embed_workspace_bytes(images, grad_weight, dtype, layout: int = LAYOUT_NCHW) -> int:
-    """Bytes of workspace of ``patch_embed_backward`` for gradients of type
-    ``dtype`` coming in (0 for shapes that do not fit)."""
-    _load()
+def _patch_bytes(images, patch: int, dim: int, dtype, layout: int) -> int:
     types = {_torch.float32: ELEM_F32, _torch.float16: ELEM_F16, _torch.bfloat16: ELEM_BF16}
     if dtype not in types or images.dtype not in types:
         raise ValueError("element types are float32, float16 and bfloat16")
-    if images.dim() != 4 or grad_weight.dim() != 4:
-        raise ValueError("images and grad_weight must be tensors of four dimensions")
+    if images.dim() != 4:
+        raise ValueError("images must be a tensor of four dimensions")
     n, a, b, c = images.shape
     ch, h, w = (a, b, c) if layout == LAYOUT_NCHW else (c, a, b)
-    shape = PatchShape(n, ch, h, w, grad_weight.shape[2], grad_weight.shape[0], layout,
-                       types[images.dtype], types[dtype])
+    shape = PatchShape(n, ch, h, w, patch, dim, layout, types[images.dtype], types[dtype])
     return int(smol.lib().smol_patch_workspace_bytes(ctypes.byref(shape)))
+
+
+def patch_embed_workspace_bytes(images, grad_weight, dtype, layout: int = LAYOUT_NCHW) -> int:
+    """Bytes of workspace of ``patch_embed_backward`` for gradients of type
+    ``dtype`` coming in (0 for shapes that do not fit). ``grad_weight`` stands
+    for its shape; the weight itself does as well."""
+    _load()
+    if grad_weight.dim() != 4:
+        raise ValueError("grad_weight must be a tensor of four dimensions")
+    return _patch_bytes(images, grad_weight.shape[2], grad_weight.shape[0], dtype, layout)
 
 
 def patch_embed_backward(grad_out, images, grad_weight, grad_bias=None, grad_pos=None,
                          layout: int = LAYOUT_NCHW, accumulate: bool = False, workspace=None,
-                         stream=None):
+                         stream=None, patch: int | None = None):
     """The projection's gradients from ``grad_out`` (n, tokens, dim): written
     to, or with ``accumulate`` added to, ``grad_weight``, ``grad_bias`` and
-    ``grad_pos``, all float32 or all of grad_out's type
-    (``smol_patch_embed_backward``). Returns the three."""
+    ``grad_pos``, all float32 or all of grad_out's type; None ones are not
+    computed (``smol_patch_embed_backward``). Without ``grad_weight`` (a frozen
+    projection) ``patch`` is the patch's side, and of ``images`` only the shape
+    and type count. Returns the three."""
     native = _native or _load()
     if workspace is None:
-        workspace = _room(patch_embed_workspace_bytes(images, grad_weight, grad_out.dtype, layout),
-                          images.device)
+        if grad_weight is not None:
+            need = patch_embed_workspace_bytes(images, grad_weight, grad_out.dtype, layout)
+        elif patch is None or grad_out.dim() != 3:
+            raise ValueError("without grad_weight the patch's side must be given, and grad_out "
+                             "must have three dimensions")
+        else:
+            need = _patch_bytes(images, patch, grad_out.shape[2], grad_out.dtype, layout)
+        workspace = _room(need, images.device)
     _done(native.patch_embed_backward(
         grad_out, images, grad_weight, grad_bias, grad_pos, layout, bool(accumulate), workspace,
-        _stream(stream, grad_out, images, grad_weight, grad_bias, grad_pos, workspace)))
+        _stream(stream, grad_out, images, grad_weight, grad_bias, grad_pos, workspace), patch))
     return grad_weight, grad_bias, grad_pos
 
 

@@ -468,6 +468,50 @@ def test_patch_gradient_large(case, image, dtype):
         ref.close(a, e.cpu(), b.cpu(), f"patch grad {name}")
 
 
+@pytest.mark.parametrize("case", [
+    (2, 3, 70, 84, 14, 130, False), (5, 4, 40, 33, 8, 7, False), (64, 3, 32, 32, 16, 4, False),
+    (2, 3, 50, 50, 7, 65, True), (3, 3, 65, 97, 16, 40, True), (17, 3, 112, 112, 14, 384, False),
+    (201, 3, 224, 224, 16, 780, False), (2, 3, 7, 7, 8, 16, False)])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_patch_gradient_without_the_weight(case, dtype):
+    """A frozen projection: bias and positions, or one of them, alone; from
+    gaps, overwritten and added to. Both ways of the sums (beside products of
+    128-wide tiles and after those of 256) give these bits too."""
+    note(f"patch grad sums {case} {dtype}")
+    n, c, h, w, p, dim, nhwc = case
+    g, img, weight, t = patch_inputs(case, F16 if dtype != F32 else F32, dtype, dim + 2)
+    layout = tokens.LAYOUT_NHWC if nhwc else tokens.LAYOUT_NCHW
+    kind = F32 if dim % 4 else dtype
+    dy = randn(g, n, t, dim, dtype=dtype)
+    seq = torch.full((n, t + 2, dim + 1), SENTINEL, dtype=dtype, device="cuda")
+    seq[:, 1:1 + t, 1:] = dev(dy)
+    old = randn(g, dim, dtype=kind), randn(g, t, dim, dtype=kind)
+    sums = dy.double().sum((0, 1)), dy.double().sum(0)
+    sizes = dy.double().abs().sum((0, 1)), dy.double().abs().sum(0)
+    bounds = [(m + 4) * ref.U32 * s for m, s in zip((n * t, n), sizes)]
+    img = dev(img)
+    for add in (False, True):
+        for which in ((True, True), (True, False), (False, True)):
+            got = [dev(o) if k else None for o, k in zip(old, which)]
+            back = tokens.patch_embed_backward(seq[:, 1:1 + t, 1:], img, None, *got,
+                                               layout=layout, accumulate=add, patch=p)
+            assert back[0] is None and back[1] is got[0] and back[2] is got[1]
+            for a, e, b, o, name in zip(got, sums, bounds, old, ("bias", "pos")):
+                if a is None:
+                    continue
+                if add:
+                    e, b = e + o.double(), b + 2 * ref.U32 * (e.abs() + o.double().abs())
+                ref.close(a, e, b, f"patch grad {name} alone add={add}")
+        if add:
+            continue
+        both = [torch.empty_like(dev(o)) for o in old]
+        gw = torch.empty(weight.shape, dtype=kind, device="cuda")
+        tokens.patch_embed_backward(dev(dy), img, gw, *both, layout=layout, patch=p)
+        alone = [torch.empty_like(o) for o in both]
+        tokens.patch_embed_backward(dev(dy), img, None, *alone, layout=layout, patch=p)
+        assert all(torch.equal(a, b) for a, b in zip(both, alone))
+
+
 def test_patch_no_images():
     img = torch.empty((0, 3, 32, 32), dtype=F16, device="cuda")
     weight = torch.randn((24, 3, 16, 16), device="cuda").half()

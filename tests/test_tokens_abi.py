@@ -322,3 +322,26 @@ def test_patch_gradients_past_a_launch():
                  row_stride=0)
     assert call("smol_patch_embed_backward", **large) == UNSUPPORTED
     assert b"too many for a launch" in smol.lib().smol_last_error()
+
+
+def test_binding_patch_gradient_without_the_weight():
+    """What then has to be given, and what has to fit."""
+    dy, img = torch.zeros((2, 4, 8)), torch.zeros((2, 3, 32, 32))
+    bias, weight = torch.zeros(8), torch.zeros((8, 3, 16, 16))
+    room = torch.zeros(1 << 20, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="side must be given"):
+        tokens.patch_embed_backward(dy, img, None, bias)
+    with pytest.raises(ValueError, match="side must be given"):
+        tokens.patch_embed_backward(dy, img, None, bias, workspace=room)
+    for bad in (dict(patch=0), dict(patch=8), dict(patch=16, grad_weight=weight[:, :2]),
+                dict(patch=8, grad_weight=weight), dict(patch=16, grad_bias=bias[:7]),
+                dict(patch=16, grad_bias=bias.double()), dict(patch=16, grad_out=dy[0]),
+                dict(patch=16, grad_bias=bias, grad_pos=torch.zeros((4, 8)).half())):
+        for workspace in (None, room):
+            args = dict(dict(grad_out=dy, images=img, grad_weight=None, grad_bias=bias,
+                             workspace=workspace), **bad)
+            with pytest.raises(ValueError) as e:
+                tokens.patch_embed_backward(**args)
+            assert "current device" not in str(e.value), bad
+    with pytest.raises(ValueError, match="current device"):
+        tokens.patch_embed_backward(dy, img, None, bias, workspace=room, patch=16)
