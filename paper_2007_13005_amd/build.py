@@ -137,11 +137,23 @@ def build_pycall(verbose: bool = False) -> str:
     return PYCALL
 
 
-def pytokens_command() -> list:
+def rocm_torch() -> str | None:
+    """The folder of the installed torch, None without one for ROCm."""
+    try:
+        import torch
+    except ImportError:
+        return None
+    return os.path.dirname(torch.__file__) if torch.version.hip else None
+
+
+def pytokens_command() -> list | None:
     """The compiler call of the token operators' binding (host code only,
-    against the headers and libraries of the installed torch)."""
+    against the headers and libraries of the installed torch); None where there
+    is no torch to bind: the C library needs none."""
+    base = rocm_torch()
+    if base is None:
+        return None
     import torch
-    base = os.path.dirname(torch.__file__)
     libs = os.path.join(base, "lib")
     cc = shutil.which("g++") or hipcc()
     return [cc, "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC", "-D__HIP_PLATFORM_AMD__",
@@ -157,8 +169,13 @@ def pytokens_command() -> list:
 def build(verbose: bool = False) -> str:
     cc = hipcc()
     build_pycall(verbose)
+    pytokens = pytokens_command()
+    if pytokens is None:
+        print("no torch for ROCm: the token operators' Python binding is not built",
+              file=sys.stderr, flush=True)
+        return _build_library(cc, verbose)
     # beside the kernels: torch's headers take a while
-    pytokens = [*pytokens_command(), "-o", PYTOKENS + ".tmp"]
+    pytokens += ["-o", PYTOKENS + ".tmp"]
     if verbose:
         print(" ".join(pytokens), flush=True)
     binding = subprocess.Popen(pytokens, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)
@@ -213,9 +230,10 @@ def _build_library(cc: str, verbose: bool) -> str:
 
 
 def sources_newer_than_lib() -> bool:
-    if not all(os.path.exists(f) for f in (LIB, PYCALL, PYTOKENS)):
+    built = [LIB, PYCALL] + ([PYTOKENS] if rocm_torch() else [])
+    if not all(os.path.exists(f) for f in built):
         return True
-    t = min(os.path.getmtime(f) for f in (LIB, PYCALL, PYTOKENS))
+    t = min(os.path.getmtime(f) for f in built)
     files = [os.path.join(CSRC, f)
              for f in SOURCES + HEADERS + ["smol_pycall.c", "smol_tokens_py.cpp"]] + [
         os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE) if f.endswith(".h")]
