@@ -500,16 +500,21 @@ __global__ void __launch_bounds__(512) embed_join_kernel(GradArgs a)
 // Up to kFewRows rows: everything in one launch, without a sort. A wave a row
 // looks for its id among all rows (in LDS); the first row of an id has their
 // list in order, and its wave adds them, or, where there are more than kAlone,
-// the eight waves of the workgroup a part each, joined in order. Workgroups
-// from fill.first on write zeros in the rows of the table that no id names:
-// `per` rows each, which they mark in LDS. 777 rows: 9.0 us a call, 12.2 with
-// the sort's three launches; past kFewRows an id that every row names would
-// keep eight waves too long.
+// the eight waves of the workgroup a part each, joined in order. The grid has
+// `groups` workgroups of rows for the first 64 * V columns, as many for the
+// next, and so on; those from fill.first on write zeros in the rows of the
+// table that no id names: `per` rows each, which they mark in LDS (once for all
+// columns: with a copy of them for every 64 * V, which left at once, 64 ids of
+// 4096 fp32 columns in a vocabulary of 5003 took 23.3 us, now 15.6; 1024 ids in
+// one of 64000, 239 and 205). 777 rows: 9.0 us a call, 12.2 with the sort's
+// three launches; past kFewRows an id that every row names would keep eight
+// waves too long.
 constexpr int kFewRows = 1024;
 constexpr uint32_t kFewFill = 2048;  // rows of the table a workgroup at most
 
 template <typename I, typename G, typename P, int V>
-__global__ void __launch_bounds__(512) embed_few_kernel(SortArgs o, GradArgs a, uint32_t per)
+__global__ void __launch_bounds__(512) embed_few_kernel(SortArgs o, GradArgs a, uint32_t per,
+                                                        uint32_t groups)
 {
     constexpr uint32_t kWaves = 8, kAlone = 16, kAhead = 8;
     __shared__ uint32_t keys[kFewRows];
@@ -521,8 +526,6 @@ __global__ void __launch_bounds__(512) embed_few_kernel(SortArgs o, GradArgs a, 
     for (uint32_t i = threadIdx.x; i < ((a.n + 63) & ~63u); i += 512)
         keys[i] = i < a.n ? key_of<I>(o, i) : (uint32_t)o.vocab;
     if (blockIdx.x >= o.fill.first) {
-        if (blockIdx.y > 0)
-            return;
         const uint32_t lo = (blockIdx.x - o.fill.first) * per;
         const uint32_t rows = a.vocab - lo < per ? a.vocab - lo : per;
         if (threadIdx.x < kFewFill / 32)
@@ -550,8 +553,9 @@ __global__ void __launch_bounds__(512) embed_few_kernel(SortArgs o, GradArgs a, 
         return;
     }
     __syncthreads();
-    const Span<V> c((int32_t)(blockIdx.y * 64 + lane) * V, a.dim);
-    const uint32_t row = blockIdx.x * kWaves + wave;
+    const uint32_t column = blockIdx.x / groups, first = (blockIdx.x - column * groups) * kWaves;
+    const Span<V> c((int32_t)(column * 64 + lane) * V, a.dim);
+    const uint32_t row = first + wave;
     const uint32_t id = row < a.n ? keys[row] : a.vocab;
     uint32_t count = 0;
     if (id != a.vocab) {
@@ -601,7 +605,7 @@ __global__ void __launch_bounds__(512) embed_few_kernel(SortArgs o, GradArgs a, 
 #pragma unroll
             for (uint32_t k = 1; k < kWaves; ++k)
                 sum += sums[k][lane];
-            write_row<P, V>(a, keys[blockIdx.x * kWaves + w], c, sum);
+            write_row<P, V>(a, keys[first + w], c, sum);
         }
         __syncthreads();
     }
@@ -803,7 +807,7 @@ extern "C" int smol_embed_backward(const smol_embed_grad_args *p, void *stream)
         per = per < 1 ? 1 : per > kFewFill ? kFewFill : per;
         if ((p->vocab + per - 1) / per > 4096)  // of which there are not too many
             per = (p->vocab + 4095) / 4096 < kFewFill ? (p->vocab + 4095) / 4096 : kFewFill;
-        o.fill.first = (uint32_t)((p->n + 7) / 8);
+        const uint32_t groups = (uint32_t)((p->n + 7) / 8);
         const unsigned zeros = p->accumulate ? 0 : (unsigned)((p->vocab + per - 1) / per);
         with_type(p->grad_type, [&](auto t) {
             typedef decltype(t) P;
@@ -811,15 +815,15 @@ extern "C" int smol_embed_backward(const smol_embed_grad_args *p, void *stream)
                 typedef decltype(g) G;
                 const auto launch = [&](auto v) {
                     constexpr int V = v.value;
-                    const unsigned columns = (unsigned)((p->dim + 64 * V - 1) / (64 * V));
-                    const dim3 grid(o.fill.first + zeros, columns);
+                    o.fill.first = groups * (uint32_t)((p->dim + 64 * V - 1) / (64 * V));
+                    const dim3 grid(o.fill.first + zeros);
                     with_ids(p->ids_type, [&](auto i) {
                         hipLaunchKernelGGL((embed_few_kernel<decltype(i), G, P, V>), grid,
-                                           dim3(512), 0, s, o, a, (uint32_t)per);
+                                           dim3(512), 0, s, o, a, (uint32_t)per, groups);
                     });
                 };
                 constexpr int V = 16 / sizeof(G);
-                if (o.fill.first + zeros == 0)
+                if (groups + zeros == 0)
                     return;
                 if (p->dim >= V)
                     launch(std::integral_constant<int, V>{});
