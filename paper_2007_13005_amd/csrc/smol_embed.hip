@@ -497,7 +497,7 @@ __global__ void __launch_bounds__(512) embed_join_kernel(GradArgs a)
     }
 }
 
-// Up to kFewRows rows: everything in one launch, without a sort. A wave a row
+// Few rows: everything in one launch, without a sort. A wave a row
 // looks for its id among all rows (in LDS); the first row of an id has their
 // list in order, and its wave adds them, or, where there are more than kAlone,
 // the eight waves of the workgroup a part each, joined in order. The grid has
@@ -506,10 +506,19 @@ __global__ void __launch_bounds__(512) embed_join_kernel(GradArgs a)
 // table that no id names: `per` rows each, which they mark in LDS (once for all
 // columns: with a copy of them for every 64 * V, which left at once, 64 ids of
 // 4096 fp32 columns in a vocabulary of 5003 took 23.3 us, now 15.6; 1024 ids in
-// one of 64000, 239 and 205). 777 rows: 9.0 us a call, 12.2 with the sort's
-// three launches; past kFewRows an id that every row names would keep eight
-// waves too long.
+// one of 64000, 239 and 205).
+//
+// Every workgroup of rows goes through all ids, so it is taken up to kFewRows
+// rows and kFewLooks ids looked at by all workgroups together. us, a
+// vocabulary of 2000, added to the table (so without zeros), one launch / with
+// the counting sort:
+//   rows x columns, fp32    512 x 4096 14.6 / 14.1    700 x 4096 20.5 / 16.0
+//     1024 x 2048 21.8 / 14.7   256 x 16384 19.2 / 16.7   256 x 65536 93 / 38
+//   bf16   700 x 4096 12.2 / 15.0   1024 x 2048 12.7 / 14.3   128 x 65536 14 / 20
+// One id that all rows name costs it more: 1024 x 1024 bf16 20.3 / 11.9, 512
+// x 1024 10.5 / 9.7; ids cannot be known here.
 constexpr int kFewRows = 1024;
+constexpr int64_t kFewLooks = 1 << 19;
 constexpr uint32_t kFewFill = 2048;  // rows of the table a workgroup at most
 
 template <typename I, typename G, typename P, int V>
@@ -801,7 +810,10 @@ extern "C" int smol_embed_backward(const smol_embed_grad_args *p, void *stream)
     a.dim = p->dim;
     a.accumulate = p->accumulate;
     a.scale = p->scale;
-    if (p->n <= kFewRows) {
+    const int lane_columns = p->n && elem_size(p->out_type) == 2 ? 8 : 4;  // of embed_few_kernel
+    const int64_t looks =
+        (p->n + 7) / 8 * ((p->dim + 64 * lane_columns - 1) / (64 * lane_columns)) * p->n;
+    if (p->n <= kFewRows && looks <= kFewLooks) {
         const int64_t bytes = (int64_t)p->dim * elem_size(p->grad_type);
         int64_t per = 65536 / bytes;  // 64 KiB of zeros a workgroup
         per = per < 1 ? 1 : per > kFewFill ? kFewFill : per;

@@ -8,6 +8,7 @@ import pytest
 import torch
 
 from paper_2007_13005_amd import smol, tokens
+from tests import tokens_util as ref
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +58,26 @@ def test_few_ids_gradient_launches_no_idle_workgroups(n, vocab, dim, accumulate)
     sums = -(-n // 8) * -(-dim // 256)
     zeros = 0 if accumulate else -(-vocab // max(65536 // (4 * dim), 1))
     assert found == [(sums + zeros, 512)]
+
+
+@pytest.mark.parametrize("n, dim, dtype, alone", [
+    (1024, 1024, torch.bfloat16, True), (1024, 2048, torch.bfloat16, True),
+    (512, 4096, torch.float32, True), (8, 65536, torch.float32, True),
+    (1024, 3, torch.float32, True), (1024, 2048, torch.float32, False),
+    (1024, 4096, torch.float32, False), (256, 65536, torch.float32, False),
+    (1025, 8, torch.float32, False)])
+def test_few_ids_gradient_in_one_launch_where_that_is_faster(n, dim, dtype, alone):
+    """Not for many rows of many columns, whose workgroups would each look at
+    all ids: those are counted, summed and joined (256 rows of 65536 fp32
+    columns, 93 us in one launch, 38 in three)."""
+    vocab = 100
+    ids = torch.arange(n, device="cuda") % vocab
+    dy = torch.randn((n, dim), device="cuda").to(dtype)
+    out = torch.zeros((vocab, dim), device="cuda")
+    room = torch.empty(tokens.embed_workspace_bytes(n, vocab, dim), dtype=torch.uint8,
+                       device="cuda")
+    found = launches(lambda: tokens.embed_backward(dy, ids, out, accumulate=True, workspace=room))
+    assert len(found) == (1 if alone else 3)
+    tokens.embed_backward(dy, ids, out, 0.5, workspace=room)
+    want, bound = ref.embed_backward(dy.cpu(), ids.cpu(), vocab, 0.5)
+    ref.close(out, want, bound, "embed grad")
