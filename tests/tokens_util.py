@@ -138,3 +138,18 @@ def layer_norm_backward(grad_out, h, weight, mean, rstd, grad_sum):
     want = (dx, (dy * xh).sum(0), dy.sum(0))
     return want, (bound, (rows + 8) * U32 * (dy.abs() * size).sum(0),
                   (rows + 4) * U32 * dy.abs().sum(0))
+
+
+def whole(g, *shape, dtype, most: int = 2):
+    """Whole numbers -most .. most. Their products, and sums of up to 2^24 /
+    most^2 of them in any order, are exact in fp32, so that a sum with a term too
+    few or too many cannot pass for rounding."""
+    return torch.randint(-most, most + 1, shape, generator=g).to(dtype)
+
+
+def same(got, want, what: str) -> None:
+    """Exactly the 64-bit values, rounded once to got's type."""
+    want = want.to(got.dtype)
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    assert torch.equal(got, want.to(got.device)), (
+        f"{what}: {int((got != want.to(got.device)).sum())} of {want.numel()} values differ")
