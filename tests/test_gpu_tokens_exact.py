@@ -64,3 +64,51 @@ def test_patch_gradient_of_whole_numbers(case, threads, image, dtype):
                                 workspace=room)
     for x, e, o, name in zip(got, want, old, names):
         ref.same(x, e + o.double(), f"{name} added")
+
+
+TYPES = [F32, F16, BF16]
+
+
+def zipf(g, n, vocab, holes):
+    """Frequent low ids: the most frequent of 300 is named by 12 % of the rows."""
+    u = torch.rand(n, generator=g, dtype=torch.float64)
+    ids = (torch.exp(u * torch.log(torch.tensor(vocab + 1.0))) - 1).long().clamp_(0, vocab - 1)
+    ids[torch.rand(n, generator=g) < holes] = -1
+    return ids
+
+
+@pytest.mark.parametrize("n, kernels", [(900, 1), (4000, 3), (7000, 3), (20000, 4)])
+@pytest.mark.parametrize("dim", [5, 72, 1030])
+@pytest.mark.parametrize("grad", TYPES)
+@pytest.mark.parametrize("act", TYPES)
+def test_table_gradient_of_whole_numbers(n, kernels, dim, grad, act):
+    """Every pair of types on every way of summing (one launch; ids counted;
+    ids sorted by one digit), with ids that reach over many pieces of the rows:
+    the exact sum rounded once, overwritten and added."""
+    note(f"embed grad whole n={n} dim={dim} {act} {grad}")
+    vocab = 300
+    g = torch.Generator().manual_seed(n + dim)
+    ids = zipf(g, n, vocab, 0.1)
+    piece = 1 if kernels == 1 else 8 if n <= 4096 else 32  # rows; more than 16 pieces
+    assert int((ids == 0).sum()) > 17 * piece
+    dy = ref.whole(g, n, dim, dtype=act)
+    some = ids >= 0
+    want = torch.zeros((vocab, dim), dtype=torch.float64).index_add_(0, ids[some],
+                                                                     dy[some].double())
+    dev_ids, dev_dy = ids.cuda(), dy.cuda()
+    out = torch.full((vocab, dim), SENTINEL, dtype=grad, device="cuda")
+    room = torch.empty(tokens.embed_workspace_bytes(n, vocab, dim), dtype=torch.uint8,
+                       device="cuda")
+    assert len(launches(lambda: tokens.embed_backward(dev_dy, dev_ids, out, 0.5,
+                                                      workspace=room))) == kernels
+    out.fill_(SENTINEL)
+    tokens.embed_backward(dev_dy, dev_ids, out, 0.5, workspace=room)
+    ref.same(out, want * 0.5, "table")
+    old = ref.whole(g, vocab, dim, dtype=grad, most=64)
+    wide = torch.full((vocab, dim + 3), SENTINEL, dtype=grad, device="cuda")
+    wide[:, 1:1 + dim] = old.cuda()
+    tokens.embed_backward(dev_dy, dev_ids, wide[:, 1:1 + dim], 2.0, padding=1, accumulate=True,
+                          workspace=room)
+    want[1] = 0
+    ref.same(wide[:, 1:1 + dim], want * 2 + old.double(), "added")
+    assert bool((wide[:, 0] == SENTINEL).all()) and bool((wide[:, 1 + dim:] == SENTINEL).all())
