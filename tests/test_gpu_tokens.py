@@ -721,3 +721,48 @@ def test_offsets_past_32_bits():
     want, bound = ref.patch_embed(last, weight, None, None, False)
     ref.close(got[-2:], want, bound, "last images")
     assert bool((got[:-2] == 0).all())
+
+
+@pytest.mark.parametrize("dim", [40, 1001, 1026, 1537, 2049, 2305, 4098, 4609, 8191])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_norm_every_place_in_place(dim, dtype):
+    """Every output that may be an input, with strides: the bits of the call
+    with outputs of their own. From 1025 columns on several waves hold a row, and
+    a last chunk that is moved back to end with it can be written by two."""
+    note(f"norm in place dim={dim} {dtype}")
+    g = gen(dim)
+    rows = 23
+    x, res, dy, ds = (randn(g, rows, dim, dtype=dtype) for _ in range(4))
+    w, b = randn(g, dim), randn(g, dim)
+
+    def new(t):
+        return dev(t, dim + 3, 1)
+
+    y, h, mean, rstd = tokens.layer_norm(dev(x), dev(w), dev(b), residual=dev(res))
+    for outputs in (("x", None), ("residual", None), (None, "x"), (None, "residual"),
+                    ("x", "residual"), ("residual", "x")):
+        at = {"x": new(x), "residual": new(res)}
+        out, tot = (at.get(k) if k else new(torch.zeros_like(x)) for k in outputs)
+        got = tokens.layer_norm(at["x"], dev(w), dev(b), residual=at["residual"], out=out,
+                                sum_out=tot)
+        assert got[0] is out and got[1] is tot, outputs
+        for a, e in zip(got, (y, h, mean, rstd)):
+            assert torch.equal(a, e), outputs
+        untouched(out)
+        untouched(tot)
+    # the sum of no residual is x itself
+    at = new(x)
+    plain = tokens.layer_norm(dev(x), dev(w), dev(b))
+    got = tokens.layer_norm(at, dev(w), dev(b), sum_out=at)
+    assert torch.equal(got[0], plain[0]) and torch.equal(at, dev(x))
+    want = [torch.empty(dim, device="cuda") for _ in range(2)]
+    dx = tokens.layer_norm_backward(dev(dy), h, dev(w), mean, rstd, None, *want,
+                                    grad_sum=dev(ds))[0]
+    for k in ("grad_out", "h", "grad_sum"):
+        at = {"grad_out": new(dy), "h": new(h), "grad_sum": new(ds)}
+        sums = [torch.empty(dim, device="cuda") for _ in range(2)]
+        got = tokens.layer_norm_backward(at["grad_out"], at["h"], dev(w), mean, rstd, at[k],
+                                         *sums, grad_sum=at["grad_sum"])[0]
+        assert got is at[k] and torch.equal(got, dx), k
+        assert torch.equal(sums[0], want[0]) and torch.equal(sums[1], want[1]), k
+        untouched(got)
