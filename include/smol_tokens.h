@@ -170,9 +170,10 @@ int smol_embed(const smol_embed_args *a, void *stream);
  *
  *   grad_table[v][c] (+)= scale * sum_{i: ids[i] = v} grad_out[i][c]
  *
- * by sorting the ids (stably, so each sum runs in the order of the rows in
- * pieces of a fixed size). With accumulate = 0 rows that no id names are
- * zeros; with 1 they are not touched.
+ * Each sum runs over its rows in their order, in pieces that are then joined
+ * in order; where the pieces begin depends on the sizes and the ids alone. (Few
+ * rows are found by their ids directly, more by sorting the ids, stably.) With
+ * accumulate = 0 rows that no id names are zeros; with 1 they are not touched.
  *   padding      an id whose row gets no gradient (-1: none; with accumulate
  *                = 0 its row is zeros)
  *   grad_type    any element type

@@ -55,7 +55,9 @@ struct EmbedArgs {
 // One wave takes kSpans * 64 * V columns of a row, four rows a workgroup; it
 // moves bytes and multiplies once a value. 33001 ids (a quarter of them of no
 // token) of 1024 fp32 columns to bf16: 23 us, 4.4 TB/s; one id of 4096 fp16
-// columns 2.2 us.
+// columns 2.2 us. Narrow rows leave lanes and the second span idle: 65536 ids of
+// bf16 rows, columns 512: 21.5 us, 4.7 TB/s, 256: 15.9, 3.1, 128: 14.0, 1.8, 64:
+// 12.2, 1.0.
 constexpr int kSpans = 2;
 
 template <typename T, typename O, typename I, int V>
@@ -163,10 +165,12 @@ __device__ __forceinline__ uint32_t key_of(const SortArgs &a, uint32_t i)
     return id >= 0 && id < a.vocab && id != a.padding ? (uint32_t)id : (uint32_t)a.vocab;
 }
 
-// Every row's place is the number of (key, row) words below its own (n^2
-// comparisons, one launch: 777 rows 4.2 us with the zeros of a 6.4 MB table; the
-// four launches of a two-pass sort take about 20). 16 rows
-// a workgroup, 16 threads a row, each counting every 16th word.
+// Every row's place is the number of (key, row) words below its own: n^2
+// comparisons, in one launch. 16 rows a workgroup, 16 threads a row, each
+// counting every 16th word. us a call, counting / with the four launches of a
+// sort by two digits: 321 fp32 columns, a vocabulary of 5003, rows 1025: 12.2 /
+// 21.8, 4096: 17.5 / 23.8, 8192: 35.5 / 34.4; 1024 bf16 columns, 32000, rows
+// 1025: 33.1 / 33.2, 4096: 35.5 / 38.2, 8192: 51.3 / 51.5.
 template <typename I>
 __global__ void __launch_bounds__(256) embed_rank_kernel(SortArgs a)
 {
@@ -509,14 +513,17 @@ __global__ void __launch_bounds__(512) embed_join_kernel(GradArgs a)
 // one of 64000, 239 and 205).
 //
 // Every workgroup of rows goes through all ids, so it is taken up to kFewRows
-// rows and kFewLooks ids looked at by all workgroups together. us, a
-// vocabulary of 2000, added to the table (so without zeros), one launch / with
-// the counting sort:
-//   rows x columns, fp32    512 x 4096 14.6 / 14.1    700 x 4096 20.5 / 16.0
-//     1024 x 2048 21.8 / 14.7   256 x 16384 19.2 / 16.7   256 x 65536 93 / 38
-//   bf16   700 x 4096 12.2 / 15.0   1024 x 2048 12.7 / 14.3   128 x 65536 14 / 20
-// One id that all rows name costs it more: 1024 x 1024 bf16 20.3 / 11.9, 512
-// x 1024 10.5 / 9.7; ids cannot be known here.
+// rows and kFewLooks ids looked at by all workgroups together. us a call added
+// to the table (so without zeros), one launch / with the counting sort, *: taken;
+// rows x columns:
+//   fp32  777 x 321 9.0* / 13.7   256 x 8192 11.9* / 13.9   256 x 16384 19.2* / 16.7
+//         512 x 4096 14.6* / 14.1   700 x 4096 20.5 / 16.0   1024 x 2048 21.8 / 14.7
+//         256 x 65536 93 / 38
+//   bf16  1024 x 1024 8.8* / 13.6   1024 x 2048 12.7* / 14.3   700 x 4096 12.2* / 15.0
+//         128 x 65536 14.0* / 20.1   1024 x 4096 17.3 / 16.8
+// One id that all rows name, which
+// cannot be known here, is the worst: 1024 x 1024 bf16 20.3 / 11.9, 512 x 1024
+// 10.5 / 9.7.
 constexpr int kFewRows = 1024;
 constexpr int64_t kFewLooks = 1 << 19;
 constexpr uint32_t kFewFill = 2048;  // rows of the table a workgroup at most
@@ -671,8 +678,12 @@ struct Workspace {
 };
 
 // Rows of a piece: few where there are few rows, so that they are summed side
-// by side (777 rows took 5 us in pieces of 8, 13 in pieces of 32); more where
-// the pieces fill the chip, so that fewer sums are written and read again.
+// by side; more where the pieces fill the chip, so that fewer sums are written
+// and read again and less room is asked for. us a call in pieces of 8 / 32: 321
+// fp32 columns, a vocabulary of 5003, rows 2048: 13.7 / 20.9, 4096: 17.5 / 24.7,
+// 8192: 31.0 / 35.5; 1024 bf16 columns, 32000, rows 4096: 35.5 / 43.1, 8192:
+// 45.8 / 51.3, 16384: 48.7 / 48.2, 65536: 90.2 / 86.4 (between 4096 and 16384
+// pieces of 8 would still be the faster, with four times the room).
 int piece_rows(int64_t n) { return n <= 4096 ? 8 : 32; }
 
 Workspace layout(int64_t n, int32_t dim)

@@ -157,8 +157,7 @@ void set_tiles(PatchArgs *a, uint32_t rows, uint32_t cols)
 uint32_t ceil_div(uint32_t n, uint32_t d) { return (n + d - 1) / d; }
 
 // The tile side of a forward call: the least of the times that the sides take
-// for patches of 768 values (the sides' times grow alike with the values).
-// Measured, us, for 224 x 224 images to 768 columns, sides 32 / 64 / 128 / 256:
+// for patches of 768 values. Measured, us, for 224 x 224 images to 768 columns, sides 32 / 64 / 128 / 256:
 //   fp16, images   1: 4.7 / 8.0 / 12.3 / 23.9     8: 12.5 / 10.1 / 13.0 / 25.6
 //                 16: 22.2 / 13.0 / 13.8 / 26.6  32: 38.0 / 19.2 / 18.9 / 27.1
 //                 64: 68.2 / 32.5 / 29.9 / 28.4  96: 101 / 45.3 / 35.7 / 30.5
@@ -166,7 +165,16 @@ uint32_t ceil_div(uint32_t n, uint32_t d) { return (n + d - 1) / d; }
 //   fp32, images   1: 10.4 / 21.5 / 57.4   4: 19.8 / 23.3 / 57.8
 //                 16: 53.4 / 48.8 / 60.1  64: 175 / 138 / 155 (128: not used)
 // (32, 64: several tiles a compute unit at once; 128: two, one for the first
-// 256; 256: one). Rows of a tile from 64 on must lie within 2^32 bytes.
+// 256; 256: one). For patches of 14 to 1024 columns the side taken (*) was the
+// fastest, for fewer values, where a tile's begin and end weigh more, sometimes
+// the second:
+//   p 14, 1024 columns,  1 image 4.7* / 10.3 / 15.4 / 27.2
+//                       16: 28.4 / 20.2 / 17.2* / 28.7  64: 94.9 / 62.2 / 40.1 / 32.4*
+//   p  9, 512 columns,   1: 10.6* / 7.8 / 12.8 / 24.6   64: 293 / 80.9 / 52.6* / 46.6
+//   p  8, 384 columns,   1: 6.1* / 4.4 / 6.8 / 13.4     16: 37.4 / 9.9 / 10.0* / 14.9
+//   p  4, 768 columns,   1: 56.7 / 10.3 / 11.2*          4: 194 / 28.8* / 24.5
+//   fp32, p 8, 384 columns, 4: 15.1* / 11.4             16: 44.6 / 23.8*
+// Rows of a tile from 64 on must lie within 2^32 bytes.
 int forward_tile(const smol_patch_shape &s, const Plan &plan)
 {
     const PatchArgs &a = plan.a;
@@ -215,8 +223,11 @@ GradPlan grad_plan(const smol_patch_shape &s, Plan *plan)
     const bool large = plan->mode != kShort && elem_size(s.image_type) == 2 && C == 8;
     // Large tiles where each compute unit has 20 of their steps or more: us of
     // fp16 images of 224 x 224 in patches of 16 to 768 bf16 columns, sides 128 /
-    // 256: 1 image 15 / 26, 16: 26 / 36, 64: 40 / 49, 128: 72 / 72, 160: 83 / 80,
-    // 256: 117 / 106; to 256 columns, 512 images: 90 / 96.
+    // 256: 1 image 15 / 26, 16: 25 / 35, 64: 41 / 48, 128: 60 / 66, 192: 81 / 82,
+    // 256: 102 / 99; to 256 columns, 512 images: 90 / 96; patches of 14 to 1024
+    // columns, 64: 53 / 57, 96: 69 / 72, 128: 89 / 86, 192: 125 / 114; of 8 to 384
+    // columns, 128: 62 / 73. (256 units: the workspace's size, which a host
+    // without the device may ask for, depends on this choice.)
     const uint64_t large_steps =
         (uint64_t)ceil_div(a.dim, 256) * ceil_div(width, 256) * ceil_div(a.rows, 64);
     g.tile = large && large_steps >= 20 * 256 ? 256 : 128;

@@ -108,12 +108,23 @@ __device__ __forceinline__ int paired_row(int h, int r) { return 8 * (r >> 2) + 
 // at once lie in different banks.
 //
 // 256 fp16 images of 224 x 224 in patches of 14 to 1024 bf16 columns, with
-// positions: 120 us (656 TFLOP/s on the patches' values; the library's product
+// positions: 122 us a call (647 TFLOP/s on the patches' values; the library's product
 // of two ready matrices of these sizes takes 94 us and holds no gather, rounding,
-// bias or positions). Of a tile's 33 us the products take 25 (11 steps at 2.2 us:
-// 1100 TFLOP/s of the 1300 to 1400 that a large library product reaches), the end
-// of the tile 5, which all units write at once (without positions 112 us where
-// with them it took 130).
+// bias or positions). By stamps, before tiles followed each other without a
+// pause: of a tile's 35 us the products took 25 (11 steps at 2.2 us: 1100
+// TFLOP/s of the 1300 to 1400 that a large library product reaches), the end of
+// the tile 6.8, which all units write at once, 2.7 without positions.
+//
+// Chunks round a run up: patches of 14 take 1.20 times their products, of 9
+// 1.78, of 17 1.41; runs shorter than a chunk are loaded value by value. us of
+// 64 fp16 images of 224 x 224 to 512 bf16 columns by the patch's side, forward /
+// the weight's gradient: 4: 157 / 87, 5: 113 / 71, 7: 89 / 62, 8: 24 / 39, 9: 50
+// / 45, 12: 25 / 34, 14: 22 / 33, 16: 19 / 30, 17: 46 / 40, 20: 28 / 35.
+//
+// fp32, 64 images, patches of 16 to 768 columns: 134 us where the products need
+// 96: the matrix units are busy for 0.72 of the time (tiles of 64: the chain of
+// loads, LDS and products of one tile is hidden by the other tiles of a unit
+// but for its begin and end).
 template <typename T, typename S, int WD, int WM, int FD, int FM, int Mode>
 __global__ void __launch_bounds__(64 * WD * WM, 2) patch_kernel(PatchArgs a)
 {
@@ -363,9 +374,11 @@ int launch_patch(const PatchArgs &a, int image_type, int mode, int tile, void *s
     with_image<T>(image_type, [&](auto s) {
         typedef decltype(s) S;
         // Large tiles: a workgroup for every compute unit goes through them
-        // (256 images of 14-pixel patches to 1024 columns: 134 us, one tile a
-        // workgroup 138). Of tiles of 128 the chip holds two a unit, and one
-        // tile a workgroup is the faster (170 us, 177).
+        // (256 images of 14-pixel patches to 1024 columns: 123 us, one tile a
+        // workgroup 128; of 16-pixel patches to 768 columns 86 and 90). Tiles of
+        // 128, of which the chip holds two a unit, are one a workgroup (the first
+        // of these calls 171 us, 161 with two workgroups a unit that go through
+        // them; a quarter of the second 30 and 29).
         const uint32_t cus = device_cus() > 0 ? device_cus() : 256;
         const dim3 grid(tile == 256 && a.tiles > cus ? cus : a.tiles);
         hipStream_t st = (hipStream_t)stream;
