@@ -27,8 +27,10 @@
  *     the current device, or NULL), nothing is synchronised and nothing is
  *     allocated: calls that need room take a workspace of the caller.
  *   - Calls return SMOL_OK, SMOL_ERR_INVALID_ARG, SMOL_ERR_UNSUPPORTED (past
- *     a limit below) or SMOL_ERR_HIP; on an error found by validation
- *     nothing is enqueued. smol_last_error() has the detail.
+ *     a limit below, or more workgroups than one launch takes: 2^24 tiles of
+ *     a patch embedding, 2^32 values of its gradients together) or
+ *     SMOL_ERR_HIP; on an error found by validation nothing is enqueued.
+ *     smol_last_error() has the detail.
  */
 #ifndef SMOL_TOKENS_H
 #define SMOL_TOKENS_H
