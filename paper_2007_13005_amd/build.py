@@ -19,8 +19,9 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libsmol.so")
 # the binding's native marshalling, named for this interpreter's ABI
 PYCALL = os.path.join(PKG, "_smolcall" + sysconfig.get_config_var("EXT_SUFFIX"))
-# the token operators' binding, which reads torch's tensors
+# the token and attention operators' bindings, which read torch's tensors
 PYTOKENS = os.path.join(PKG, "_smoltokens" + sysconfig.get_config_var("EXT_SUFFIX"))
+PYATTENTION = os.path.join(PKG, "_smolattention" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 # The row-streaming kernels are split into parts (input, output type, row
 # walk, output layout) so that the compiler runs on the parts in parallel.
@@ -54,9 +55,22 @@ SOURCES = [
     "smol_patch_grad_bf16.hip",
     "smol_embed.hip",
     "smol_norm.hip",
+    "smol_heads.hip",
+    "smol_heads_f32.hip",
+    "smol_heads_f16.hip",
+    "smol_heads_bf16.hip",
+    "smol_attend.hip",
+    "smol_attend_f32.hip",
+    "smol_attend_f16.hip",
+    "smol_attend_bf16.hip",
+    "smol_attend_grad_f32.hip",
+    "smol_attend_grad_f16.hip",
+    "smol_attend_grad_bf16.hip",
 ]
 HEADERS = ["smol_internal.h", "smol_device.h", "smol_rows.h", "smol_rows_rgb.h", "smol_rows_yuv.h",
-           "smol_magic.h", "smol_tokens_device.h", "smol_patch.h", "smol_patch_kernels.h"]
+           "smol_magic.h", "smol_tokens_device.h", "smol_patch.h", "smol_patch_kernels.h",
+           "smol_tokens_py.h", "smol_heads.h", "smol_heads_kernels.h", "smol_attend.h",
+           "smol_attend_device.h", "smol_attend_kernels.h", "smol_attend_grad_kernels.h"]
 
 # -ffp-contract=off: the kernels round every multiply and add on their own, as
 # the definition does; fused multiply-adds are never formed implicitly.
@@ -146,10 +160,10 @@ def rocm_torch() -> str | None:
     return os.path.dirname(torch.__file__) if torch.version.hip else None
 
 
-def pytokens_command() -> list | None:
-    """The compiler call of the token operators' binding (host code only,
-    against the headers and libraries of the installed torch); None where there
-    is no torch to bind: the C library needs none."""
+def pytokens_command(source: str = "smol_tokens_py.cpp") -> list | None:
+    """The compiler call of the token or attention operators' binding (host code
+    only, against the headers and libraries of the installed torch); None where
+    there is no torch to bind: the C library needs none."""
     base = rocm_torch()
     if base is None:
         return None
@@ -162,7 +176,7 @@ def pytokens_command() -> list | None:
             "-isystem", os.path.join(base, "include"),
             "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
             "-isystem", os.path.join(os.path.dirname(os.path.dirname(hipcc())), "include"),
-            os.path.join(CSRC, "smol_tokens_py.cpp"), "-L", libs, "-Wl,--no-as-needed",
+            os.path.join(CSRC, source), "-L", libs, "-Wl,--no-as-needed",
             "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10_hip", "-lc10"]
 
 
@@ -171,21 +185,30 @@ def build(verbose: bool = False) -> str:
     build_pycall(verbose)
     pytokens = pytokens_command()
     if pytokens is None:
-        print("no torch for ROCm: the token operators' Python binding is not built",
+        print("no torch for ROCm: the token and attention operators' Python binding is not built",
               file=sys.stderr, flush=True)
         return _build_library(cc, verbose)
     # beside the kernels: torch's headers take a while
-    pytokens += ["-o", PYTOKENS + ".tmp"]
-    if verbose:
-        print(" ".join(pytokens), flush=True)
-    binding = subprocess.Popen(pytokens, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)
+    bindings = []
+    for to, cmd in ((PYTOKENS, pytokens), (PYATTENTION, pytokens_command("smol_attention_py.cpp"))):
+        cmd += ["-o", to + ".tmp"]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        bindings.append((to, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.PIPE,
+                                              text=True)))
     try:
         return _build_library(cc, verbose)
     finally:
-        _, err = binding.communicate()
-        if binding.returncode != 0:
-            raise RuntimeError(f"building _smoltokens failed ({binding.returncode}):\n{err}")
-        os.replace(PYTOKENS + ".tmp", PYTOKENS)
+        errors = []
+        for to, binding in bindings:
+            _, err = binding.communicate()
+            if binding.returncode != 0:
+                errors.append(f"building {os.path.basename(to)} failed "
+                              f"({binding.returncode}):\n{err}")
+            else:
+                os.replace(to + ".tmp", to)
+        if errors:
+            raise RuntimeError("\n".join(errors))
 
 
 def _build_library(cc: str, verbose: bool) -> str:
@@ -230,12 +253,13 @@ def _build_library(cc: str, verbose: bool) -> str:
 
 
 def sources_newer_than_lib() -> bool:
-    built = [LIB, PYCALL] + ([PYTOKENS] if rocm_torch() else [])
+    built = [LIB, PYCALL] + ([PYTOKENS, PYATTENTION] if rocm_torch() else [])
     if not all(os.path.exists(f) for f in built):
         return True
     t = min(os.path.getmtime(f) for f in built)
     files = [os.path.join(CSRC, f)
-             for f in SOURCES + HEADERS + ["smol_pycall.c", "smol_tokens_py.cpp"]] + [
+             for f in SOURCES + HEADERS + ["smol_pycall.c", "smol_tokens_py.cpp",
+                                   "smol_attention_py.cpp"]] + [
         os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE) if f.endswith(".h")]
     return any(os.path.getmtime(f) > t for f in files)
 

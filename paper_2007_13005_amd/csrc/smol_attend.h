@@ -1,0 +1,59 @@
+// smol_attend.h -- arguments of the attention kernels (smol_attend_kernels.h,
+// smol_attend_grad_kernels.h), and their launchers, one file per type.
+#ifndef SMOL_ATTEND_H
+#define SMOL_ATTEND_H
+
+#include <stdint.h>
+
+#include "smol_tokens_device.h"
+
+namespace smol {
+
+// A matrix of heads: strides in elements.
+struct HeadRows {
+    const void *p;
+    int64_t batch, row, head;
+};
+
+struct AttendArgs {
+    HeadRows q, k, v, out, dout;  // out is written by the forward pass, read by the backward
+    HeadRows dq, dk, dv;          // written
+    const void *rest_in;
+    void *rest;
+    float *lse;    // batch x queries x heads
+    float *delta;  // the same (backward)
+    float *part;   // forward, splits > 1: sums of parts of the keys
+    const int32_t *q_lengths, *k_lengths;
+    int32_t queries, keys, heads, dim;
+    int32_t columns;       // queries * group: pairs of a query and one of a key head's heads
+    int32_t window, sinks; // window 0: none
+    int32_t causal;
+    int32_t tiles;         // of the columns, or of the keys (gradients of keys)
+    int32_t pairs;         // batch * kv_heads
+    int32_t splits;
+    float scale, scale_log2;  // the second times log2 e
+    Divisor group, pair_div, kv_heads, tile_div;
+};
+
+constexpr int kAttendKeys = 64;     // of a tile that four waves share
+constexpr int kAttendColumns = 32;  // of a wave
+constexpr int kAttendWaves = 4;     // of a workgroup
+constexpr int kAttendFewKeys = 32;  // of a tile of one wave (few columns)
+constexpr int kAttendSplits = 64;   // parts of the keys at most
+
+// Kernels: the forward pass with the waves over columns, or over keys (few
+// columns); the join of its splits; the gradients of queries, and of keys and
+// values.
+enum { kAttendMany, kAttendFew, kAttendJoin, kAttendGradQ, kAttendGradK };
+
+// wide: values of a head in 32s, rounded up.
+int launch_attend_f32(const AttendArgs &a, int kernel, int wide, unsigned grid, void *s);
+int launch_attend_f16(const AttendArgs &a, int kernel, int wide, unsigned grid, void *s);
+int launch_attend_bf16(const AttendArgs &a, int kernel, int wide, unsigned grid, void *s);
+int launch_attend_grad_f32(const AttendArgs &a, int kernel, int wide, unsigned grid, void *s);
+int launch_attend_grad_f16(const AttendArgs &a, int kernel, int wide, unsigned grid, void *s);
+int launch_attend_grad_bf16(const AttendArgs &a, int kernel, int wide, unsigned grid, void *s);
+
+}  // namespace smol
+
+#endif  // SMOL_ATTEND_H

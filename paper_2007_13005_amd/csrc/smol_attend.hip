@@ -1,0 +1,304 @@
+// smol_attend.hip -- attention: checks, parts of the keys, launches
+// (smol_attend, smol_attend_backward).
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "smol.h"
+#include "smol_attend.h"
+#include "smol_attention.h"
+#include "smol_internal.h"
+
+namespace smol {
+namespace {
+
+constexpr int64_t kMostColumns = 1 << 30;  // queries times a key head's query heads
+constexpr int64_t kMostGroups = (1 << 24) - 1;  // workgroups of 256 threads of a launch
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int check_shape(const smol_attend_shape &s)
+{
+    if (s.batch < 0 || s.queries < 0 || s.keys < 0 || s.heads < 1 || s.kv_heads < 1 || s.dim < 1)
+        return set_error(SMOL_ERR_INVALID_ARG,
+                         "batch %d, queries %d, keys %d, heads %d, kv_heads %d or dim %d out of "
+                         "range",
+                         s.batch, s.queries, s.keys, s.heads, s.kv_heads, s.dim);
+    if (s.heads % s.kv_heads)
+        return set_error(SMOL_ERR_INVALID_ARG, "%d heads are no multiple of %d kv_heads", s.heads,
+                         s.kv_heads);
+    if (s.type < SMOL_ELEM_F32 || s.type > SMOL_ELEM_BF16)
+        return set_error(SMOL_ERR_INVALID_ARG, "type %d unknown", s.type);
+    if (s.causal != 0 && s.causal != 1)
+        return set_error(SMOL_ERR_INVALID_ARG, "causal %d is neither 0 nor 1", s.causal);
+    if (s.window < 0 || s.sinks < 0 || (!s.causal && (s.window || s.sinks)))
+        return set_error(SMOL_ERR_INVALID_ARG,
+                         "window %d or sinks %d negative, or given without causal", s.window,
+                         s.sinks);
+    if (!(s.scale > 0.0f) || isinf(s.scale))
+        return set_error(SMOL_ERR_INVALID_ARG, "scale is not positive and finite");
+    if (s.reserved)
+        return set_error(SMOL_ERR_INVALID_ARG, "reserved field is not zero");
+    if ((uintptr_t)s.q_lengths % 4 || (uintptr_t)s.k_lengths % 4)
+        return set_error(SMOL_ERR_INVALID_ARG, "lengths are not aligned to their elements");
+    if (s.dim % 8 || s.dim > SMOL_MAX_ATTEND_DIM)
+        return set_error(SMOL_ERR_UNSUPPORTED, "dim %d beyond %d or no multiple of 8", s.dim,
+                         SMOL_MAX_ATTEND_DIM);
+    if (s.batch > SMOL_MAX_ATTEND_BATCH || s.queries > SMOL_MAX_ATTEND_ROWS ||
+        s.keys > SMOL_MAX_ATTEND_ROWS || s.heads > SMOL_MAX_HEADS)
+        return set_error(SMOL_ERR_UNSUPPORTED,
+                         "batch %d beyond %d, queries %d or keys %d beyond %d, or heads %d "
+                         "beyond %d",
+                         s.batch, SMOL_MAX_ATTEND_BATCH, s.queries, s.keys, SMOL_MAX_ATTEND_ROWS,
+                         s.heads, SMOL_MAX_HEADS);
+    const int64_t columns = (int64_t)s.queries * (s.heads / s.kv_heads);
+    const int64_t pairs = (int64_t)s.batch * s.kv_heads;
+    if (columns > kMostColumns || ceil_div(columns, 128) * pairs > kMostGroups ||
+        ceil_div(s.keys, 128) * pairs > kMostGroups)
+        return set_error(SMOL_ERR_UNSUPPORTED, "too many rows and heads for a launch");
+    return SMOL_OK;
+}
+
+// How the forward pass is split.
+struct Split {
+    bool few;
+    int32_t tiles, splits;
+};
+
+Split split_of(const smol_attend_shape &s)
+{
+    Split p;
+    const int64_t columns = (int64_t)s.queries * (s.heads / s.kv_heads);
+    const int64_t pairs = (int64_t)s.batch * s.kv_heads;
+    // a tile of columns that one wave holds: the waves then share the keys
+    p.few = columns <= kAttendColumns;
+    p.tiles = (int32_t)ceil_div(columns, p.few ? kAttendColumns : kAttendColumns * kAttendWaves);
+    // two workgroups a compute unit, each with 256 keys or more
+    int64_t keys = s.keys;
+    if (s.causal && s.window)
+        keys = std::min<int64_t>(keys, (int64_t)s.window + s.sinks + s.queries);
+    const int64_t groups = std::max<int64_t>(1, p.tiles * pairs);
+    int64_t splits = std::min<int64_t>(512 / groups, ceil_div(keys, 256));
+    splits = std::max<int64_t>(1, std::min<int64_t>(splits, kAttendSplits));
+    p.splits = (int32_t)splits;
+    return p;
+}
+
+int wide_of(int32_t dim) { return (dim + 31) / 32; }
+
+int64_t part_bytes(const smol_attend_shape &s, const Split &p)
+{
+    if (p.splits == 1)
+        return 0;
+    const int64_t rows = (int64_t)s.queries * s.heads * s.batch;
+    return p.splits * rows * (wide_of(s.dim) * 32 + 2) * 4;
+}
+
+int64_t delta_bytes(const smol_attend_shape &s)
+{
+    return (int64_t)s.queries * s.heads * s.batch * 4;
+}
+
+// Strides of sequences, rows and heads: those that are read may be 0; what is
+// written does not overlap.
+int check_rows(const char *name, const void *p, int64_t batch, int64_t rows, int64_t heads,
+               const int64_t (&strides)[3], int dim, int type, bool written)
+{
+    if (!p)
+        return set_error(SMOL_ERR_INVALID_ARG, "%s is NULL", name);
+    if ((uintptr_t)p % elem_size(type))
+        return set_error(SMOL_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
+    const int64_t sizes[3] = {batch, rows, heads};
+    int order[3] = {0, 1, 2};
+    for (int k = 0; k < 3; ++k)
+        if (sizes[k] > 1 && (strides[k] < 0 || strides[k] > INT64_MAX / 64 / sizes[k]))
+            return set_error(SMOL_ERR_INVALID_ARG, "%s: stride %lld out of range", name,
+                             (long long)strides[k]);
+    if (!written)
+        return SMOL_OK;
+    std::sort(order, order + 3, [&](int a, int b) { return strides[a] < strides[b]; });
+    int64_t extent = dim;
+    for (int k : order) {
+        if (sizes[k] <= 1)
+            continue;
+        if (strides[k] < extent)
+            return set_error(SMOL_ERR_INVALID_ARG, "%s: heads or rows overlap", name);
+        extent += (sizes[k] - 1) * strides[k];
+    }
+    return SMOL_OK;
+}
+
+template <typename R>
+int take(HeadRows *to, const char *name, const R &m, int64_t batch, int64_t rows, int64_t heads,
+         int dim, int type, bool written)
+{
+    to->p = m.data;
+    to->batch = m.batch_stride;
+    to->row = m.row_stride;
+    to->head = m.head_stride;
+    if (rows == 0 || batch == 0)
+        return SMOL_OK;
+    return check_rows(name, m.data, batch, rows, heads,
+                      {m.batch_stride, m.row_stride, m.head_stride}, dim, type, written);
+}
+
+AttendArgs args_of(const smol_attend_shape &s)
+{
+    AttendArgs a = {};
+    const int32_t group = s.heads / s.kv_heads;
+    a.q_lengths = s.q_lengths;
+    a.k_lengths = s.k_lengths;
+    a.queries = s.queries;
+    a.keys = s.keys;
+    a.heads = s.heads;
+    a.dim = s.dim;
+    a.columns = s.queries * group;
+    // past all keys a window hides none; nor do more sinks than keys show more
+    a.window = s.window < s.keys ? s.window : 0;
+    a.sinks = a.window ? std::min(s.sinks, s.keys) : 0;
+    a.causal = s.causal;
+    a.pairs = s.batch * s.kv_heads;
+    a.scale = s.scale;
+    a.scale_log2 = (float)(s.scale * 1.44269504088896340736);
+    a.group = make_divisor(group);
+    a.pair_div = make_divisor(a.pairs);
+    a.kv_heads = make_divisor(s.kv_heads);
+    a.tile_div = make_divisor(1);
+    a.tiles = a.splits = 1;
+    return a;
+}
+
+int check_workspace(const void *p, int64_t have, int64_t need)
+{
+    if (need && (!p || (uintptr_t)p % 16 || have < need))
+        return set_error(SMOL_ERR_INVALID_ARG,
+                         "workspace must be 16-byte aligned and hold %lld bytes",
+                         (long long)need);
+    return SMOL_OK;
+}
+
+int launch(const AttendArgs &a, int kernel, int type, int dim, int64_t grid, void *s)
+{
+    const bool grad = kernel == kAttendGradQ || kernel == kAttendGradK;
+    const auto f = type == SMOL_ELEM_F32   ? grad ? launch_attend_grad_f32 : launch_attend_f32
+                   : type == SMOL_ELEM_F16 ? grad ? launch_attend_grad_f16 : launch_attend_f16
+                   : grad                  ? launch_attend_grad_bf16
+                                           : launch_attend_bf16;
+    return f(a, kernel, wide_of(dim), (unsigned)grid, s);
+}
+
+}  // namespace
+}  // namespace smol
+
+extern "C" int64_t smol_attend_workspace_bytes(const smol_attend_shape *s)
+{
+    using namespace smol;
+    if (!s || check_shape(*s) != SMOL_OK)
+        return 0;
+    return part_bytes(*s, split_of(*s)) + 16;
+}
+
+extern "C" int64_t smol_attend_backward_workspace_bytes(const smol_attend_shape *s)
+{
+    using namespace smol;
+    if (!s || check_shape(*s) != SMOL_OK)
+        return 0;
+    return delta_bytes(*s) + 16;
+}
+
+extern "C" int smol_attend(const smol_attend_args *p, void *stream)
+{
+    using namespace smol;
+    clear_error();
+    if (!p)
+        return set_error(SMOL_ERR_INVALID_ARG, "args is NULL");
+    const smol_attend_shape &s = p->shape;
+    int st = check_shape(s);
+    if (st != SMOL_OK)
+        return st;
+    if (s.batch == 0 || s.queries == 0)
+        return SMOL_OK;
+    AttendArgs a = args_of(s);
+    if ((st = take(&a.q, "q", p->q, s.batch, s.queries, s.heads, s.dim, s.type, false)) !=
+            SMOL_OK ||
+        (st = take(&a.k, "k", p->k, s.batch, s.keys, s.kv_heads, s.dim, s.type, false)) !=
+            SMOL_OK ||
+        (st = take(&a.v, "v", p->v, s.batch, s.keys, s.kv_heads, s.dim, s.type, false)) !=
+            SMOL_OK ||
+        (st = take(&a.out, "out", p->out, s.batch, s.queries, s.heads, s.dim, s.type, true)) !=
+            SMOL_OK)
+        return st;
+    if ((uintptr_t)p->lse % 4 || (uintptr_t)p->rest % elem_size(s.type))
+        return set_error(SMOL_ERR_INVALID_ARG, "lse or rest is not aligned to its elements");
+    const Split split = split_of(s);
+    if ((st = check_workspace(p->workspace, p->workspace_bytes, part_bytes(s, split))) != SMOL_OK)
+        return st;
+    a.lse = p->lse;
+    a.rest = p->rest;
+    a.part = (float *)p->workspace;
+    a.tiles = split.tiles;
+    a.tile_div = make_divisor(split.tiles);
+    a.splits = split.splits;
+    int e = launch(a, split.few ? kAttendFew : kAttendMany, s.type, s.dim,
+                   (int64_t)split.tiles * a.pairs * split.splits, stream);
+    if (e == hipSuccess && split.splits > 1)
+        e = launch(a, kAttendJoin, s.type, s.dim,
+                   ceil_div((int64_t)a.pairs * a.columns, kAttendWaves), stream);
+    if (e != hipSuccess)
+        return set_error(SMOL_ERR_HIP, "attention launch: %s", hipGetErrorString((hipError_t)e));
+    return SMOL_OK;
+}
+
+extern "C" int smol_attend_backward(const smol_attend_grad_args *p, void *stream)
+{
+    using namespace smol;
+    clear_error();
+    if (!p)
+        return set_error(SMOL_ERR_INVALID_ARG, "args is NULL");
+    const smol_attend_shape &s = p->shape;
+    int st = check_shape(s);
+    if (st != SMOL_OK)
+        return st;
+    if (s.batch == 0 || (s.queries == 0 && s.keys == 0))
+        return SMOL_OK;
+    AttendArgs a = args_of(s);
+    const auto of_queries = [&](HeadRows *to, const char *name, const auto &m, bool written) {
+        return take(to, name, m, s.batch, s.queries, s.heads, s.dim, s.type, written);
+    };
+    const auto of_keys = [&](HeadRows *to, const char *name, const auto &m, bool written) {
+        return take(to, name, m, s.batch, s.keys, s.kv_heads, s.dim, s.type, written);
+    };
+    if ((st = of_queries(&a.dout, "grad_out", p->grad_out, false)) != SMOL_OK ||
+        (st = of_queries(&a.q, "q", p->q, false)) != SMOL_OK ||
+        (st = of_keys(&a.k, "k", p->k, false)) != SMOL_OK ||
+        (st = of_keys(&a.v, "v", p->v, false)) != SMOL_OK ||
+        (st = of_queries(&a.out, "out", p->out, false)) != SMOL_OK ||
+        (st = of_queries(&a.dq, "grad_q", p->grad_q, true)) != SMOL_OK ||
+        (st = of_keys(&a.dk, "grad_k", p->grad_k, true)) != SMOL_OK ||
+        (st = of_keys(&a.dv, "grad_v", p->grad_v, true)) != SMOL_OK)
+        return st;
+    if (s.queries > 0 && (!p->lse || (uintptr_t)p->lse % 4))
+        return set_error(SMOL_ERR_INVALID_ARG, "lse is NULL or not aligned to its elements");
+    if ((uintptr_t)p->rest % elem_size(s.type))
+        return set_error(SMOL_ERR_INVALID_ARG, "rest is not aligned to its elements");
+    if ((st = check_workspace(p->workspace, p->workspace_bytes, delta_bytes(s))) != SMOL_OK)
+        return st;
+    a.lse = (float *)p->lse;
+    a.rest_in = p->rest;
+    a.delta = (float *)p->workspace;
+    int e = hipSuccess;
+    if (s.queries > 0) {
+        a.tiles = (int32_t)ceil_div(a.columns, kAttendColumns * kAttendWaves);
+        e = launch(a, kAttendGradQ, s.type, s.dim, (int64_t)a.tiles * a.pairs, stream);
+    }
+    if (e == hipSuccess && s.keys > 0) {
+        a.tiles = (int32_t)ceil_div(s.keys, kAttendColumns * kAttendWaves);
+        e = launch(a, kAttendGradK, s.type, s.dim, (int64_t)a.tiles * a.pairs, stream);
+    }
+    if (e != hipSuccess)
+        return set_error(SMOL_ERR_HIP, "attention backward launch: %s",
+                         hipGetErrorString((hipError_t)e));
+    return SMOL_OK;
+}

@@ -1,0 +1,305 @@
+// smol_attend_device.h -- what the attention kernels share: operands of the
+// matrix instructions and their tiles in LDS, which keys a query sees, and the
+// walk over the tiles that have any.
+//
+// Columns. The `group` query heads that read one key head are taken together:
+// column c of a sequence and key head is query c / group and the group's head
+// c % group, so single tokens of grouped heads fill a tile's columns, and keys
+// are read once for all of them.
+//
+// Operands. All products are 32 x 32 x 16 (fp32: eight of 32 x 32 x 2). A lane
+// holds eight values of the summed index for one row of an operand (lane %
+// 32); which values is free as long as both operands agree. Lane l of a result
+// has column l % 32 and, in register 4 g + r, row 8 g + 4 (l / 32) + r. So with
+// scores formed as (keys x columns), a lane's eight registers 8 s .. 8 s + 7 hold
+// keys 16 s + {0 .. 3, 8 .. 11} + 4 (l / 32) of its own column: the second
+// operand of the next product, as they are, if its first operand takes the
+// keys in that order. Row statistics are sums over a lane's registers and one
+// exchange with the other half of the wave.
+#ifndef SMOL_ATTEND_DEVICE_H
+#define SMOL_ATTEND_DEVICE_H
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <type_traits>
+
+#include "smol_attend.h"
+
+namespace smol {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLowest = -3.0e38f;  // below every finite maximum of scores
+constexpr float kLn2 = 0.693147180559945309f;
+constexpr float kLog2e = 1.44269504088896341f;
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <typename T>
+__device__ __forceinline__ void multiply(f32x16 &sum, vec<T, 8> a, vec<T, 8> b)
+{
+    if constexpr (std::is_same<T, f16>::value)
+        sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, sum, 0, 0, 0);
+    else if constexpr (std::is_same<T, bf16>::value)
+        sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, sum, 0, 0, 0);
+    else
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            sum = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], sum, 0, 0, 0);
+}
+
+// Eight neighbouring registers of a result as an operand.
+template <typename T>
+__device__ __forceinline__ vec<T, 8> operand(const f32x16 &x, int s)
+{
+    vec<float, 8> v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v[e] = x[8 * s + e];
+    return from_f32<T, 8>(v);
+}
+
+// x of both halves of the wave joined by f.
+template <typename F>
+__device__ __forceinline__ float both_halves(float x, F f)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x),
+                                                    __builtin_bit_cast(uint32_t, x), false, false);
+    return f(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+
+// Rows of N * 32 values in LDS, `Pad` bytes apart. With 16 bytes the rows of a
+// row operand's eight lanes lie in different banks (the stride is an odd number
+// of 16 bytes); with 32 those of four rows by 32 bytes, which a transposing read
+// takes, do.
+template <typename T, int N, int Pad>
+struct LdsRows {
+    static constexpr int kStride = N * 32 * (int)sizeof(T) + Pad;
+    static constexpr int kChunks = N * 32 * (int)sizeof(T) / 16;
+    static constexpr int kEach = 16 / (int)sizeof(T);
+    typedef vec<T, kEach> Chunk;
+
+    static __device__ __forceinline__ void put(char *tile, int row, int chunk, Chunk v)
+    {
+        *(Chunk *)(tile + row * kStride + chunk * 16) = v;
+    }
+    // Row operand: of row lane % 32, values 16 t + 8 (lane / 32) .. + 7.
+    static __device__ __forceinline__ int row_at(int lane)
+    {
+        return (lane & 31) * kStride + (lane >> 5) * 8 * (int)sizeof(T);
+    }
+    static __device__ __forceinline__ vec<T, 8> row(const char *tile, int at, int row0, int t)
+    {
+        const char *p = tile + at + row0 * kStride + t * 16 * (int)sizeof(T);
+        if constexpr (sizeof(T) == 2) {
+            return *(const vec<T, 8> *)p;
+        } else {
+            const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 16);
+            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+    // Column operand: of column 32 n + lane % 32, rows row0 + {0 .. 3, 8 .. 11} +
+    // 4 (lane / 32).
+    static __device__ __forceinline__ int column_at(int lane)
+    {
+        if (sizeof(T) == 4)
+            return (lane >> 5) * 4 * kStride + (lane & 31) * 4;
+        return ((lane >> 5) * 4 + ((lane & 15) >> 2)) * kStride +
+               ((lane >> 4 & 1) * 16 + (lane & 3) * 4) * 2;
+    }
+    static __device__ __forceinline__ vec<T, 8> column(const char *tile, int at, int row0, int n)
+    {
+        const char *p = tile + at + row0 * kStride + n * 32 * (int)sizeof(T);
+        if constexpr (sizeof(T) == 2) {
+            // 16 lanes give the places of four rows by 16 columns and get a column each
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s16x4 Shared;
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)p);
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)(p + 8 * kStride));
+            return __builtin_bit_cast(vec<T, 8>,
+                                      __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            vec<T, 8> v;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[e] = *(const float *)(p + (e < 4 ? e : e + 4) * kStride);
+            return v;
+        }
+    }
+};
+
+// A sequence and one of its key heads.
+struct Sequence {
+    int32_t b, kv, q_length, k_length, shift;  // query i stands at shift + i
+    __device__ __forceinline__ Sequence(const AttendArgs &a, uint32_t pair)
+    {
+        b = (int32_t)divide(pair, a.kv_heads);
+        kv = (int32_t)(pair - b * a.kv_heads.d);
+        q_length = a.q_lengths ? a.q_lengths[b] : a.queries;
+        k_length = a.k_lengths ? a.k_lengths[b] : a.keys;
+        q_length = q_length < 0 ? 0 : q_length < a.queries ? q_length : a.queries;
+        k_length = k_length < 0 ? 0 : k_length < a.keys ? k_length : a.keys;
+        shift = k_length - q_length;
+    }
+    // The last and first key that query i sees, sinks aside; last < 0: none.
+    __device__ __forceinline__ int32_t last(const AttendArgs &a, int32_t i) const
+    {
+        return i >= q_length ? -1 : a.causal ? shift + i : k_length - 1;
+    }
+    __device__ __forceinline__ int32_t first(const AttendArgs &a, int32_t i) const
+    {
+        const int32_t lo = a.window ? shift + i - a.window + 1 : 0;
+        return lo > 0 ? lo : 0;
+    }
+    template <typename T>
+    __device__ __forceinline__ const T *rows(const HeadRows &m, int32_t head) const
+    {
+        return (const T *)m.p + b * m.batch + head * m.head;
+    }
+};
+
+__device__ __forceinline__ bool sees(int32_t j, int32_t last, int32_t first, int32_t sinks)
+{
+    return j <= last && (j >= first || j < sinks);
+}
+
+// Column c's query and head. c past the last: the last.
+struct Column {
+    int32_t i, head;
+    bool exists;
+    __device__ __forceinline__ Column(const AttendArgs &a, const Sequence &s, int32_t c)
+    {
+        exists = c < a.columns;
+        c = exists ? c : a.columns - 1;
+        i = (int32_t)divide((uint32_t)c, a.group);
+        head = s.kv * (int32_t)a.group.d + c - i * (int32_t)a.group.d;
+    }
+};
+
+// The tiles of `Keys` keys that any of queries i0 .. i1 sees: those of the first
+// keys (sinks), then a run.
+template <int Keys>
+struct Walk {
+    int32_t head, from, count;
+    __device__ __forceinline__ Walk(const AttendArgs &a, const Sequence &s, int32_t i0, int32_t i1)
+    {
+        i1 = i1 < s.q_length ? i1 : s.q_length - 1;
+        const int32_t last = i0 <= i1 ? s.last(a, i1) : -1;
+        head = from = count = 0;
+        if (last < 0)
+            return;
+        from = s.first(a, i0) / Keys;
+        const int32_t sinks = (a.sinks + Keys - 1) / Keys;
+        head = sinks < from ? sinks : from;
+        count = head + last / Keys - from + 1;
+    }
+    __device__ __forceinline__ int32_t tile(int32_t n) const
+    {
+        return n < head ? n : n - head + from;
+    }
+};
+
+// Eight values from 16 t + 8 (lane / 32) on of the lane's row, zeros past the head.
+template <typename T, int N>
+__device__ __forceinline__ void row_operands(const T *row, int32_t dim, int lane,
+                                             vec<T, 8> (&v)[2 * N])
+{
+#pragma unroll
+    for (int t = 0; t < 2 * N; ++t) {
+        const int32_t d = 16 * t + 8 * (lane >> 5);
+        v[t] = load<T, 8>(row + (d < dim ? d : 0));
+        if (d >= dim)
+            v[t] = (vec<T, 8>)(T)0.0f;
+    }
+}
+
+// Chunks of a tile's rows that one of `Threads` threads moves to LDS.
+template <typename T, int N, int Rows, int Threads>
+struct Mover {
+    typedef LdsRows<T, N, 16> Layout;
+    static constexpr int kCount = Rows * Layout::kChunks / Threads;
+    static_assert(kCount * Threads == Rows * Layout::kChunks, "whole chunks a thread");
+    typename Layout::Chunk v[kCount];
+    // Rows row0 .. of `rows` (>= 1), zeros past them and past the head.
+    __device__ __forceinline__ void fetch(const T *p, int64_t stride, int32_t row0, int32_t rows,
+                                          int32_t dim, int thread)
+    {
+#pragma unroll
+        for (int n = 0; n < kCount; ++n) {
+            const int id = thread + Threads * n, r = id / Layout::kChunks;
+            const int32_t at = id % Layout::kChunks * Layout::kEach, row = row0 + r;
+            const bool some = row < rows && at < dim;
+            v[n] = load<T, Layout::kEach>(p + (row < rows ? row : rows - 1) * stride +
+                                          (at < dim ? at : 0));
+            if (!some)
+                v[n] = (typename Layout::Chunk)(T)0.0f;
+        }
+    }
+    template <int Pad>
+    __device__ __forceinline__ void put(char *tile, int thread) const
+    {
+#pragma unroll
+        for (int n = 0; n < kCount; ++n) {
+            const int id = thread + Threads * n;
+            LdsRows<T, N, Pad>::put(tile, id / Layout::kChunks, id % Layout::kChunks, v[n]);
+        }
+    }
+};
+
+// Whether any of a result's N tiles has a value that is not finite.
+template <int N>
+__device__ __forceinline__ bool any_not_finite(const f32x16 (&x)[N])
+{
+    bool bad = false;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            bad |= !(fabsf(x[n][e]) < INFINITY);
+    return bad;
+}
+
+// A row of up to 128 values over the wave: values lane and lane + 64.
+struct Spread {
+    float x, y;
+    template <typename T>
+    static __device__ __forceinline__ Spread of(const T *p, int32_t dim, int lane)
+    {
+        return {lane < dim ? (float)p[lane] : 0.0f, lane + 64 < dim ? (float)p[lane + 64] : 0.0f};
+    }
+};
+__device__ __forceinline__ float dot(const Spread &a, const Spread &b)
+{
+    return wave_sum(a.x * b.x + a.y * b.y);
+}
+// Whether all values of a sum are NaN, which no further term changes.
+__device__ __forceinline__ bool settled(const Spread &s, int32_t dim, int lane)
+{
+    return !__any((lane < dim && s.x == s.x) || (lane + 64 < dim && s.y == s.y));
+}
+// The value at `d` of a spread row, any d a lane.
+__device__ __forceinline__ float value_at(const Spread &s, int d)
+{
+    const float x = __shfl(s.x, d & 63), y = __shfl(s.y, d & 63);
+    return d < 64 ? x : y;
+}
+// Sets the registers of the lanes of column `column` to a spread row.
+template <int N>
+__device__ __forceinline__ void set_column(f32x16 (&x)[N], const Spread &s, int column, int lane)
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float v = value_at(s, 32 * n + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3));
+            x[n][e] = (lane & 31) == column ? v : x[n][e];
+        }
+}
+
+}  // namespace
+}  // namespace smol
+
+#endif  // SMOL_ATTEND_DEVICE_H

@@ -1,0 +1,454 @@
+// smol_attend_kernels.h -- attention forward, as templates for one type
+// (instantiated by smol_attend_<type>.hip).
+//
+// One pass over the keys with the running maximum m and sum l of a softmax in
+// base 2: weights 2^(s - m) are rounded to the type and multiplied with the
+// values in fp32; a maximum that grows scales what was summed before. m may
+// stay up to 8 behind the maximum (weights up to 256, exact in any type's
+// exponent), so most tiles scale nothing.
+//
+// What a query does not see takes no part: its score is set to minus infinity
+// before the maximum. A weight of 0 times a NaN or an infinity among the values
+// would still spoil the sums (of a tile that other queries see); so a column
+// whose sums are not finite in the end, though its weights are, is summed
+// again key by key, over what it sees alone.
+#ifndef SMOL_ATTEND_KERNELS_H
+#define SMOL_ATTEND_KERNELS_H
+
+#include "smol_attend_device.h"
+
+namespace smol {
+namespace {
+
+constexpr float kBehind = 8.0f;
+
+// One wave's 32 columns: scores, weights and sums.
+template <typename T, int N>
+struct Columns {
+    vec<T, 8> q[2 * N];
+    f32x16 sum[N];   // [values x columns]
+    float m, l;      // l: of this half of the wave
+    int32_t last, first;
+    int32_t last_min, last_max, first_min, first_max;  // over the wave's columns
+
+    __device__ __forceinline__ void start(const AttendArgs &a, const Sequence &s, int32_t c0,
+                                          int lane)
+    {
+        const Column c(a, s, c0 + (lane & 31));
+        row_operands<T, N>(s.rows<T>(a.q, c.head) + c.i * a.q.row, a.dim, lane, q);
+        last = c.exists ? s.last(a, c.i) : -1;
+        first = s.first(a, c.i);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            sum[n] = (f32x16)0.0f;
+        m = kLowest;
+        l = 0.0f;
+        const Column lo(a, s, c0), hi(a, s, c0 + 31);
+        last_max = s.last(a, hi.i < s.q_length ? hi.i : s.q_length - 1);
+        last_max = lo.i < s.q_length ? last_max : -1;
+        last_min = c0 + 31 < a.columns && hi.i < s.q_length ? s.last(a, lo.i) : -1;
+        first_min = s.first(a, lo.i);
+        first_max = s.first(a, hi.i);
+    }
+    // Whether any column sees a key of j0 .. j1; whether all see all.
+    __device__ __forceinline__ bool any(const AttendArgs &a, int32_t j0, int32_t j1) const
+    {
+        return j0 <= last_max && (j1 >= first_min || j0 < a.sinks);
+    }
+    __device__ __forceinline__ bool all(const AttendArgs &a, int32_t j0, int32_t j1) const
+    {
+        return j1 <= last_min && (j0 >= first_max || j1 < a.sinks);
+    }
+    // Scores x of keys j0 + 32 k (register rows) to weights, and the state.
+    template <int K>
+    __device__ __forceinline__ void weigh(const AttendArgs &a, f32x16 (&x)[K], int32_t j0, int lane)
+    {
+        if (!all(a, j0, j0 + 32 * K - 1))
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int32_t j = j0 + 32 * k + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+                    x[k][e] = sees(j, last, first, a.sinks) ? x[k][e] : -INFINITY;
+                }
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                top = fmaxf(top, x[k][e]);
+        top = both_halves(top, [](float u, float v) { return fmaxf(u, v); }) * a.scale_log2;
+        if (__any(top > m + kBehind)) {
+            const float to = fmaxf(m, top), f = exp2_of(m - to);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+                sum[n] *= f;
+        }
+        float add = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                x[k][e] = exp2_of(fmaf(x[k][e], a.scale_log2, -m));
+                add += x[k][e];
+            }
+        l += add;
+    }
+    // Columns whose sums alone are not finite, again: over keys j0 .. j1 of each
+    // tile that next gives (false: none left), what the column sees.
+    template <typename Next>
+    __device__ __forceinline__ void mend(const AttendArgs &a, const Sequence &s, int32_t c0,
+                                         int lane, Next next)
+    {
+        const bool bad = any_not_finite(sum) && fabsf(l) < INFINITY && last >= 0;
+        uint64_t which = __ballot(bad);
+        which = (which | which >> 32) & 0xffffffffu;
+        while (which) {
+            const int col = __builtin_ctzll(which);
+            which &= which - 1;
+            const int32_t to = __builtin_amdgcn_readlane(last, col);
+            const int32_t from = __builtin_amdgcn_readlane(first, col);
+            const float top = __builtin_bit_cast(
+                float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), col));
+            const Column c(a, s, c0 + col);
+            const Spread x = Spread::of(s.rows<T>(a.q, c.head) + c.i * a.q.row, a.dim, lane);
+            Spread y = {0.0f, 0.0f};
+            int32_t j0, j1;
+            for (int32_t n = 0; next(n, &j0, &j1); ++n)
+                for (int32_t j = j0; j <= j1 && j <= to; ++j) {
+                    if (!sees(j, to, from, a.sinks))
+                        continue;
+                    const Spread k = Spread::of(s.rows<T>(a.k, s.kv) + j * a.k.row, a.dim, lane);
+                    const Spread v = Spread::of(s.rows<T>(a.v, s.kv) + j * a.v.row, a.dim, lane);
+                    // not 0: an infinity counts however small its weight
+                    const float w =
+                        fmaxf(exp2_of(fmaf(dot(x, k), a.scale_log2, -top)), 1.0e-37f);
+                    y.x = fmaf(w, v.x, y.x);
+                    y.y = fmaf(w, v.y, y.y);
+                    if (settled(y, a.dim, lane))
+                        break;
+                }
+            set_column(sum, y, col, lane);
+        }
+    }
+    // Rows of out, rest and lse; or, of a part of the keys, sums, m and l.
+    __device__ __forceinline__ void finish(const AttendArgs &a, const Sequence &s, int32_t c0,
+                                           uint32_t pair, uint32_t split, int lane)
+    {
+        l = both_halves(l, [](float u, float v) { return u + v; });
+        const int32_t at = c0 + (lane & 31);
+        if (at >= a.columns)
+            return;
+        if (a.splits > 1) {
+            const int64_t row = ((int64_t)split * a.pairs + pair) * a.columns + at;
+            float *p = a.part + row * (N * 32);
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *(f32x4 *)(p + 32 * n + 8 * g + 4 * (lane >> 5)) =
+                        f32x4{sum[n][4 * g], sum[n][4 * g + 1], sum[n][4 * g + 2],
+                              sum[n][4 * g + 3]};
+            if (lane < 32) {
+                float *ml = a.part + (int64_t)a.splits * a.pairs * a.columns * (N * 32) + 2 * row;
+                ml[0] = m;
+                ml[1] = l;
+            }
+            return;
+        }
+        const Column c(a, s, at);
+        const float f = last < 0 ? 0.0f : 1.0f / l;
+        T *out = (T *)s.rows<T>(a.out, c.head) + c.i * a.out.row;
+        const int64_t row = ((int64_t)s.b * a.queries + c.i) * a.heads + c.head;
+        T *rest = a.rest ? (T *)a.rest + row * a.dim : nullptr;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int32_t d = 32 * n + 8 * g + 4 * (lane >> 5);
+                if (d >= a.dim)
+                    continue;
+                vec<float, 4> y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    y[e] = last < 0 ? 0.0f : sum[n][4 * g + e] * f;
+                const vec<T, 4> z = from_f32<T, 4>(y);
+                store<T, 4>(out + d, z);
+                if (rest)
+                    store<T, 4>(rest + d, from_f32<T, 4>(y - to_f32<4, T>(z)));
+            }
+        if (a.lse && lane < 32)
+            a.lse[row] = last < 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+};
+
+// Which work a workgroup has: a pair of a sequence and a key head (the fastest
+// index: neighbours on a die's L2 share keys), a tile of columns, a part of the
+// keys. Causal tiles run from the last, which has most keys.
+struct Task {
+    uint32_t pair, tile, split;
+    __device__ __forceinline__ Task(const AttendArgs &a)
+    {
+        const uint32_t rest = divide(blockIdx.x, a.pair_div);
+        pair = blockIdx.x - rest * a.pair_div.d;
+        split = divide(rest, a.tile_div);
+        tile = rest - split * a.tile_div.d;
+        if (a.causal)
+            tile = a.tiles - 1 - tile;
+    }
+};
+
+// Four waves of 32 columns each over shared tiles of 64 keys.
+template <typename T, int N>
+__global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
+    attend_kernel(AttendArgs a)
+{
+    constexpr int kThreads = 64 * kAttendWaves, kKeys = kAttendKeys;
+    typedef LdsRows<T, N, 16> KeyRows;
+    typedef LdsRows<T, N, sizeof(T) == 2 ? 32 : 16> ValueRows;
+    constexpr int kKeyBytes = kKeys * KeyRows::kStride, kValueBytes = kKeys * ValueRows::kStride;
+    __shared__ __attribute__((aligned(16))) char lds[2][kKeyBytes + kValueBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Task task(a);
+    const Sequence s(a, task.pair);
+    const int32_t c0 = task.tile * (kAttendWaves * 32), mine = c0 + wave * 32;
+    const Column c_first(a, s, c0), c_last(a, s, c0 + kAttendWaves * 32 - 1);
+    const Walk<kKeys> walk(a, s, c_first.i, c_last.i);
+    const int32_t lo = (int32_t)((int64_t)walk.count * task.split / a.splits);
+    const int32_t hi = (int32_t)((int64_t)walk.count * (task.split + 1) / a.splits);
+    Columns<T, N> cols;
+    cols.start(a, s, mine, lane);
+    const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
+    Mover<T, N, kKeys, kThreads> k, v;
+    const auto fetch = [&](int32_t n) {
+        const int32_t j0 = walk.tile(n) * kKeys;
+        k.fetch(kp, a.k.row, j0, s.k_length, a.dim, threadIdx.x);
+        v.fetch(vp, a.v.row, j0, s.k_length, a.dim, threadIdx.x);
+    };
+    if (lo < hi)
+        fetch(lo);
+    const int key_at = KeyRows::row_at(lane), value_at = ValueRows::column_at(lane);
+    for (int32_t n = lo; n < hi; ++n) {
+        char *keys = lds[(n - lo) & 1], *values = keys + kKeyBytes;
+        k.template put<16>(keys, threadIdx.x);
+        v.template put<sizeof(T) == 2 ? 32 : 16>(values, threadIdx.x);
+        // a tile is written again two turns on, behind the next turn's barrier
+        __syncthreads();
+        if (n + 1 < hi)
+            fetch(n + 1);
+        const int32_t j0 = walk.tile(n) * kKeys;
+        if (!cols.any(a, j0, j0 + kKeys - 1))
+            continue;
+        f32x16 x[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            x[h] = (f32x16)0.0f;
+#pragma unroll
+            for (int t = 0; t < 2 * N; ++t)
+                multiply<T>(x[h], KeyRows::row(keys, key_at, 32 * h, t), cols.q[t]);
+        }
+        cols.weigh(a, x, j0, lane);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const vec<T, 8> w = operand<T>(x[g >> 1], g & 1);
+#pragma unroll
+            for (int n2 = 0; n2 < N; ++n2)
+                multiply<T>(cols.sum[n2], ValueRows::column(values, value_at, 16 * g, n2), w);
+        }
+    }
+    cols.mend(a, s, mine, lane, [&](int32_t n, int32_t *j0, int32_t *j1) {
+        if (lo + n >= hi)
+            return false;
+        *j0 = walk.tile(lo + n) * kKeys;
+        *j1 = *j0 + kKeys - 1;
+        return true;
+    });
+    cols.finish(a, s, mine, task.pair, task.split, lane);
+}
+
+// 32 columns a workgroup: its four waves take tiles of 32 keys in turn, each
+// with its own piece of LDS and no barrier, and join their sums at the end.
+template <typename T, int N>
+__global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
+    attend_few_kernel(AttendArgs a)
+{
+    constexpr int kKeys = kAttendFewKeys;
+    typedef LdsRows<T, N, sizeof(T) == 2 ? 32 : 16> ValueRows;
+    constexpr int kBytes = kKeys * ValueRows::kStride;
+    static_assert(kAttendWaves * kBytes >= 2 * 64 * N * 16 * 4, "room for two waves' sums");
+    __shared__ __attribute__((aligned(16))) char lds[kAttendWaves * kBytes];
+    __shared__ float tops[kAttendWaves][32], sums[kAttendWaves][32];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Task task(a);
+    const Sequence s(a, task.pair);
+    const int32_t c0 = task.tile * 32;
+    const Column c_first(a, s, c0), c_last(a, s, c0 + 31);
+    const Walk<kKeys> walk(a, s, c_first.i, c_last.i);
+    const int32_t lo = (int32_t)((int64_t)walk.count * task.split / a.splits);
+    const int32_t hi = (int32_t)((int64_t)walk.count * (task.split + 1) / a.splits);
+    Columns<T, N> cols;
+    cols.start(a, s, c0, lane);
+    const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
+    char *values = lds + wave * kBytes;
+    vec<T, 8> k[2 * N];
+    Mover<T, N, kKeys, 64> v;
+    const auto fetch = [&](int32_t n) {
+        const int32_t j0 = walk.tile(n) * kKeys, j = j0 + (lane & 31);
+        row_operands<T, N>(kp + (j < s.k_length ? j : s.k_length - 1) * a.k.row, a.dim, lane, k);
+        v.fetch(vp, a.v.row, j0, s.k_length, a.dim, lane);
+    };
+    const int32_t own = lo + wave;
+    if (own < hi)
+        fetch(own);
+    const int value_at = ValueRows::column_at(lane);
+    for (int32_t n = own; n < hi; n += kAttendWaves) {
+        const int32_t j0 = walk.tile(n) * kKeys;
+        f32x16 x[1] = {(f32x16)0.0f};
+#pragma unroll
+        for (int t = 0; t < 2 * N; ++t)
+            multiply<T>(x[0], k[t], cols.q[t]);
+        asm volatile("" ::: "memory");  // the wave's reads of the last tile come first
+        v.template put<sizeof(T) == 2 ? 32 : 16>(values, lane);
+        asm volatile("" ::: "memory");  // other lanes read what this one writes
+        if (n + kAttendWaves < hi)
+            fetch(n + kAttendWaves);
+        cols.weigh(a, x, j0, lane);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const vec<T, 8> w = operand<T>(x[0], g);
+#pragma unroll
+            for (int n2 = 0; n2 < N; ++n2)
+                multiply<T>(cols.sum[n2], ValueRows::column(values, value_at, 16 * g, n2), w);
+        }
+    }
+    cols.mend(a, s, c0, lane, [&](int32_t n, int32_t *j0, int32_t *j1) {
+        if (own + n * kAttendWaves >= hi)
+            return false;
+        *j0 = walk.tile(own + n * kAttendWaves) * kKeys;
+        *j1 = *j0 + kKeys - 1;
+        return true;
+    });
+    // the waves' sums at one maximum, then waves 2 and 3 into 0 and 1, 1 into 0
+    const float half = both_halves(cols.l, [](float u, float v) { return u + v; });
+    if (lane < 32) {
+        tops[wave][lane] = cols.m;
+        sums[wave][lane] = half;
+    }
+    __syncthreads();
+    float top = tops[0][lane & 31], total = 0.0f;
+#pragma unroll
+    for (int w = 1; w < kAttendWaves; ++w)
+        top = fmaxf(top, tops[w][lane & 31]);
+#pragma unroll
+    for (int w = 0; w < kAttendWaves; ++w)
+        total += sums[w][lane & 31] * exp2_of(tops[w][lane & 31] - top);
+    const float f = exp2_of(cols.m - top);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+        cols.sum[n] *= f;
+    cols.m = top;
+    float *room = (float *)lds;
+#pragma unroll
+    for (int step = 2; step >= 1; step >>= 1) {
+        if (wave >= step && wave < 2 * step)
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    room[((wave - step) * N * 16 + n * 16 + e) * 64 + lane] = cols.sum[n][e];
+        __syncthreads();
+        if (wave < step)
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    cols.sum[n][e] += room[(wave * N * 16 + n * 16 + e) * 64 + lane];
+        __syncthreads();
+    }
+    if (wave != 0)
+        return;
+    cols.l = lane < 32 ? total : 0.0f;  // finish adds the halves
+    cols.finish(a, s, c0, task.pair, task.split, lane);
+}
+
+// Joins the parts of the keys, in order: a wave a column.
+template <typename T, int N>
+__global__ void __launch_bounds__(64 * kAttendWaves) attend_join_kernel(AttendArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t at = (int64_t)blockIdx.x * kAttendWaves +
+                       __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (at >= (int64_t)a.pairs * a.columns)
+        return;
+    const uint32_t pair = (uint32_t)(at / a.columns);
+    const Sequence s(a, pair);
+    const Column c(a, s, (int32_t)(at - (int64_t)pair * a.columns));
+    const int64_t rows = (int64_t)a.pairs * a.columns;
+    const float *ml = a.part + (int64_t)a.splits * rows * (N * 32) + 2 * at;
+    const bool own = lane < a.splits;  // splits <= 64
+    const float m = own ? ml[2 * lane * rows] : kLowest, l = own ? ml[2 * lane * rows + 1] : 0.0f;
+    float top = m;
+#pragma unroll
+    for (int step = 32; step; step >>= 1)
+        top = fmaxf(top, __shfl_xor(top, step));
+    const float f = exp2_of(m - top);
+    const float total = wave_sum(l * f);
+    Spread y = {0.0f, 0.0f};
+    for (int k = 0; k < a.splits; ++k) {
+        const float w = __shfl(f, k);
+        const float *p = a.part + (k * rows + at) * (N * 32);
+        y.x = fmaf(w, lane < N * 32 ? p[lane] : 0.0f, y.x);
+        if (N > 2)
+            y.y = fmaf(w, lane + 64 < N * 32 ? p[lane + 64] : 0.0f, y.y);
+    }
+    const bool none = s.last(a, c.i) < 0;
+    const float inv = 1.0f / total;
+    T *out = (T *)s.rows<T>(a.out, c.head) + c.i * a.out.row;
+    const int64_t row = ((int64_t)s.b * a.queries + c.i) * a.heads + c.head;
+    const auto write = [&](int32_t d, float v) {
+        if (d >= a.dim)
+            return;
+        v = none ? 0.0f : v * inv;
+        const T z = (T)v;
+        out[d] = z;
+        if (a.rest)
+            ((T *)a.rest)[row * a.dim + d] = (T)(v - (float)z);
+    };
+    write(lane, y.x);
+    if (N > 2)
+        write(lane + 64, y.y);
+    if (a.lse && lane == 0)
+        a.lse[row] = none ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
+template <typename T>
+int launch_attend(const AttendArgs &a, int kernel, int wide, unsigned grid, void *s)
+{
+    const auto with = [&](auto n) {
+        constexpr int N = decltype(n)::value;
+        const dim3 g(grid), b(64 * kAttendWaves);
+        hipStream_t st = (hipStream_t)s;
+        if (kernel == kAttendMany)
+            hipLaunchKernelGGL((attend_kernel<T, N>), g, b, 0, st, a);
+        else if (kernel == kAttendFew)
+            hipLaunchKernelGGL((attend_few_kernel<T, N>), g, b, 0, st, a);
+        else
+            hipLaunchKernelGGL((attend_join_kernel<T, N>), g, b, 0, st, a);
+    };
+    if (wide == 1)
+        with(std::integral_constant<int, 1>{});
+    else if (wide == 2)
+        with(std::integral_constant<int, 2>{});
+    else if (wide == 3)
+        with(std::integral_constant<int, 3>{});
+    else
+        with(std::integral_constant<int, 4>{});
+    return (int)hipGetLastError();
+}
+
+}  // namespace
+}  // namespace smol
+
+#endif  // SMOL_ATTEND_KERNELS_H

@@ -13,29 +13,10 @@
 
 #include <type_traits>
 
-#include "smol_magic.h"
 #include "smol_tokens.h"
 #include "smol_tokens_device.h"
 
 namespace smol {
-
-// Division by a fixed divisor (smol_magic.h).
-struct Divisor {
-    uint32_t d, m, s;
-};
-
-inline Divisor make_divisor(uint32_t d)
-{
-    Divisor v;
-    v.d = d;
-    magic_divisor(d, &v.m, &v.s);
-    return v;
-}
-
-__device__ __forceinline__ uint32_t divide(uint32_t n, const Divisor &v)
-{
-    return (uint32_t)((uint64_t)n * v.m >> v.s);
-}
 
 struct PatchArgs {
     const void *images, *weight, *bias, *pos;

@@ -1,10 +1,13 @@
-// smol_tokens_device.h -- what the token kernels share: element types, loads
-// and stores at element alignment, sums over a wave.
+// smol_tokens_device.h -- what the token and attention kernels share: element
+// types, loads and stores at element alignment, sums over a wave, division by a
+// fixed divisor.
 #ifndef SMOL_TOKENS_DEVICE_H
 #define SMOL_TOKENS_DEVICE_H
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include "smol_magic.h"
 
 namespace smol {
 
@@ -72,6 +75,24 @@ __device__ __forceinline__ float wave_sum(float x)
     SMOL_DPP_ADD(0x143, 0xc);  // row_bcast:31 into rows 2 and 3
 #undef SMOL_DPP_ADD
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
+// Division by a fixed divisor (smol_magic.h).
+struct Divisor {
+    uint32_t d, m, s;
+};
+
+inline Divisor make_divisor(uint32_t d)
+{
+    Divisor v;
+    v.d = d;
+    magic_divisor(d, &v.m, &v.s);
+    return v;
+}
+
+__device__ __forceinline__ uint32_t divide(uint32_t n, const Divisor &v)
+{
+    return (uint32_t)((uint64_t)n * v.m >> v.s);
 }
 
 // Calls f with a value of the C++ type of an element type.
