@@ -189,6 +189,17 @@ SIGNATURES = {
     "smol_layer_norm": (ctypes.c_int, [_vp, _vp]),
     "smol_layer_norm_backward": (ctypes.c_int, [_vp, _vp]),
     "smol_norm_workspace_bytes": (ctypes.c_int64, [ctypes.c_int64, ctypes.c_int32]),
+    "smol_rotary_frequencies": (ctypes.c_int, [_vp, _vp, _vp]),
+    "smol_rotate": (ctypes.c_int, [_vp, _vp]),
+    "smol_rotate_backward": (ctypes.c_int, [_vp, _vp]),
+    "smol_head_norm": (ctypes.c_int, [_vp, _vp]),
+    "smol_head_norm_backward": (ctypes.c_int, [_vp, _vp]),
+    "smol_head_norm_workspace_bytes": (ctypes.c_int64, [ctypes.c_int64, ctypes.c_int32,
+                                                        ctypes.c_int32, ctypes.c_int32]),
+    "smol_attend": (ctypes.c_int, [_vp, _vp]),
+    "smol_attend_backward": (ctypes.c_int, [_vp, _vp]),
+    "smol_attend_workspace_bytes": (ctypes.c_int64, [_vp]),
+    "smol_attend_backward_workspace_bytes": (ctypes.c_int64, [_vp]),
     "smol_stream_probe": (ctypes.c_int, [_vp, ctypes.c_uint64, _vp, ctypes.c_uint64,
                                          ctypes.c_int32, ctypes.c_int32, _vp]),
     "smol_valu_probe": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp, _vp]),

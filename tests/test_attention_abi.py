@@ -194,14 +194,7 @@ def test_empty_calls_enqueue_nothing():
 
 def test_workspace_sizes():
     lib = smol.lib()
-    for name in ("smol_head_norm_workspace_bytes", "smol_attend_workspace_bytes",
-                 "smol_attend_backward_workspace_bytes"):
-        getattr(lib, name).restype = ctypes.c_int64
-    norm = lib.smol_head_norm_workspace_bytes
-
-    def bytes_of(*a):
-        return norm(ctypes.c_int64(a[0]), *a[1:])
-
+    bytes_of = lib.smol_head_norm_workspace_bytes
     assert bytes_of(0, 4, 4, 64) > 0 and 0 < bytes_of(2 ** 30, 1024, 1024, 256) < 1 << 24
     for bad in ((-1, 1, 1, 64), (2 ** 30 + 1, 1, 1, 64), (1, -1, 1, 64), (1, 1, 1025, 64),
                 (1, 1, 1, 0), (1, 1, 1, 257)):
