@@ -22,17 +22,21 @@ struct AttendArgs {
     void *rest;
     float *lse;    // batch x queries x heads
     float *delta;  // the same (backward)
-    float *part;   // forward, splits > 1: sums of parts of the keys
+    float *part;   // sums of parts of the keys (forward, splits > 1), of the columns
+                   // (gradients of keys)
     const int32_t *q_lengths, *k_lengths;
     int32_t queries, keys, heads, dim;
     int32_t columns;       // queries * group: pairs of a query and one of a key head's heads
     int32_t window, sinks; // window 0: none
     int32_t causal;
-    int32_t tiles;         // of the columns, or of the keys (gradients of keys)
+    int32_t tiles;         // of the columns
     int32_t pairs;         // batch * kv_heads
     int32_t splits;
     float scale, scale_log2;  // the second times log2 e
-    Divisor group, pair_div, kv_heads, tile_div;
+    // gradients of keys: tiles of keys that hold sinks, and columns of a part of
+    // these and of the other tiles (as many parts: the two divisors)
+    int32_t sink_tiles, sink_part, tile_part;
+    Divisor group, pair_div, kv_heads, tile_div, sink_div;
 };
 
 constexpr int kAttendKeys = 64;     // of a tile that four waves share
@@ -40,11 +44,12 @@ constexpr int kAttendColumns = 32;  // of a wave
 constexpr int kAttendWaves = 4;     // of a workgroup
 constexpr int kAttendFewKeys = 32;  // of a tile of one wave (few columns)
 constexpr int kAttendSplits = 64;   // parts of the keys at most
+constexpr int kAttendJoinKeys = 4;  // of a workgroup that joins gradients of keys
 
 // Kernels: the forward pass with the waves over columns, or over keys (few
 // columns); the join of its splits; the gradients of queries, and of keys and
-// values.
-enum { kAttendMany, kAttendFew, kAttendJoin, kAttendGradQ, kAttendGradK };
+// values; the join of the latter's parts.
+enum { kAttendMany, kAttendFew, kAttendJoin, kAttendGradQ, kAttendGradK, kAttendGradJoin };
 
 // wide: values of a head in 32s, rounded up.
 int launch_attend_f32(const AttendArgs &a, int kernel, int wide, unsigned grid, void *s);

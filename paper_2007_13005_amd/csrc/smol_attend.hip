@@ -96,9 +96,64 @@ int64_t part_bytes(const smol_attend_shape &s, const Split &p)
     return p.splits * rows * (wide_of(s.dim) * 32 + 2) * 4;
 }
 
+constexpr int64_t kTileGroups = 512, kSinkGroups = 256;  // workgroups that parts make
+constexpr int64_t kKeyParts = 64, kLeastColumns = 512;   // of a tile; of a part
+
+// The parts in which the gradients of keys are formed: a tile of 128 keys takes
+// the columns of all queries that see it, or a part of them.
+struct KeyParts {
+    int32_t tiles, sink_tiles;       // of keys; those that hold sinks
+    int32_t sink_parts, tile_parts;  // of a tile's columns
+    int32_t sink_part, tile_part;    // columns of a part
+    int64_t groups, slots;           // workgroups; those that write a part
+};
+
+KeyParts key_parts_of(const smol_attend_shape &s)
+{
+    constexpr int32_t kKeys = kAttendColumns * kAttendWaves;
+    KeyParts p;
+    const int64_t group = s.heads / s.kv_heads, pairs = (int64_t)s.batch * s.kv_heads;
+    const int64_t all = s.queries * group;
+    const bool window = s.causal && s.window && s.window < s.keys;
+    const int64_t seen =
+        window ? std::min<int64_t>(s.queries, (int64_t)s.window + kKeys - 1) * group : all;
+    p.tiles = (int32_t)ceil_div(s.keys, kKeys);
+    p.sink_tiles = window ? (int32_t)std::min<int64_t>(ceil_div(s.sinks, kKeys), p.tiles) : 0;
+    // two workgroups a compute unit, each with 512 columns or more
+    const auto parts = [&](int64_t groups, int64_t tiles, int64_t columns, int64_t least) {
+        const int64_t n = std::min(groups / std::max<int64_t>(1, tiles * pairs),
+                                   ceil_div(columns, least));
+        return (int32_t)std::max<int64_t>(1, std::min<int64_t>(n, kKeyParts));
+    };
+    p.tile_parts = parts(kTileGroups, p.tiles, seen, kLeastColumns);
+    p.tile_part = (int32_t)(ceil_div(ceil_div(seen, p.tile_parts), 32) * 32);
+    // those of sinks as long as the others' columns
+    p.sink_parts =
+        parts(kSinkGroups, p.sink_tiles, all, std::max<int64_t>(p.tile_part, kLeastColumns));
+    p.sink_part = (int32_t)(ceil_div(ceil_div(all, p.sink_parts), 32) * 32);
+    const int64_t first = (int64_t)p.sink_tiles * p.sink_parts;
+    const int64_t rest = (int64_t)(p.tiles - p.sink_tiles) * p.tile_parts;
+    p.groups = (first + rest) * pairs;
+    // a workgroup's sums stand at its own place
+    p.slots = p.tile_parts > 1 ? p.groups : p.sink_parts > 1 ? first * pairs : 0;
+    return p;
+}
+
 int64_t delta_bytes(const smol_attend_shape &s)
 {
-    return (int64_t)s.queries * s.heads * s.batch * 4;
+    return ((int64_t)s.queries * s.heads * s.batch * 4 + 15) / 16 * 16;
+}
+
+// Whatever the mask: the parts that there can be.
+int64_t grad_bytes(const smol_attend_shape &s)
+{
+    const int64_t keys = kAttendColumns * kAttendWaves, group = s.heads / s.kv_heads;
+    const int64_t parts = std::min(kKeyParts, ceil_div(s.queries * group, kLeastColumns));
+    const int64_t slots = parts > 1 ? std::min(kTileGroups + kSinkGroups,
+                                               ceil_div(s.keys, keys) * s.batch * s.kv_heads *
+                                                   parts)
+                                    : 0;
+    return delta_bytes(s) + slots * 2 * keys * wide_of(s.dim) * 32 * 4;
 }
 
 // Strides of sequences, rows and heads: those that are read may be 0; what is
@@ -181,7 +236,7 @@ int check_workspace(const void *p, int64_t have, int64_t need)
 
 int launch(const AttendArgs &a, int kernel, int type, int dim, int64_t grid, void *s)
 {
-    const bool grad = kernel == kAttendGradQ || kernel == kAttendGradK;
+    const bool grad = kernel >= kAttendGradQ;
     const auto f = type == SMOL_ELEM_F32   ? grad ? launch_attend_grad_f32 : launch_attend_f32
                    : type == SMOL_ELEM_F16 ? grad ? launch_attend_grad_f16 : launch_attend_f16
                    : grad                  ? launch_attend_grad_bf16
@@ -205,7 +260,7 @@ extern "C" int64_t smol_attend_backward_workspace_bytes(const smol_attend_shape 
     using namespace smol;
     if (!s || check_shape(*s) != SMOL_OK)
         return 0;
-    return delta_bytes(*s) + 16;
+    return grad_bytes(*s) + 16;
 }
 
 extern "C" int smol_attend(const smol_attend_args *p, void *stream)
@@ -244,8 +299,7 @@ extern "C" int smol_attend(const smol_attend_args *p, void *stream)
     int e = launch(a, split.few ? kAttendFew : kAttendMany, s.type, s.dim,
                    (int64_t)split.tiles * a.pairs * split.splits, stream);
     if (e == hipSuccess && split.splits > 1)
-        e = launch(a, kAttendJoin, s.type, s.dim,
-                   ceil_div((int64_t)a.pairs * a.columns, kAttendWaves), stream);
+        e = launch(a, kAttendJoin, s.type, s.dim, (int64_t)a.pairs * a.columns, stream);
     if (e != hipSuccess)
         return set_error(SMOL_ERR_HIP, "attention launch: %s", hipGetErrorString((hipError_t)e));
     return SMOL_OK;
@@ -283,8 +337,11 @@ extern "C" int smol_attend_backward(const smol_attend_grad_args *p, void *stream
         return set_error(SMOL_ERR_INVALID_ARG, "lse is NULL or not aligned to its elements");
     if ((uintptr_t)p->rest % elem_size(s.type))
         return set_error(SMOL_ERR_INVALID_ARG, "rest is not aligned to its elements");
-    if ((st = check_workspace(p->workspace, p->workspace_bytes, delta_bytes(s))) != SMOL_OK)
+    if ((st = check_workspace(p->workspace, p->workspace_bytes, grad_bytes(s))) != SMOL_OK)
         return st;
+    const KeyParts parts = key_parts_of(s);
+    if (parts.groups > kMostGroups)
+        return set_error(SMOL_ERR_UNSUPPORTED, "too many rows and heads for a launch");
     a.lse = (float *)p->lse;
     a.rest_in = p->rest;
     a.delta = (float *)p->workspace;
@@ -294,8 +351,19 @@ extern "C" int smol_attend_backward(const smol_attend_grad_args *p, void *stream
         e = launch(a, kAttendGradQ, s.type, s.dim, (int64_t)a.tiles * a.pairs, stream);
     }
     if (e == hipSuccess && s.keys > 0) {
-        a.tiles = (int32_t)ceil_div(s.keys, kAttendColumns * kAttendWaves);
-        e = launch(a, kAttendGradK, s.type, s.dim, (int64_t)a.tiles * a.pairs, stream);
+        a.part = (float *)((char *)p->workspace + delta_bytes(s));
+        a.sink_tiles = parts.sink_tiles;
+        a.sink_part = parts.sink_part;
+        a.tile_part = parts.tile_part;
+        a.sink_div = make_divisor(parts.sink_parts);
+        a.tile_div = make_divisor(parts.tile_parts);
+        e = launch(a, kAttendGradK, s.type, s.dim, parts.groups, stream);
+        const int64_t joined = parts.tile_parts > 1   ? parts.tiles
+                               : parts.sink_parts > 1 ? parts.sink_tiles
+                                                      : 0;
+        if (e == hipSuccess && joined)
+            e = launch(a, kAttendGradJoin, s.type, s.dim,
+                       joined * (kAttendColumns * kAttendWaves / kAttendJoinKeys) * a.pairs, stream);
     }
     if (e != hipSuccess)
         return set_error(SMOL_ERR_HIP, "attention backward launch: %s",

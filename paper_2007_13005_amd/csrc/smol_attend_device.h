@@ -216,36 +216,63 @@ __device__ __forceinline__ void row_operands(const T *row, int32_t dim, int lane
     }
 }
 
-// Chunks of a tile's rows that one of `Threads` threads moves to LDS.
+// Chunks of a tile's rows that one of `Threads` threads moves to LDS: chunk c of
+// rows r, r + kPass, .... Where the tile's rows all exist a chunk's address is a
+// base that the wave shares and 32 bits of the lane's own; past the last row (and
+// where strides do not fit 32 bits) rows are looked at one by one.
 template <typename T, int N, int Rows, int Threads>
 struct Mover {
     typedef LdsRows<T, N, 16> Layout;
-    static constexpr int kCount = Rows * Layout::kChunks / Threads;
-    static_assert(kCount * Threads == Rows * Layout::kChunks, "whole chunks a thread");
-    typename Layout::Chunk v[kCount];
-    // Rows row0 .. of `rows` (>= 1), zeros past them and past the head.
-    __device__ __forceinline__ void fetch(const T *p, int64_t stride, int32_t row0, int32_t rows,
-                                          int32_t dim, int thread)
+    typedef typename Layout::Chunk Chunk;
+    static constexpr int kSlots = Layout::kChunks == 12 ? 16 : Layout::kChunks == 24 ? 32
+                                                                               : Layout::kChunks;
+    static constexpr int kPass = Threads / kSlots, kCount = Rows / kPass;
+    static_assert(kPass * kSlots == Threads && kCount * kPass == Rows, "whole passes");
+    Chunk v[kCount];
+    int32_t r, c;
+    bool some;  // the lane's chunk is within the head; else it stays zeros
+    __device__ __forceinline__ Mover(int32_t dim, int thread)
     {
+        r = thread / kSlots;
+        c = thread % kSlots;
+        some = c * Layout::kEach < dim;
+#pragma unroll
+        for (int n = 0; n < kCount; ++n)
+            v[n] = (Chunk)(T)0.0f;
+    }
+    // Whether kPass rows' offsets fit 32 bits.
+    static __device__ __forceinline__ bool near(int64_t stride)
+    {
+        return stride < ((int64_t)1 << 31) / (kPass * (int)sizeof(T));
+    }
+    // Rows row0 .. of `rows` (>= 1), zeros past them.
+    __device__ __forceinline__ void fetch(const T *p, int64_t stride, int32_t row0, int32_t rows)
+    {
+        if (near(stride) && row0 + Rows <= rows) {
+            const char *base = (const char *)(p + row0 * stride);
+            const uint32_t at = (uint32_t)(r * (int32_t)stride + c * Layout::kEach) * sizeof(T);
+            if (some)
+#pragma unroll
+                for (int n = 0; n < kCount; ++n)
+                    v[n] = load<T, Layout::kEach>(
+                        (const T *)(base + n * kPass * stride * (int)sizeof(T) + at));
+            return;
+        }
 #pragma unroll
         for (int n = 0; n < kCount; ++n) {
-            const int id = thread + Threads * n, r = id / Layout::kChunks;
-            const int32_t at = id % Layout::kChunks * Layout::kEach, row = row0 + r;
-            const bool some = row < rows && at < dim;
-            v[n] = load<T, Layout::kEach>(p + (row < rows ? row : rows - 1) * stride +
-                                          (at < dim ? at : 0));
-            if (!some)
-                v[n] = (typename Layout::Chunk)(T)0.0f;
+            const int32_t row = row0 + r + kPass * n;
+            v[n] = (Chunk)(T)0.0f;
+            if (some && row < rows)
+                v[n] = load<T, Layout::kEach>(p + row * stride + c * Layout::kEach);
         }
     }
     template <int Pad>
-    __device__ __forceinline__ void put(char *tile, int thread) const
+    __device__ __forceinline__ void put(char *tile) const
     {
+        if (kSlots == Layout::kChunks || c < Layout::kChunks)
 #pragma unroll
-        for (int n = 0; n < kCount; ++n) {
-            const int id = thread + Threads * n;
-            LdsRows<T, N, Pad>::put(tile, id / Layout::kChunks, id % Layout::kChunks, v[n]);
-        }
+            for (int n = 0; n < kCount; ++n)
+                LdsRows<T, N, Pad>::put(tile, r + kPass * n, c, v[n]);
     }
 };
 

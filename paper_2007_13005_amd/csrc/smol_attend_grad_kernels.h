@@ -119,19 +119,19 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     for (int n = 0; n < N; ++n)
         sum[n] = (f32x16)0.0f;
     const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
-    Mover<T, N, kKeys, kThreads> k, v;
+    Mover<T, N, kKeys, kThreads> k(a.dim, threadIdx.x), v(a.dim, threadIdx.x);
     const auto fetch = [&](int32_t n) {
         const int32_t j0 = walk.tile(n) * kKeys;
-        k.fetch(kp, a.k.row, j0, s.k_length, a.dim, threadIdx.x);
-        v.fetch(vp, a.v.row, j0, s.k_length, a.dim, threadIdx.x);
+        k.fetch(kp, a.k.row, j0, s.k_length);
+        v.fetch(vp, a.v.row, j0, s.k_length);
     };
     if (walk.count)
         fetch(0);
     const int row_at = Rows::row_at(lane), column_at = Rows::column_at(lane);
     for (int32_t n = 0; n < walk.count; ++n) {
         char *keys = lds[n & 1], *values = keys + kBytes;
-        k.template put<16>(keys, threadIdx.x);
-        v.template put<16>(values, threadIdx.x);
+        k.template put<16>(keys);
+        v.template put<16>(values);
         __syncthreads();  // a tile is written again two turns on
         if (n + 1 < walk.count)
             fetch(n + 1);
@@ -203,84 +203,140 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
                         a.scale * kCarried<T>, last < 0, a.dim, lane);
 }
 
+// The queries that see any of keys j0 .. j1, and their columns.
+struct KeySpan {
+    int32_t begin, end;  // columns
+    __device__ __forceinline__ KeySpan(const AttendArgs &a, const Sequence &s, int32_t j0,
+                                       int32_t j1)
+    {
+        int32_t i0 = 0, i1 = s.q_length - 1;
+        if (a.causal) {
+            i0 = j0 - s.shift > 0 ? j0 - s.shift : 0;
+            // position p sees down to p - window + 1 (a window is less than the keys)
+            if (a.window && j0 >= a.sinks && j1 + a.window - 1 - s.shift < i1)
+                i1 = j1 + a.window - 1 - s.shift;
+        }
+        const bool some = j0 < s.k_length && i0 <= i1;
+        begin = some ? i0 * (int32_t)a.group.d : 0;
+        end = some ? (i1 + 1) * (int32_t)a.group.d : 0;
+    }
+};
+
+// A workgroup's keys and part of their columns. Tiles that hold sinks come first:
+// all later queries see them, so they have most columns, and parts of their own
+// size.
+struct KeyTask {
+    uint32_t pair, tile, part;
+    bool whole;  // the only part
+    int32_t begin, end;
+    __device__ __forceinline__ KeyTask(const AttendArgs &a)
+    {
+        const uint32_t unit = divide(blockIdx.x, a.pair_div);
+        pair = blockIdx.x - unit * a.pair_div.d;
+        const uint32_t first = a.sink_tiles * a.sink_div.d;
+        if (unit < first) {
+            tile = divide(unit, a.sink_div);
+            part = unit - tile * a.sink_div.d;
+            whole = a.sink_div.d == 1;
+        } else {
+            const uint32_t n = divide(unit - first, a.tile_div);
+            tile = a.sink_tiles + n;
+            part = unit - first - n * a.tile_div.d;
+            whole = a.tile_div.d == 1;
+        }
+    }
+    __device__ __forceinline__ int32_t size(const AttendArgs &a) const
+    {
+        return tile < (uint32_t)a.sink_tiles ? a.sink_part : a.tile_part;
+    }
+};
+
 // Gradients of keys and values: four waves of 32 keys each over shared tiles of
-// 32 columns, all the columns (queries and heads) that read these keys.
+// 32 columns, the columns (queries and heads) that read these keys or a part of
+// them. Keys stay in registers and values in LDS, which leaves room for two waves
+// a SIMD.
 template <typename T, int N>
-__global__ void __launch_bounds__(64 * kAttendWaves, 1) attend_grad_k_kernel(AttendArgs a)
+__global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
+    attend_grad_k_kernel(AttendArgs a)
 {
-    constexpr int kThreads = 64 * kAttendWaves, kCols = 32;
+    constexpr int kThreads = 64 * kAttendWaves, kCols = 32, kKeys = kAttendWaves * 32;
     typedef LdsRows<T, N, 16> Rows;
+    typedef typename Rows::Chunk Chunk;
     constexpr int kBytes = kCols * Rows::kStride;
     __shared__ __attribute__((aligned(16))) char lds[2][2 * kBytes];
+    __shared__ __attribute__((aligned(16))) char values[kKeys * Rows::kStride];
     __shared__ __attribute__((aligned(16))) float lses[2][kCols], deltas[2][kCols];
     __shared__ __attribute__((aligned(16))) int32_t lasts[2][kCols], firsts[2][kCols];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t tile = divide(blockIdx.x, a.pair_div);
-    const uint32_t pair = blockIdx.x - tile * a.pair_div.d;
-    const Sequence s(a, pair);
-    const int32_t j0 = tile * (kAttendWaves * 32), j1 = j0 + kAttendWaves * 32 - 1;
-    const int32_t mine = j0 + wave * 32, j = mine + (lane & 31);
-    const int32_t group = (int32_t)a.group.d;
-    // the queries that see any key of the workgroup's
-    int32_t i0 = 0, i1 = s.q_length - 1;
-    if (a.causal) {
-        i0 = j0 - s.shift > 0 ? j0 - s.shift : 0;
-        // position p sees down to p - window + 1 (windows reach 2^25 at most)
-        if (a.window && j0 >= a.sinks && j1 + a.window - 1 - s.shift < i1)
-            i1 = j1 + a.window - 1 - s.shift;
+    const KeyTask task(a);
+    const Sequence s(a, task.pair);
+    const int32_t j0 = task.tile * kKeys, mine = j0 + wave * 32, j = mine + (lane & 31);
+    const int32_t group = (int32_t)a.group.d, head0 = s.kv * group;
+    const KeySpan span(a, s, j0, j0 + kKeys - 1);
+    int32_t c_begin = span.begin, c_end = span.end;
+    if (!task.whole) {
+        const int32_t size = task.size(a);
+        const int64_t from = (int64_t)c_begin + (int64_t)task.part * size;
+        c_begin = from < c_end ? (int32_t)from : c_end;
+        c_end = c_end - c_begin < size ? c_end : c_begin + size;
+        if (c_begin >= c_end)
+            return;  // the join knows that this part is empty
     }
-    const bool some = j0 < s.k_length && i0 <= i1;
-    const int32_t c_begin = i0 * group, c_end = some ? (i1 + 1) * group : c_begin;
     f32x16 dk[N], dv[N];
 #pragma unroll
     for (int n = 0; n < N; ++n)
         dk[n] = dv[n] = (f32x16)0.0f;
     const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
-    vec<T, 8> k[2 * N], v[2 * N];
-    {
-        const int32_t row = j < a.keys ? j : a.keys - 1;
-        row_operands<T, N>(kp + row * a.k.row, a.dim, lane, k);
-        row_operands<T, N>(vp + row * a.v.row, a.dim, lane, v);
+    vec<T, 8> k[2 * N];
+    if (c_begin < c_end) {
+        row_operands<T, N>(kp + (j < a.keys ? j : a.keys - 1) * a.k.row, a.dim, lane, k);
+        Mover<T, N, kKeys, kThreads> v(a.dim, threadIdx.x);
+        v.fetch(vp, a.v.row, j0, s.k_length);
+        v.template put<16>(values);
     }
-    typedef typename Rows::Chunk Chunk;
-    constexpr int kTotal = kCols * Rows::kChunks;
-    constexpr int kMoved = (kTotal + kThreads - 1) / kThreads;
+    // what the thread moves: chunk m_c of rows m_r, m_r + kPass, ..., and of the
+    // first 32 threads one column's numbers
+    constexpr int kSlots = Mover<T, N, kKeys, kThreads>::kSlots, kPass = kThreads / kSlots;
+    constexpr int kMoved = kPass < kCols ? kCols / kPass : 1;
+    const int m_r = threadIdx.x / kSlots, m_c = threadIdx.x % kSlots;
+    const bool m_some = m_c * Rows::kEach < a.dim && m_r < kCols;
+    const T *qp = s.rows<T>(a.q, head0) + m_c * Rows::kEach;
+    const T *dp = s.rows<T>(a.dout, head0) + m_c * Rows::kEach;
+    const int64_t stat0 = (int64_t)s.b * a.queries * a.heads + head0;
     Chunk mq[kMoved], md[kMoved];
     float m_lse = 0.0f, m_delta = 0.0f;
     int32_t m_last = -1, m_first = 0;
     const auto fetch = [&](int32_t c0) {
 #pragma unroll
         for (int n = 0; n < kMoved; ++n) {
-            const int id = threadIdx.x + kThreads * n, r = id / Rows::kChunks;
-            const int32_t at = id % Rows::kChunks * Rows::kEach;
-            const int32_t cc = c0 + r < c_end ? c0 + r : c_end - 1;
-            const Column c(a, s, cc);
-            const int32_t d = at < a.dim ? at : 0;
-            mq[n] = load<T, Rows::kEach>(s.rows<T>(a.q, c.head) + c.i * a.q.row + d);
-            md[n] = load<T, Rows::kEach>(s.rows<T>(a.dout, c.head) + c.i * a.dout.row + d);
-            if (c0 + r >= c_end || at >= a.dim)
-                mq[n] = md[n] = (Chunk)(T)0.0f;
+            const int32_t c = c0 + m_r + n * kPass, i = (int32_t)divide(c, a.group);
+            const int32_t g = c - i * group;
+            mq[n] = md[n] = (Chunk)(T)0.0f;
+            if (m_some && c < c_end) {
+                mq[n] = load<T, Rows::kEach>(qp + (i * a.q.row + g * a.q.head));
+                md[n] = load<T, Rows::kEach>(dp + (i * a.dout.row + g * a.dout.head));
+            }
         }
         if (threadIdx.x < kCols) {
-            const int32_t at = c0 + threadIdx.x;
-            const Column c(a, s, at < c_end ? at : c_end - 1);
-            const int64_t row = ((int64_t)s.b * a.queries + c.i) * a.heads + c.head;
-            m_last = at < c_end ? s.last(a, c.i) : -1;
-            m_first = s.first(a, c.i);
-            m_lse = m_last < 0 ? 0.0f : a.lse[row] * kLog2e;
-            m_delta = a.delta[row];
+            const int32_t c = c0 + threadIdx.x, i = (int32_t)divide(c, a.group);
+            m_last = c < c_end ? s.last(a, i) : -1;
+            m_first = s.first(a, i);
+            m_lse = m_delta = 0.0f;
+            if (m_last >= 0) {
+                const int64_t row = stat0 + (int64_t)i * a.heads + c - i * group;
+                m_lse = a.lse[row] * kLog2e;
+                m_delta = a.delta[row];
+            }
         }
     };
     const auto put = [&](int buffer) {
         char *to = lds[buffer];
+        if (m_c < Rows::kChunks && m_r < kCols)
 #pragma unroll
-        for (int n = 0; n < kMoved; ++n) {
-            const int id = threadIdx.x + kThreads * n;
-            if (kTotal % kThreads == 0 || id < kTotal) {
-                Rows::put(to, id / Rows::kChunks, id % Rows::kChunks, mq[n]);
-                Rows::put(to + kBytes, id / Rows::kChunks, id % Rows::kChunks, md[n]);
+            for (int n = 0; n < kMoved; ++n) {
+                Rows::put(to, m_r + n * kPass, m_c, mq[n]);
+                Rows::put(to + kBytes, m_r + n * kPass, m_c, md[n]);
             }
-        }
         if (threadIdx.x < kCols) {
             lses[buffer][threadIdx.x] = m_lse;
             deltas[buffer][threadIdx.x] = m_delta;
@@ -310,7 +366,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 1) attend_grad_k_kernel(Att
 #pragma unroll
         for (int t = 0; t < 2 * N; ++t) {
             multiply<T>(x, Rows::row(qs, row_at, 0, t), k[t]);
-            multiply<T>(y, Rows::row(dys, row_at, 0, t), v[t]);
+            multiply<T>(y, Rows::row(dys, row_at, 0, t), Rows::row(values, row_at, wave * 32, t));
         }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -373,13 +429,53 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 1) attend_grad_k_kernel(Att
         set_column(dk, Spread{gk.x * up, gk.y * up}, col, lane);
         set_column(dv, Spread{gv.x * up, gv.y * up}, col, lane);
     }
+    const bool none = j >= s.k_length;
+    const float fk = a.scale * kCarried<T>, fv = kCarried<T>;
+    if (!task.whole) {
+        float *p = a.part + ((int64_t)blockIdx.x * 2 * kKeys + wave * 32 + (lane & 31)) * (N * 32);
+        write_row<float, N>(p, dk, fk, none, N * 32, lane);
+        write_row<float, N>(p + kKeys * (N * 32), dv, fv, none, N * 32, lane);
+        return;
+    }
     if (j >= a.keys)
         return;
-    const bool none = j >= s.k_length;
-    write_row<T, N>((T *)s.rows<T>(a.dk, s.kv) + j * a.dk.row, dk, a.scale * kCarried<T>, none,
-                    a.dim, lane);
-    write_row<T, N>((T *)s.rows<T>(a.dv, s.kv) + j * a.dv.row, dv, kCarried<T>, none, a.dim,
-                    lane);
+    write_row<T, N>((T *)s.rows<T>(a.dk, s.kv) + j * a.dk.row, dk, fk, none, a.dim, lane);
+    write_row<T, N>((T *)s.rows<T>(a.dv, s.kv) + j * a.dv.row, dv, fv, none, a.dim, lane);
+}
+
+// Joins the parts of the keys' gradients, in order: four keys a workgroup, four
+// values a thread.
+template <typename T, int N>
+__global__ void __launch_bounds__(64 * kAttendWaves) attend_grad_join_kernel(AttendArgs a)
+{
+    constexpr int kKeys = kAttendWaves * 32, kFours = N * 8, kRows = kAttendJoinKeys;
+    static_assert(kRows * kFours * 2 <= 64 * kAttendWaves, "a thread for each four values");
+    const uint32_t unit = divide(blockIdx.x, a.pair_div);
+    const uint32_t pair = blockIdx.x - unit * a.pair_div.d;
+    const uint32_t tile = unit / (kKeys / kRows), row0 = unit % (kKeys / kRows) * kRows;
+    const Sequence s(a, pair);
+    const KeySpan span(a, s, tile * kKeys, tile * kKeys + kKeys - 1);
+    const bool sink = tile < (uint32_t)a.sink_tiles;
+    const int32_t size = sink ? a.sink_part : a.tile_part;
+    const int32_t parts = (int32_t)(((int64_t)span.end - span.begin + size - 1) / size);
+    // the first part's place among the workgroups' sums
+    const int64_t first = sink ? (int64_t)tile * a.sink_div.d
+                               : (int64_t)a.sink_tiles * a.sink_div.d +
+                                     (int64_t)(tile - a.sink_tiles) * a.tile_div.d;
+    const int matrix = threadIdx.x & 1, at = threadIdx.x >> 1;
+    const int row = row0 + at / kFours, d = at % kFours * 4;
+    const int32_t j = tile * kKeys + row;
+    if (at >= kRows * kFours || j >= a.keys || d >= a.dim)
+        return;
+    const int64_t step = (int64_t)a.pairs * 2 * kKeys * (N * 32);
+    const float *p = a.part + first * step +
+                     (((int64_t)pair * 2 + matrix) * kKeys + row) * (N * 32) + d;
+    f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int32_t k = 0; k < parts; ++k)
+        y += *(const f32x4 *)(p + k * step);
+    const HeadRows &to = matrix ? a.dv : a.dk;
+    store<T, 4>((T *)s.rows<T>(to, s.kv) + j * to.row + d, from_f32<T, 4>(y));
 }
 
 template <typename T>
@@ -391,8 +487,10 @@ int launch_attend_grad(const AttendArgs &a, int kernel, int wide, unsigned grid,
         hipStream_t st = (hipStream_t)s;
         if (kernel == kAttendGradQ)
             hipLaunchKernelGGL((attend_grad_q_kernel<T, N>), g, b, 0, st, a);
-        else
+        else if (kernel == kAttendGradK)
             hipLaunchKernelGGL((attend_grad_k_kernel<T, N>), g, b, 0, st, a);
+        else
+            hipLaunchKernelGGL((attend_grad_join_kernel<T, N>), g, b, 0, st, a);
     };
     if (wide == 1)
         with(std::integral_constant<int, 1>{});

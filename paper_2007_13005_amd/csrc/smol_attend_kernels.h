@@ -221,19 +221,19 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     Columns<T, N> cols;
     cols.start(a, s, mine, lane);
     const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
-    Mover<T, N, kKeys, kThreads> k, v;
+    Mover<T, N, kKeys, kThreads> k(a.dim, threadIdx.x), v(a.dim, threadIdx.x);
     const auto fetch = [&](int32_t n) {
         const int32_t j0 = walk.tile(n) * kKeys;
-        k.fetch(kp, a.k.row, j0, s.k_length, a.dim, threadIdx.x);
-        v.fetch(vp, a.v.row, j0, s.k_length, a.dim, threadIdx.x);
+        k.fetch(kp, a.k.row, j0, s.k_length);
+        v.fetch(vp, a.v.row, j0, s.k_length);
     };
     if (lo < hi)
         fetch(lo);
     const int key_at = KeyRows::row_at(lane), value_at = ValueRows::column_at(lane);
     for (int32_t n = lo; n < hi; ++n) {
         char *keys = lds[(n - lo) & 1], *values = keys + kKeyBytes;
-        k.template put<16>(keys, threadIdx.x);
-        v.template put<sizeof(T) == 2 ? 32 : 16>(values, threadIdx.x);
+        k.template put<16>(keys);
+        v.template put<sizeof(T) == 2 ? 32 : 16>(values);
         // a tile is written again two turns on, behind the next turn's barrier
         __syncthreads();
         if (n + 1 < hi)
@@ -241,14 +241,12 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         const int32_t j0 = walk.tile(n) * kKeys;
         if (!cols.any(a, j0, j0 + kKeys - 1))
             continue;
-        f32x16 x[2];
+        f32x16 x[2] = {(f32x16)0.0f, (f32x16)0.0f};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            x[h] = (f32x16)0.0f;
+        for (int t = 0; t < 2 * N; ++t)
 #pragma unroll
-            for (int t = 0; t < 2 * N; ++t)
+            for (int h = 0; h < 2; ++h)
                 multiply<T>(x[h], KeyRows::row(keys, key_at, 32 * h, t), cols.q[t]);
-        }
         cols.weigh(a, x, j0, lane);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -293,11 +291,11 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
     char *values = lds + wave * kBytes;
     vec<T, 8> k[2 * N];
-    Mover<T, N, kKeys, 64> v;
+    Mover<T, N, kKeys, 64> v(a.dim, lane);
     const auto fetch = [&](int32_t n) {
         const int32_t j0 = walk.tile(n) * kKeys, j = j0 + (lane & 31);
         row_operands<T, N>(kp + (j < s.k_length ? j : s.k_length - 1) * a.k.row, a.dim, lane, k);
-        v.fetch(vp, a.v.row, j0, s.k_length, a.dim, lane);
+        v.fetch(vp, a.v.row, j0, s.k_length);
     };
     const int32_t own = lo + wave;
     if (own < hi)
@@ -310,7 +308,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         for (int t = 0; t < 2 * N; ++t)
             multiply<T>(x[0], k[t], cols.q[t]);
         asm volatile("" ::: "memory");  // the wave's reads of the last tile come first
-        v.template put<sizeof(T) == 2 ? 32 : 16>(values, lane);
+        v.template put<sizeof(T) == 2 ? 32 : 16>(values);
         asm volatile("" ::: "memory");  // other lanes read what this one writes
         if (n + kAttendWaves < hi)
             fetch(n + kAttendWaves);
@@ -373,20 +371,29 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     cols.finish(a, s, c0, task.pair, task.split, lane);
 }
 
-// Joins the parts of the keys, in order: a wave a column.
+// Joins the parts of the keys: a workgroup a column, each wave a quarter of the
+// parts in order (all their loads at once), then the four waves' sums in order.
 template <typename T, int N>
 __global__ void __launch_bounds__(64 * kAttendWaves) attend_join_kernel(AttendArgs a)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t at = (int64_t)blockIdx.x * kAttendWaves +
-                       __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (at >= (int64_t)a.pairs * a.columns)
-        return;
-    const uint32_t pair = (uint32_t)(at / a.columns);
+    constexpr int kParts = kAttendSplits / kAttendWaves;
+    __shared__ Spread quarter[kAttendWaves][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t pair = blockIdx.x / (uint32_t)a.columns;
     const Sequence s(a, pair);
-    const Column c(a, s, (int32_t)(at - (int64_t)pair * a.columns));
+    const Column c(a, s, (int32_t)(blockIdx.x - pair * (uint32_t)a.columns));
     const int64_t rows = (int64_t)a.pairs * a.columns;
-    const float *ml = a.part + (int64_t)a.splits * rows * (N * 32) + 2 * at;
+    const int per = (a.splits + kAttendWaves - 1) / kAttendWaves;
+    const float *p = a.part + (wave * per * rows + blockIdx.x) * (N * 32);
+    Spread x[kParts];
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+        const bool own = k < per && wave * per + k < a.splits;
+        const float *at = p + k * rows * (N * 32);
+        x[k].x = own && lane < N * 32 ? at[lane] : 0.0f;
+        x[k].y = own && lane + 64 < N * 32 ? at[lane + 64] : 0.0f;
+    }
+    const float *ml = a.part + (int64_t)a.splits * rows * (N * 32) + 2 * (int64_t)blockIdx.x;
     const bool own = lane < a.splits;  // splits <= 64
     const float m = own ? ml[2 * lane * rows] : kLowest, l = own ? ml[2 * lane * rows + 1] : 0.0f;
     float top = m;
@@ -396,12 +403,21 @@ __global__ void __launch_bounds__(64 * kAttendWaves) attend_join_kernel(AttendAr
     const float f = exp2_of(m - top);
     const float total = wave_sum(l * f);
     Spread y = {0.0f, 0.0f};
-    for (int k = 0; k < a.splits; ++k) {
-        const float w = __shfl(f, k);
-        const float *p = a.part + (k * rows + at) * (N * 32);
-        y.x = fmaf(w, lane < N * 32 ? p[lane] : 0.0f, y.x);
-        if (N > 2)
-            y.y = fmaf(w, lane + 64 < N * 32 ? p[lane + 64] : 0.0f, y.y);
+#pragma unroll
+    for (int k = 0; k < kParts; ++k)
+        if (k < per) {
+            const float w = __shfl(f, (wave * per + k) & 63);
+            y.x = fmaf(w, x[k].x, y.x);
+            y.y = fmaf(w, x[k].y, y.y);
+        }
+    quarter[wave][lane] = y;
+    __syncthreads();
+    if (wave != 0)
+        return;
+#pragma unroll
+    for (int w = 1; w < kAttendWaves; ++w) {
+        y.x += quarter[w][lane].x;
+        y.y += quarter[w][lane].y;
     }
     const bool none = s.last(a, c.i) < 0;
     const float inv = 1.0f / total;
