@@ -71,65 +71,99 @@ __device__ __forceinline__ float both_halves(float x, F f)
     return f(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
 }
 
-// Rows of N * 32 values in LDS, `Pad` bytes apart. With 16 bytes the rows of a
-// row operand's eight lanes lie in different banks (the stride is an odd number
-// of 16 bytes); with 32 those of four rows by 32 bytes, which a transposing read
-// takes, do.
-template <typename T, int N, int Pad>
+// Rows of N * 32 values in LDS, in chunks of 16 bytes whose places within a row
+// are turned by the row (an exclusive or), so that both kinds of reads spread
+// over the 256 bytes of the banks: a row operand's 16 neighbouring lanes read one
+// chunk of 16 rows; a transposing read takes 64 bytes of four rows, a column read
+// of fp32 128 bytes of two. Rows of a multiple of 256 bytes turn by all four bits
+// of the chunk; others have strides of 64 or 192 bytes past such a multiple and
+// turn by two. (Padding alone, 16 or 32 bytes a row, left a quarter to a half of
+// the LDS cycles to conflicts.) Tiles begin at a multiple of 512 bytes.
+template <typename T, int N>
 struct LdsRows {
-    static constexpr int kStride = N * 32 * (int)sizeof(T) + Pad;
-    static constexpr int kChunks = N * 32 * (int)sizeof(T) / 16;
+    static constexpr int kBytes = N * 32 * (int)sizeof(T);
+    static constexpr int kChunks = kBytes / 16;
     static constexpr int kEach = 16 / (int)sizeof(T);
+    static constexpr bool kFull = kBytes % 256 == 0;
+    static constexpr int kStride = kFull || kBytes % 128 ? kBytes : kBytes + 64;
     typedef vec<T, kEach> Chunk;
 
+    static __device__ __forceinline__ int turn(int row)
+    {
+        return (kFull ? (row & 3) << 2 : 0) | (row >> 2 & 3);
+    }
+    static __device__ __forceinline__ int place(int row, int chunk)
+    {
+        return row * kStride + ((chunk ^ turn(row)) << 4);
+    }
     static __device__ __forceinline__ void put(char *tile, int row, int chunk, Chunk v)
     {
-        *(Chunk *)(tile + row * kStride + chunk * 16) = v;
+        *(Chunk *)(tile + place(row, chunk)) = v;
     }
-    // Row operand: of row lane % 32, values 16 t + 8 (lane / 32) .. + 7.
+    // `bytes` further in a row, a multiple of 64 (full turns: of 32) below its size
+    static __device__ __forceinline__ int along(int at, int bytes)
+    {
+        return kFull ? at ^ bytes : (at ^ (bytes & 32)) + (bytes & ~32);
+    }
+    // Row operand: of row row0 + lane % 32, values 16 t + 8 (lane / 32) .. + 7; row0
+    // a multiple of 32.
     static __device__ __forceinline__ int row_at(int lane)
     {
-        return (lane & 31) * kStride + (lane >> 5) * 8 * (int)sizeof(T);
+        return place(lane & 31, (lane >> 5) * 8 * (int)sizeof(T) / 16);
     }
     static __device__ __forceinline__ vec<T, 8> row(const char *tile, int at, int row0, int t)
     {
-        const char *p = tile + at + row0 * kStride + t * 16 * (int)sizeof(T);
+        const int p = along(at, t * 16 * (int)sizeof(T)) + row0 * kStride;
         if constexpr (sizeof(T) == 2) {
-            return *(const vec<T, 8> *)p;
+            return *(const vec<T, 8> *)(tile + p);
         } else {
-            const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 16);
+            const f32x4 a = *(const f32x4 *)(tile + p), b = *(const f32x4 *)(tile + (p ^ 16));
             return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
     // Column operand: of column 32 n + lane % 32, rows row0 + {0 .. 3, 8 .. 11} +
-    // 4 (lane / 32).
+    // 4 (lane / 32); row0 a multiple of 16.
     static __device__ __forceinline__ int column_at(int lane)
     {
+        const int row = (lane >> 5) * 4;
         if (sizeof(T) == 4)
-            return (lane >> 5) * 4 * kStride + (lane & 31) * 4;
-        return ((lane >> 5) * 4 + ((lane & 15) >> 2)) * kStride +
-               ((lane >> 4 & 1) * 16 + (lane & 3) * 4) * 2;
+            return place(row, (lane & 31) >> 2) + (lane & 3) * 4;
+        return place(row + ((lane & 15) >> 2), (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) +
+               (lane & 1) * 8;
     }
     static __device__ __forceinline__ vec<T, 8> column(const char *tile, int at, int row0, int n)
     {
-        const char *p = tile + at + row0 * kStride + n * 32 * (int)sizeof(T);
+        const int p = along(at, n * 32 * (int)sizeof(T)) + row0 * kStride;
+        // eight rows further the turn's second bit is the other
+        const int q = (p ^ 32) + 8 * kStride;
         if constexpr (sizeof(T) == 2) {
             // 16 lanes give the places of four rows by 16 columns and get a column each
             typedef short s16x4 __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) s16x4 Shared;
-            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)p);
-            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)(p + 8 * kStride));
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)(tile + p));
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)(tile + q));
             return __builtin_bit_cast(vec<T, 8>,
                                       __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             vec<T, 8> v;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                v[e] = *(const float *)(p + (e < 4 ? e : e + 4) * kStride);
+            for (int e = 0; e < 4; ++e) {
+                const int step = kFull ? e << 6 : 0;
+                v[e] = *(const float *)(tile + (p ^ step) + e * kStride);
+                v[e + 4] = *(const float *)(tile + (q ^ step) + e * kStride);
+            }
             return v;
         }
     }
 };
+
+// x as if it were new: what is computed from it is not kept over a loop's turns
+// (a dozen addresses would take the registers of operands).
+__device__ __forceinline__ int fresh(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
 
 // A sequence and one of its key heads.
 struct Sequence {
@@ -222,7 +256,7 @@ __device__ __forceinline__ void row_operands(const T *row, int32_t dim, int lane
 // where strides do not fit 32 bits) rows are looked at one by one.
 template <typename T, int N, int Rows, int Threads>
 struct Mover {
-    typedef LdsRows<T, N, 16> Layout;
+    typedef LdsRows<T, N> Layout;
     typedef typename Layout::Chunk Chunk;
     static constexpr int kSlots = Layout::kChunks == 12 ? 16 : Layout::kChunks == 24 ? 32
                                                                                : Layout::kChunks;
@@ -266,13 +300,12 @@ struct Mover {
                 v[n] = load<T, Layout::kEach>(p + row * stride + c * Layout::kEach);
         }
     }
-    template <int Pad>
     __device__ __forceinline__ void put(char *tile) const
     {
         if (kSlots == Layout::kChunks || c < Layout::kChunks)
 #pragma unroll
             for (int n = 0; n < kCount; ++n)
-                LdsRows<T, N, Pad>::put(tile, r + kPass * n, c, v[n]);
+                Layout::put(tile, r + kPass * n, c, v[n]);
     }
 };
 

@@ -69,9 +69,9 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     attend_grad_q_kernel(AttendArgs a)
 {
     constexpr int kThreads = 64 * kAttendWaves, kKeys = kAttendKeys;
-    typedef LdsRows<T, N, 16> Rows;
+    typedef LdsRows<T, N> Rows;
     constexpr int kBytes = kKeys * Rows::kStride;
-    __shared__ __attribute__((aligned(16))) char lds[2][2 * kBytes];
+    __shared__ __attribute__((aligned(512))) char lds[2][2 * kBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t turn = divide(blockIdx.x, a.pair_div);
     const uint32_t pair = blockIdx.x - turn * a.pair_div.d;
@@ -127,11 +127,11 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     };
     if (walk.count)
         fetch(0);
-    const int row_at = Rows::row_at(lane), column_at = Rows::column_at(lane);
+    const int row_at0 = Rows::row_at(lane), column_at0 = Rows::column_at(lane);
     for (int32_t n = 0; n < walk.count; ++n) {
         char *keys = lds[n & 1], *values = keys + kBytes;
-        k.template put<16>(keys);
-        v.template put<16>(values);
+        k.put(keys);
+        v.put(values);
         __syncthreads();  // a tile is written again two turns on
         if (n + 1 < walk.count)
             fetch(n + 1);
@@ -141,6 +141,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
             const int32_t k0 = j0 + 32 * h, k1 = k0 + 31;
             if (k0 > last_max || (k1 < first_min && k0 >= a.sinks))
                 continue;
+            const int row_at = fresh(row_at0), column_at = fresh(column_at0);
             f32x16 x = (f32x16)0.0f, y = (f32x16)0.0f;
 #pragma unroll
             for (int t = 0; t < 2 * N; ++t) {
@@ -260,11 +261,11 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     attend_grad_k_kernel(AttendArgs a)
 {
     constexpr int kThreads = 64 * kAttendWaves, kCols = 32, kKeys = kAttendWaves * 32;
-    typedef LdsRows<T, N, 16> Rows;
+    typedef LdsRows<T, N> Rows;
     typedef typename Rows::Chunk Chunk;
     constexpr int kBytes = kCols * Rows::kStride;
-    __shared__ __attribute__((aligned(16))) char lds[2][2 * kBytes];
-    __shared__ __attribute__((aligned(16))) char values[kKeys * Rows::kStride];
+    __shared__ __attribute__((aligned(512))) char lds[2][2 * kBytes];
+    __shared__ __attribute__((aligned(512))) char values[kKeys * Rows::kStride];
     __shared__ __attribute__((aligned(16))) float lses[2][kCols], deltas[2][kCols];
     __shared__ __attribute__((aligned(16))) int32_t lasts[2][kCols], firsts[2][kCols];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -292,7 +293,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         row_operands<T, N>(kp + (j < a.keys ? j : a.keys - 1) * a.k.row, a.dim, lane, k);
         Mover<T, N, kKeys, kThreads> v(a.dim, threadIdx.x);
         v.fetch(vp, a.v.row, j0, s.k_length);
-        v.template put<16>(values);
+        v.put(values);
     }
     // what the thread moves: chunk m_c of rows m_r, m_r + kPass, ..., and of the
     // first 32 threads one column's numbers
@@ -346,7 +347,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     };
     if (c_begin < c_end)
         fetch(c_begin);
-    const int row_at = Rows::row_at(lane), column_at = Rows::column_at(lane);
+    const int row_at0 = Rows::row_at(lane), column_at0 = Rows::column_at(lane);
     int buffer = 0;
     for (int32_t c0 = c_begin; c0 < c_end; c0 += kCols, buffer ^= 1) {
         put(buffer);
@@ -362,6 +363,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         const bool whole = c0 + kCols <= c_end && mine1 <= s.last(a, ia) &&
                            (mine >= s.first(a, ib) || mine1 < a.sinks);
         const char *qs = lds[buffer], *dys = qs + kBytes;
+        const int row_at = fresh(row_at0), column_at = fresh(column_at0);
         f32x16 x = (f32x16)0.0f, y = (f32x16)0.0f;
 #pragma unroll
         for (int t = 0; t < 2 * N; ++t) {

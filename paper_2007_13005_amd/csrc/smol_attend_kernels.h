@@ -206,10 +206,9 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     attend_kernel(AttendArgs a)
 {
     constexpr int kThreads = 64 * kAttendWaves, kKeys = kAttendKeys;
-    typedef LdsRows<T, N, 16> KeyRows;
-    typedef LdsRows<T, N, sizeof(T) == 2 ? 32 : 16> ValueRows;
-    constexpr int kKeyBytes = kKeys * KeyRows::kStride, kValueBytes = kKeys * ValueRows::kStride;
-    __shared__ __attribute__((aligned(16))) char lds[2][kKeyBytes + kValueBytes];
+    typedef LdsRows<T, N> Rows;
+    constexpr int kBytes = kKeys * Rows::kStride;
+    __shared__ __attribute__((aligned(512))) char lds[2][2 * kBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Task task(a);
     const Sequence s(a, task.pair);
@@ -229,11 +228,11 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     };
     if (lo < hi)
         fetch(lo);
-    const int key_at = KeyRows::row_at(lane), value_at = ValueRows::column_at(lane);
+    const int key_at0 = Rows::row_at(lane), value_at0 = Rows::column_at(lane);
     for (int32_t n = lo; n < hi; ++n) {
-        char *keys = lds[(n - lo) & 1], *values = keys + kKeyBytes;
-        k.template put<16>(keys);
-        v.template put<sizeof(T) == 2 ? 32 : 16>(values);
+        char *keys = lds[(n - lo) & 1], *values = keys + kBytes;
+        k.put(keys);
+        v.put(values);
         // a tile is written again two turns on, behind the next turn's barrier
         __syncthreads();
         if (n + 1 < hi)
@@ -241,19 +240,20 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         const int32_t j0 = walk.tile(n) * kKeys;
         if (!cols.any(a, j0, j0 + kKeys - 1))
             continue;
+        const int key_at = fresh(key_at0), value_at = fresh(value_at0);
         f32x16 x[2] = {(f32x16)0.0f, (f32x16)0.0f};
 #pragma unroll
         for (int t = 0; t < 2 * N; ++t)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                multiply<T>(x[h], KeyRows::row(keys, key_at, 32 * h, t), cols.q[t]);
+                multiply<T>(x[h], Rows::row(keys, key_at, 32 * h, t), cols.q[t]);
         cols.weigh(a, x, j0, lane);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const vec<T, 8> w = operand<T>(x[g >> 1], g & 1);
 #pragma unroll
             for (int n2 = 0; n2 < N; ++n2)
-                multiply<T>(cols.sum[n2], ValueRows::column(values, value_at, 16 * g, n2), w);
+                multiply<T>(cols.sum[n2], Rows::column(values, value_at, 16 * g, n2), w);
         }
     }
     cols.mend(a, s, mine, lane, [&](int32_t n, int32_t *j0, int32_t *j1) {
@@ -273,10 +273,10 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     attend_few_kernel(AttendArgs a)
 {
     constexpr int kKeys = kAttendFewKeys;
-    typedef LdsRows<T, N, sizeof(T) == 2 ? 32 : 16> ValueRows;
-    constexpr int kBytes = kKeys * ValueRows::kStride;
+    typedef LdsRows<T, N> Rows;
+    constexpr int kBytes = kKeys * Rows::kStride;
     static_assert(kAttendWaves * kBytes >= 2 * 64 * N * 16 * 4, "room for two waves' sums");
-    __shared__ __attribute__((aligned(16))) char lds[kAttendWaves * kBytes];
+    __shared__ __attribute__((aligned(512))) char lds[kAttendWaves * kBytes];
     __shared__ float tops[kAttendWaves][32], sums[kAttendWaves][32];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Task task(a);
@@ -300,15 +300,16 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     const int32_t own = lo + wave;
     if (own < hi)
         fetch(own);
-    const int value_at = ValueRows::column_at(lane);
+    const int value_at0 = Rows::column_at(lane);
     for (int32_t n = own; n < hi; n += kAttendWaves) {
         const int32_t j0 = walk.tile(n) * kKeys;
+        const int value_at = fresh(value_at0);
         f32x16 x[1] = {(f32x16)0.0f};
 #pragma unroll
         for (int t = 0; t < 2 * N; ++t)
             multiply<T>(x[0], k[t], cols.q[t]);
         asm volatile("" ::: "memory");  // the wave's reads of the last tile come first
-        v.template put<sizeof(T) == 2 ? 32 : 16>(values);
+        v.put(values);
         asm volatile("" ::: "memory");  // other lanes read what this one writes
         if (n + kAttendWaves < hi)
             fetch(n + kAttendWaves);
@@ -318,7 +319,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
             const vec<T, 8> w = operand<T>(x[0], g);
 #pragma unroll
             for (int n2 = 0; n2 < N; ++n2)
-                multiply<T>(cols.sum[n2], ValueRows::column(values, value_at, 16 * g, n2), w);
+                multiply<T>(cols.sum[n2], Rows::column(values, value_at, 16 * g, n2), w);
         }
     }
     cols.mend(a, s, c0, lane, [&](int32_t n, int32_t *j0, int32_t *j1) {
