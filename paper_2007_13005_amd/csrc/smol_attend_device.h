@@ -113,7 +113,8 @@ struct LdsRows {
     }
     static __device__ __forceinline__ vec<T, 8> row(const char *tile, int at, int row0, int t)
     {
-        const int p = along(at, t * 16 * (int)sizeof(T)) + row0 * kStride;
+        const int p = along(at, t * 16 * (int)sizeof(T));
+        tile += row0 * kStride;
         if constexpr (sizeof(T) == 2) {
             return *(const vec<T, 8> *)(tile + p);
         } else {
@@ -133,15 +134,17 @@ struct LdsRows {
     }
     static __device__ __forceinline__ vec<T, 8> column(const char *tile, int at, int row0, int n)
     {
-        const int p = along(at, n * 32 * (int)sizeof(T)) + row0 * kStride;
+        const int p = along(at, n * 32 * (int)sizeof(T));
         // eight rows further the turn's second bit is the other
-        const int q = (p ^ 32) + 8 * kStride;
+        const int q = p ^ 32;
+        tile += row0 * kStride;
+        const char *further = tile + 8 * kStride;
         if constexpr (sizeof(T) == 2) {
             // 16 lanes give the places of four rows by 16 columns and get a column each
             typedef short s16x4 __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) s16x4 Shared;
             const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)(tile + p));
-            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)(tile + q));
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)(further + q));
             return __builtin_bit_cast(vec<T, 8>,
                                       __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
@@ -149,8 +152,8 @@ struct LdsRows {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int step = kFull ? e << 6 : 0;
-                v[e] = *(const float *)(tile + (p ^ step) + e * kStride);
-                v[e + 4] = *(const float *)(tile + (q ^ step) + e * kStride);
+                v[e] = *(const float *)(tile + e * kStride + (p ^ step));
+                v[e + 4] = *(const float *)(further + e * kStride + (q ^ step));
             }
             return v;
         }
@@ -160,6 +163,16 @@ struct LdsRows {
 // x as if it were new: what is computed from it is not kept over a loop's turns
 // (a dozen addresses would take the registers of operands).
 __device__ __forceinline__ int fresh(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// Nothing moves past this: the compiler keeps the order that is written.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// x is formed here and not where it is first used.
+__device__ __forceinline__ float here(float x)
 {
     asm volatile("" : "+v"(x));
     return x;

@@ -3,9 +3,9 @@
 //
 // One pass over the keys with the running maximum m and sum l of a softmax in
 // base 2: weights 2^(s - m) are rounded to the type and multiplied with the
-// values in fp32; a maximum that grows scales what was summed before. m may
-// stay up to 8 behind the maximum (weights up to 256, exact in any type's
-// exponent), so most tiles scale nothing.
+// values in fp32; a maximum that grows scales what was summed before. m is a
+// whole number and may stay up to 8 behind the maximum (weights up to 256), so
+// most tiles scale nothing, and scaling rounds nothing.
 //
 // What a query does not see takes no part: its score is set to minus infinity
 // before the maximum. A weight of 0 times a NaN or an infinity among the values
@@ -59,42 +59,44 @@ struct Columns {
     {
         return j1 <= last_min && (j0 >= first_max || j1 < a.sinks);
     }
-    // Scores x of keys j0 + 32 k (register rows) to weights, and the state.
-    template <int K>
-    __device__ __forceinline__ void weigh(const AttendArgs &a, f32x16 (&x)[K], int32_t j0, int lane)
+    // Scores x of 32 keys from j0 on (register rows): what is not seen leaves, and
+    // the maximum follows. True (and f) where what was summed, and weights formed
+    // before, are to be scaled by f. The maximum is kept as a whole number, so f is a
+    // power of two and scaling rounds nothing.
+    __device__ __forceinline__ bool look(const AttendArgs &a, f32x16 &x, int32_t j0, int lane,
+                                         float *f)
     {
-        if (!all(a, j0, j0 + 32 * K - 1))
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int32_t j = j0 + 32 * k + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
-                    x[k][e] = sees(j, last, first, a.sinks) ? x[k][e] : -INFINITY;
-                }
-        float top = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                top = fmaxf(top, x[k][e]);
-        top = both_halves(top, [](float u, float v) { return fmaxf(u, v); }) * a.scale_log2;
-        if (__any(top > m + kBehind)) {
-            const float to = fmaxf(m, top), f = exp2_of(m - to);
-            m = to;
-            l *= f;
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-                sum[n] *= f;
-        }
-        float add = 0.0f;
-#pragma unroll
-        for (int k = 0; k < K; ++k)
+        if (!all(a, j0, j0 + 31))
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                x[k][e] = exp2_of(fmaf(x[k][e], a.scale_log2, -m));
-                add += x[k][e];
+                const int32_t j = j0 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+                x[e] = sees(j, last, first, a.sinks) ? x[e] : -INFINITY;
             }
-        l += add;
+        float top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            top = fmaxf(top, x[e]);
+        top = both_halves(top, [](float u, float v) { return fmaxf(u, v); }) * a.scale_log2;
+        if (!__any(top > m + kBehind))
+            return false;
+        const float to = fmaxf(m, ceilf(top));
+        *f = exp2_of(m - to);
+        m = to;
+        l *= *f;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            sum[n] *= *f;
+        return true;
+    }
+    // Weights of elements from .. to - 1.
+    __device__ __forceinline__ void weigh(const AttendArgs &a, f32x16 &x, int from, int to)
+    {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (e >= from && e < to) {
+                x[e] = here(exp2_of(fmaf(x[e], a.scale_log2, -m)));
+                l += x[e];
+            }
     }
     // Columns whose sums alone are not finite, again: over keys j0 .. j1 of each
     // tile that next gives (false: none left), what the column sees.
@@ -240,20 +242,62 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         const int32_t j0 = walk.tile(n) * kKeys;
         if (!cols.any(a, j0, j0 + kKeys - 1))
             continue;
-        const int key_at = fresh(key_at0), value_at = fresh(value_at0);
+        const int key_at = fresh(key_at0 + (n - lo & 1) * (2 * kBytes));
+        const int value_at = fresh(value_at0 + (n - lo & 1) * (2 * kBytes) + kBytes);
+        // operands in the order of their products, kAhead read before they are used:
+        // scores of the first 32 keys, of the second, values with the first 32 keys'
+        // weights, with the second's
+        constexpr int kAhead = 4, kHalf = 2 * N;
+        vec<T, 8> ahead[kAhead];
+        const auto read = [&](int k) {
+            if (k < 2 * kHalf)
+                ahead[k % kAhead] = Rows::row(lds[0], key_at, k / kHalf * 32, k % kHalf);
+            else if (k < 4 * kHalf)
+                ahead[k % kAhead] =
+                    Rows::column(lds[0], value_at, (k - 2 * kHalf) / N * 16, (k - 2 * kHalf) % N);
+        };
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            read(k);
+        in_order();
         f32x16 x[2] = {(f32x16)0.0f, (f32x16)0.0f};
+        vec<T, 8> w[4];
+        float f;
 #pragma unroll
-        for (int t = 0; t < 2 * N; ++t)
+        for (int k = 0; k < kHalf; ++k) {
+            multiply<T>(x[0], ahead[k % kAhead], cols.q[k]);
+            read(k + kAhead);
+            in_order();
+        }
+        cols.look(a, x[0], j0, lane, &f);
+        // from here on products and exponentials take turns, so that both units work
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                multiply<T>(x[h], Rows::row(keys, key_at, 32 * h, t), cols.q[t]);
-        cols.weigh(a, x, j0, lane);
+        for (int k = 0; k < kHalf; ++k) {
+            multiply<T>(x[1], ahead[(kHalf + k) % kAhead], cols.q[k]);
+            read(kHalf + k + kAhead);
+            cols.weigh(a, x[0], 16 * k / kHalf, 16 * (k + 1) / kHalf);
+            in_order();
+        }
+        w[0] = operand<T>(x[0], 0);
+        w[1] = operand<T>(x[0], 1);
+        if (cols.look(a, x[1], j0 + 32, lane, &f)) {
+            w[0] = from_f32<T, 8>(to_f32<8, T>(w[0]) * f);
+            w[1] = from_f32<T, 8>(to_f32<8, T>(w[1]) * f);
+        }
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const vec<T, 8> w = operand<T>(x[g >> 1], g & 1);
+        for (int k = 0; k < kHalf; ++k) {
+            multiply<T>(cols.sum[k % N], ahead[(2 * kHalf + k) % kAhead], w[k / N]);
+            read(2 * kHalf + k + kAhead);
+            cols.weigh(a, x[1], 16 * k / kHalf, 16 * (k + 1) / kHalf);
+            in_order();
+        }
+        w[2] = operand<T>(x[1], 0);
+        w[3] = operand<T>(x[1], 1);
 #pragma unroll
-            for (int n2 = 0; n2 < N; ++n2)
-                multiply<T>(cols.sum[n2], Rows::column(values, value_at, 16 * g, n2), w);
+        for (int k = 0; k < kHalf; ++k) {
+            multiply<T>(cols.sum[k % N], ahead[(3 * kHalf + k) % kAhead], w[2 + k / N]);
+            read(3 * kHalf + k + kAhead);
+            in_order();
         }
     }
     cols.mend(a, s, mine, lane, [&](int32_t n, int32_t *j0, int32_t *j1) {
@@ -313,7 +357,9 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         asm volatile("" ::: "memory");  // other lanes read what this one writes
         if (n + kAttendWaves < hi)
             fetch(n + kAttendWaves);
-        cols.weigh(a, x, j0, lane);
+        float f;
+        cols.look(a, x[0], j0, lane, &f);
+        cols.weigh(a, x[0], 0, 16);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             const vec<T, 8> w = operand<T>(x[0], g);

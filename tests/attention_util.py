@@ -164,7 +164,9 @@ def attend(q, k, v, scale=None, causal=True, window=0, sinks=0, q_lengths=None, 
             total = e + count * U32  # of the sum of weights
             rel = (e + total + unit + (count + 4) * U32)[:, None]
             out[n, :, a] = p @ vv
-            eout[n, :, a] = (p @ vv.abs()) * rel + (see.double() @ vv.abs()) * STEP[dtype]
+            # (weights are relative to a maximum rounded up to a power of two: their sum is
+            # a half at least, so a step of a weight is two of the quotient)
+            eout[n, :, a] = (p @ vv.abs()) * rel + (see.double() @ vv.abs()) * 2 * STEP[dtype]
             lse[n, :, a] = torch.where(some, z, -math.inf)
             else_[n, :, a] = total + 4 * U32 * (top.abs() + z.abs() + 1)
     return (out, eout), (lse, else_)
