@@ -29,6 +29,7 @@ struct AttendArgs {
     int32_t columns;       // queries * group: pairs of a query and one of a key head's heads
     int32_t window, sinks; // window 0: none
     int32_t causal;
+    int32_t direct_keys, direct_rows;  // k and v, q and dout go to LDS without registers
     int32_t tiles;         // of the columns
     int32_t pairs;         // batch * kv_heads
     int32_t splits;

@@ -71,39 +71,52 @@ __device__ __forceinline__ float both_halves(float x, F f)
     return f(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
 }
 
-// Rows of N * 32 values in LDS, in chunks of 16 bytes whose places within a row
-// are turned by the row (an exclusive or), so that both kinds of reads spread
-// over the 256 bytes of the banks: a row operand's 16 neighbouring lanes read one
-// chunk of 16 rows; a transposing read takes 64 bytes of four rows, a column read
-// of fp32 128 bytes of two. Rows of a multiple of 256 bytes turn by all four bits
-// of the chunk; others have strides of 64 or 192 bytes past such a multiple and
-// turn by two. (Padding alone, 16 or 32 bytes a row, left a quarter to a half of
-// the LDS cycles to conflicts.) Tiles begin at a multiple of 512 bytes.
+// x as if it were new: what is computed from it is not kept over a loop's turns
+// (a dozen addresses would take the registers of operands).
+__device__ __forceinline__ int fresh(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// Nothing moves past this: the compiler keeps the order that is written.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// x is formed here and not where it is first used.
+__device__ __forceinline__ float here(float x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// Rows of N * 32 values in LDS, one after the other, in chunks of 16 bytes whose
+// places within a row are turned by the row (an exclusive or), so that both kinds
+// of reads spread over the 256 bytes of the banks: a row operand's 16 neighbouring
+// lanes read one chunk of 16 rows; a transposing read takes 64 bytes of four rows.
+// (Padding alone, 16 or 32 bytes a row, left a quarter to a half of the LDS cycles
+// to conflicts.) Tiles begin at a multiple of 512 bytes.
 template <typename T, int N>
 struct LdsRows {
-    static constexpr int kBytes = N * 32 * (int)sizeof(T);
-    static constexpr int kChunks = kBytes / 16;
+    static constexpr int kStride = N * 32 * (int)sizeof(T);
+    static constexpr int kChunks = kStride / 16;
     static constexpr int kEach = 16 / (int)sizeof(T);
-    static constexpr bool kFull = kBytes % 256 == 0;
-    static constexpr int kStride = kFull || kBytes % 128 ? kBytes : kBytes + 64;
+    // the bytes within a row that turn: all of 256, of half a bank line, of 64
+    static constexpr int kTurned = kStride % 256 == 0 ? 0xf0 : kStride % 128 == 0 ? 0x70 : 0x30;
     typedef vec<T, kEach> Chunk;
 
     static __device__ __forceinline__ int turn(int row)
     {
-        return (kFull ? (row & 3) << 2 : 0) | (row >> 2 & 3);
+        const int high = kTurned == 0xf0 ? (row & 3) << 2 : kTurned == 0x70 ? (row & 2) << 1 : 0;
+        return high | (row >> 2 & 3);
     }
     static __device__ __forceinline__ int place(int row, int chunk)
     {
         return row * kStride + ((chunk ^ turn(row)) << 4);
     }
-    static __device__ __forceinline__ void put(char *tile, int row, int chunk, Chunk v)
-    {
-        *(Chunk *)(tile + place(row, chunk)) = v;
-    }
-    // `bytes` further in a row, a multiple of 64 (full turns: of 32) below its size
+    // `bytes` further in a row
     static __device__ __forceinline__ int along(int at, int bytes)
     {
-        return kFull ? at ^ bytes : (at ^ (bytes & 32)) + (bytes & ~32);
+        return (at ^ (bytes & kTurned)) + (bytes & ~kTurned);
     }
     // Row operand: of row row0 + lane % 32, values 16 t + 8 (lane / 32) .. + 7; row0
     // a multiple of 32.
@@ -151,7 +164,7 @@ struct LdsRows {
             vec<T, 8> v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int step = kFull ? e << 6 : 0;
+                const int step = turn(e) << 4;  // e < 4
                 v[e] = *(const float *)(tile + e * kStride + (p ^ step));
                 v[e + 4] = *(const float *)(further + e * kStride + (q ^ step));
             }
@@ -159,24 +172,6 @@ struct LdsRows {
         }
     }
 };
-
-// x as if it were new: what is computed from it is not kept over a loop's turns
-// (a dozen addresses would take the registers of operands).
-__device__ __forceinline__ int fresh(int x)
-{
-    asm volatile("" : "+v"(x));
-    return x;
-}
-
-// Nothing moves past this: the compiler keeps the order that is written.
-__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
-
-// x is formed here and not where it is first used.
-__device__ __forceinline__ float here(float x)
-{
-    asm volatile("" : "+v"(x));
-    return x;
-}
 
 // A sequence and one of its key heads.
 struct Sequence {
@@ -263,64 +258,70 @@ __device__ __forceinline__ void row_operands(const T *row, int32_t dim, int lane
     }
 }
 
-// Chunks of a tile's rows that one of `Threads` threads moves to LDS: chunk c of
-// rows r, r + kPass, .... Where the tile's rows all exist a chunk's address is a
-// base that the wave shares and 32 bits of the lane's own; past the last row (and
-// where strides do not fit 32 bits) rows are looked at one by one.
-template <typename T, int N, int Rows, int Threads>
-struct Mover {
+// Moves one chunk a lane from base + offset to `to` + 16 * lane in LDS, without
+// registers between; zeros where offset is kNoChunk. Complete once loads_done says
+// so (the compiler does not count these loads).
+constexpr uint32_t kNoChunk = ~15u;
+__device__ __forceinline__ void load_to_lds(const void *base, uint32_t offset, const char *to)
+{
+    typedef __attribute__((address_space(3))) void Shared;
+    // a raw buffer of 2^31 bytes: what lies past it reads as zero
+    const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x80000000u, 0x00027000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (Shared *)to, 16, offset, 0, 0, 0);
+}
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// A tile of rows on its way to LDS, by `Waves` waves. place(row, &from) gives where
+// a row stands, in elements from p, or false for none: zeros, as past the head.
+// direct: everything is aligned to 16 bytes and rows lie within 2^31 bytes of p;
+// else they go through registers, and the wave waits.
+template <typename T, int N, int Rows, int Waves, typename Place>
+__device__ __forceinline__ void move_tile(const T *p, bool direct, int32_t dim, char *tile,
+                                          int wave, int lane, Place place)
+{
     typedef LdsRows<T, N> Layout;
-    typedef typename Layout::Chunk Chunk;
-    static constexpr int kSlots = Layout::kChunks == 12 ? 16 : Layout::kChunks == 24 ? 32
-                                                                               : Layout::kChunks;
-    static constexpr int kPass = Threads / kSlots, kCount = Rows / kPass;
-    static_assert(kPass * kSlots == Threads && kCount * kPass == Rows, "whole passes");
-    Chunk v[kCount];
-    int32_t r, c;
-    bool some;  // the lane's chunk is within the head; else it stays zeros
-    __device__ __forceinline__ Mover(int32_t dim, int thread)
-    {
-        r = thread / kSlots;
-        c = thread % kSlots;
-        some = c * Layout::kEach < dim;
+    constexpr int kTotal = Rows * Layout::kChunks, kIssues = (kTotal + 64 * Waves - 1) /
+                                                             (64 * Waves);
+    static_assert(kTotal % 64 == 0, "whole waves");
+    lane = fresh(lane);
+    const auto each = [&](auto move) {
 #pragma unroll
-        for (int n = 0; n < kCount; ++n)
-            v[n] = (Chunk)(T)0.0f;
-    }
-    // Whether kPass rows' offsets fit 32 bits.
-    static __device__ __forceinline__ bool near(int64_t stride)
-    {
-        return stride < ((int64_t)1 << 31) / (kPass * (int)sizeof(T));
-    }
-    // Rows row0 .. of `rows` (>= 1), zeros past them.
-    __device__ __forceinline__ void fetch(const T *p, int64_t stride, int32_t row0, int32_t rows)
-    {
-        if (near(stride) && row0 + Rows <= rows) {
-            const char *base = (const char *)(p + row0 * stride);
-            const uint32_t at = (uint32_t)(r * (int32_t)stride + c * Layout::kEach) * sizeof(T);
+        for (int n = 0; n < kIssues; ++n) {
+            const int first = (n * Waves + wave) * 64, id = first + lane;
+            if (kTotal % (64 * Waves) && first >= kTotal)
+                break;
+            const int row = id / Layout::kChunks;
+            const int at = ((id % Layout::kChunks) ^ Layout::turn(row)) * Layout::kEach;
+            int64_t from;
+            const bool some = place(row, &from) && at < dim;
+            move(tile + first * 16, some, from + at);
+        }
+    };
+    if (direct)
+        each([&](char *to, bool some, int64_t from) {
+            load_to_lds(p, some ? (uint32_t)from * (uint32_t)sizeof(T) : kNoChunk, to);
+        });
+    else
+        each([&](char *to, bool some, int64_t from) {
+            typename Layout::Chunk v = (typename Layout::Chunk)(T)0.0f;
             if (some)
-#pragma unroll
-                for (int n = 0; n < kCount; ++n)
-                    v[n] = load<T, Layout::kEach>(
-                        (const T *)(base + n * kPass * stride * (int)sizeof(T) + at));
-            return;
-        }
-#pragma unroll
-        for (int n = 0; n < kCount; ++n) {
-            const int32_t row = row0 + r + kPass * n;
-            v[n] = (Chunk)(T)0.0f;
-            if (some && row < rows)
-                v[n] = load<T, Layout::kEach>(p + row * stride + c * Layout::kEach);
-        }
-    }
-    __device__ __forceinline__ void put(char *tile) const
-    {
-        if (kSlots == Layout::kChunks || c < Layout::kChunks)
-#pragma unroll
-            for (int n = 0; n < kCount; ++n)
-                Layout::put(tile, r + kPass * n, c, v[n]);
-    }
-};
+                v = load<T, Layout::kEach>(p + from);
+            *(typename Layout::Chunk *)(to + lane * 16) = v;
+        });
+}
+
+// Rows row0 .. of `rows` rows of keys or values.
+template <typename T, int N, int Rows, int Waves>
+__device__ __forceinline__ void move_rows(const T *p, int64_t stride, bool direct, int32_t dim,
+                                          char *tile, int wave, int lane, int32_t row0,
+                                          int32_t rows)
+{
+    move_tile<T, N, Rows, Waves>(p + row0 * stride, direct, dim, tile, wave, lane,
+                                 [&](int32_t row, int64_t *from) {
+                                     *from = row * stride;
+                                     return row0 + row < rows;
+                                 });
+}
 
 // Whether any of a result's N tiles has a value that is not finite.
 template <int N>

@@ -14,8 +14,9 @@
 // both are carried times 2^6 (a weight of 2^-20 is then still a normal number);
 // d past 2^10 overflows, and its row is summed again as below.
 //
-// What a query does not see has p and d zero, by selection. Sums that are not
-// finite in the end are formed again over what is seen alone (smol_attend_kernels.h).
+// What a query does not see has a score of minus infinity, so p and d are zero.
+// Where it holds a NaN or an infinity they may not be: sums that are not finite in
+// the end are formed again over what is seen alone (as in smol_attend_kernels.h).
 #ifndef SMOL_ATTEND_GRAD_KERNELS_H
 #define SMOL_ATTEND_GRAD_KERNELS_H
 
@@ -68,7 +69,7 @@ template <typename T, int N>
 __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     attend_grad_q_kernel(AttendArgs a)
 {
-    constexpr int kThreads = 64 * kAttendWaves, kKeys = kAttendKeys;
+    constexpr int kKeys = kAttendKeys;
     typedef LdsRows<T, N> Rows;
     constexpr int kBytes = kKeys * Rows::kStride;
     __shared__ __attribute__((aligned(512))) char lds[2][2 * kBytes];
@@ -111,7 +112,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         }
         delta = both_halves(delta, [](float u, float v) { return u + v; });
     }
-    const float lse2 = last < 0 ? 0.0f : a.lse[at] * kLog2e;
+    const float lse2 = last < 0 ? 0.0f : a.lse[at] * kLog2e, minus_lse = kCarry<T> - lse2;
     if (c.exists && lane < 32)
         a.delta[at] = delta;
     f32x16 sum[N];
@@ -119,53 +120,86 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     for (int n = 0; n < N; ++n)
         sum[n] = (f32x16)0.0f;
     const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
-    Mover<T, N, kKeys, kThreads> k(a.dim, threadIdx.x), v(a.dim, threadIdx.x);
     const auto fetch = [&](int32_t n) {
         const int32_t j0 = walk.tile(n) * kKeys;
-        k.fetch(kp, a.k.row, j0, s.k_length);
-        v.fetch(vp, a.v.row, j0, s.k_length);
+        char *to = lds[n & 1];
+        move_rows<T, N, kKeys, kAttendWaves>(kp, a.k.row, a.direct_keys, a.dim, to, wave, lane,
+                                             j0, s.k_length);
+        move_rows<T, N, kKeys, kAttendWaves>(vp, a.v.row, a.direct_keys, a.dim, to + kBytes, wave,
+                                             lane, j0, s.k_length);
     };
     if (walk.count)
         fetch(0);
     const int row_at0 = Rows::row_at(lane), column_at0 = Rows::column_at(lane);
     for (int32_t n = 0; n < walk.count; ++n) {
-        char *keys = lds[n & 1], *values = keys + kBytes;
-        k.put(keys);
-        v.put(values);
-        __syncthreads();  // a tile is written again two turns on
+        // tile n is there, for all waves; the other buffer's tile has been used by all
+        loads_done();
+        __syncthreads();
         if (n + 1 < walk.count)
             fetch(n + 1);
         const int32_t j0 = walk.tile(n) * kKeys;
+        if (j0 > last_max || (j0 + kKeys - 1 < first_min && j0 >= a.sinks))
+            continue;
+        const int at_keys = (n & 1) * (2 * kBytes);
+        const int row_at = fresh(row_at0 + at_keys), column_at = fresh(column_at0 + at_keys);
+        // operands in the order of their products, kAhead read before they are used;
+        // of each 32 keys: scores, grad_out v^T, then (after the second 32 keys') d k
+        constexpr int kAhead = 4, kHalf = 2 * N;
+        vec<T, 8> ahead[kAhead];
+        const auto read = [&](int k) {
+            const int part = k / kHalf, t = k % kHalf;
+            if (part < 4)
+                ahead[k % kAhead] =
+                    Rows::row(lds[0] + (part & 1) * kBytes, row_at, (part >> 1) * 32, t);
+            else if (part < 6)
+                ahead[k % kAhead] =
+                    Rows::column(lds[0], column_at, (part - 4) * 32 + t / N * 16, t % N);
+        };
+        // scores start from minus infinity where a key is not seen, which leaves
+        // weights of zero
+        f32x16 x[2] = {(f32x16)0.0f, (f32x16)0.0f}, y[2] = {(f32x16)0.0f, (f32x16)0.0f};
+        vec<T, 8> d[4];
+        if (!(j0 + kKeys - 1 <= last_min && (j0 >= first_max || j0 + kKeys - 1 < a.sinks)))
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int32_t k0 = j0 + 32 * h, k1 = k0 + 31;
-            if (k0 > last_max || (k1 < first_min && k0 >= a.sinks))
-                continue;
-            const int row_at = fresh(row_at0), column_at = fresh(column_at0);
-            f32x16 x = (f32x16)0.0f, y = (f32x16)0.0f;
-#pragma unroll
-            for (int t = 0; t < 2 * N; ++t) {
-                multiply<T>(x, Rows::row(keys, row_at, 32 * h, t), q[t]);
-                multiply<T>(y, Rows::row(values, row_at, 32 * h, t), dy[t]);
+            for (int e = 0; e < 32; ++e) {
+                const int32_t j = j0 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+                x[e >> 4][e & 15] = sees(j, last, first, a.sinks) ? 0.0f : -INFINITY;
             }
-            const bool whole = k1 <= last_min && (k0 >= first_max || k1 < a.sinks);
+        const auto weigh = [&](int h, int k) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float p = exp2_of(fmaf(x[e], a.scale_log2, kCarry<T> - lse2));
-                x[e] = p * (y[e] - delta);
+            for (int e = 16 * k / kHalf; e < 16 * (k + 1) / kHalf; ++e)
+                x[h][e] = here(exp2_of(fmaf(x[h][e], a.scale_log2, minus_lse)));
+        };
+        const auto differ = [&](int h, int k) {
+#pragma unroll
+            for (int e = 16 * k / kHalf; e < 16 * (k + 1) / kHalf; ++e)
+                x[h][e] = here(x[h][e] * (y[h][e] - delta));
+        };
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            read(k);
+        in_order();
+#pragma unroll
+        for (int part = 0; part < 6; ++part) {
+#pragma unroll
+            for (int k = 0; k < kHalf; ++k) {
+                const vec<T, 8> next = ahead[(part * kHalf + k) % kAhead];
+                if (part == 0 || part == 2)
+                    multiply<T>(x[part >> 1], next, q[k]);
+                else if (part < 4)
+                    multiply<T>(y[part >> 1], next, dy[k]);
+                else
+                    multiply<T>(sum[k % N], next, d[2 * (part - 4) + k / N]);
+                read(part * kHalf + k + kAhead);
+                if (part == 1 || part == 3)
+                    weigh(part >> 1, k);
+                else if (part == 2 || part == 4)
+                    differ((part >> 1) - 1, k);
+                in_order();
             }
-            if (!whole)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int32_t j = k0 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
-                    x[e] = sees(j, last, first, a.sinks) ? x[e] : 0.0f;
-                }
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const vec<T, 8> w = operand<T>(x, g);
-#pragma unroll
-                for (int n2 = 0; n2 < N; ++n2)
-                    multiply<T>(sum[n2], Rows::column(keys, column_at, 32 * h + 16 * g, n2), w);
+            if (part == 2 || part == 4) {
+                d[part - 2] = operand<T>(x[(part >> 1) - 1], 0);
+                d[part - 1] = operand<T>(x[(part >> 1) - 1], 1);
             }
         }
     }
@@ -260,9 +294,8 @@ template <typename T, int N>
 __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     attend_grad_k_kernel(AttendArgs a)
 {
-    constexpr int kThreads = 64 * kAttendWaves, kCols = 32, kKeys = kAttendWaves * 32;
+    constexpr int kCols = 32, kKeys = kAttendWaves * 32;
     typedef LdsRows<T, N> Rows;
-    typedef typename Rows::Chunk Chunk;
     constexpr int kBytes = kCols * Rows::kStride;
     __shared__ __attribute__((aligned(512))) char lds[2][2 * kBytes];
     __shared__ __attribute__((aligned(512))) char values[kKeys * Rows::kStride];
@@ -288,72 +321,59 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     for (int n = 0; n < N; ++n)
         dk[n] = dv[n] = (f32x16)0.0f;
     const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
-    vec<T, 8> k[2 * N];
+    vec<T, 8> k_rows[2 * N];
     if (c_begin < c_end) {
-        row_operands<T, N>(kp + (j < a.keys ? j : a.keys - 1) * a.k.row, a.dim, lane, k);
-        Mover<T, N, kKeys, kThreads> v(a.dim, threadIdx.x);
-        v.fetch(vp, a.v.row, j0, s.k_length);
-        v.put(values);
+        row_operands<T, N>(kp + (j < a.keys ? j : a.keys - 1) * a.k.row, a.dim, lane,
+                           k_rows);
+        move_rows<T, N, kKeys, kAttendWaves>(vp, a.v.row, a.direct_keys, a.dim, values, wave, lane,
+                                             j0, s.k_length);
     }
-    // what the thread moves: chunk m_c of rows m_r, m_r + kPass, ..., and of the
-    // first 32 threads one column's numbers
-    constexpr int kSlots = Mover<T, N, kKeys, kThreads>::kSlots, kPass = kThreads / kSlots;
-    constexpr int kMoved = kPass < kCols ? kCols / kPass : 1;
-    const int m_r = threadIdx.x / kSlots, m_c = threadIdx.x % kSlots;
-    const bool m_some = m_c * Rows::kEach < a.dim && m_r < kCols;
-    const T *qp = s.rows<T>(a.q, head0) + m_c * Rows::kEach;
-    const T *dp = s.rows<T>(a.dout, head0) + m_c * Rows::kEach;
+    const T *qp = s.rows<T>(a.q, head0), *dp = s.rows<T>(a.dout, head0);
     const int64_t stat0 = (int64_t)s.b * a.queries * a.heads + head0;
-    Chunk mq[kMoved], md[kMoved];
+    // of the first 32 threads one column's numbers
     float m_lse = 0.0f, m_delta = 0.0f;
     int32_t m_last = -1, m_first = 0;
-    const auto fetch = [&](int32_t c0) {
-#pragma unroll
-        for (int n = 0; n < kMoved; ++n) {
-            const int32_t c = c0 + m_r + n * kPass, i = (int32_t)divide(c, a.group);
-            const int32_t g = c - i * group;
-            mq[n] = md[n] = (Chunk)(T)0.0f;
-            if (m_some && c < c_end) {
-                mq[n] = load<T, Rows::kEach>(qp + (i * a.q.row + g * a.q.head));
-                md[n] = load<T, Rows::kEach>(dp + (i * a.dout.row + g * a.dout.head));
-            }
-        }
+    const auto fetch = [&](int32_t c0, int buffer) {
+        const int32_t i0 = (int32_t)divide(c0, a.group);
+        const auto move = [&](const T *p, const HeadRows &m, char *to) {
+            move_tile<T, N, kCols, kAttendWaves>(
+                p + i0 * m.row, a.direct_rows, a.dim, to, wave, lane,
+                [&](int32_t row, int64_t *from) {
+                    const int32_t c = c0 + row, i = (int32_t)divide(c, a.group);
+                    *from = (i - i0) * m.row + (c - i * group) * m.head;
+                    return c < c_end;
+                });
+        };
+        move(qp, a.q, lds[buffer]);
+        move(dp, a.dout, lds[buffer] + kBytes);
         if (threadIdx.x < kCols) {
             const int32_t c = c0 + threadIdx.x, i = (int32_t)divide(c, a.group);
             m_last = c < c_end ? s.last(a, i) : -1;
             m_first = s.first(a, i);
-            m_lse = m_delta = 0.0f;
+            m_lse = m_delta = 0.0f;  // what the scores' and the products' sums start from
             if (m_last >= 0) {
                 const int64_t row = stat0 + (int64_t)i * a.heads + c - i * group;
-                m_lse = a.lse[row] * kLog2e;
-                m_delta = a.delta[row];
+                m_lse = (kCarry<T> - a.lse[row] * kLog2e) * (1.0f / a.scale_log2);
+                m_delta = -a.delta[row];
             }
         }
     };
-    const auto put = [&](int buffer) {
-        char *to = lds[buffer];
-        if (m_c < Rows::kChunks && m_r < kCols)
-#pragma unroll
-            for (int n = 0; n < kMoved; ++n) {
-                Rows::put(to, m_r + n * kPass, m_c, mq[n]);
-                Rows::put(to + kBytes, m_r + n * kPass, m_c, md[n]);
-            }
+    if (c_begin < c_end)
+        fetch(c_begin, 0);
+    const int row_at0 = Rows::row_at(lane), column_at0 = Rows::column_at(lane);
+    int buffer = 0;
+    for (int32_t c0 = c_begin; c0 < c_end; c0 += kCols, buffer ^= 1) {
         if (threadIdx.x < kCols) {
             lses[buffer][threadIdx.x] = m_lse;
             deltas[buffer][threadIdx.x] = m_delta;
             lasts[buffer][threadIdx.x] = m_last;
             firsts[buffer][threadIdx.x] = m_first;
         }
-    };
-    if (c_begin < c_end)
-        fetch(c_begin);
-    const int row_at0 = Rows::row_at(lane), column_at0 = Rows::column_at(lane);
-    int buffer = 0;
-    for (int32_t c0 = c_begin; c0 < c_end; c0 += kCols, buffer ^= 1) {
-        put(buffer);
-        __syncthreads();  // a tile is written again two turns on
+        // the tile is there, for all waves; the other buffer's tile has been used by all
+        loads_done();
+        __syncthreads();
         if (c0 + kCols < c_end)
-            fetch(c0 + kCols);
+            fetch(c0 + kCols, buffer ^ 1);
         // the wave's keys against the tile's first and last query
         const int32_t end = c0 + kCols < c_end ? c0 + kCols : c_end;
         const int32_t ia = (int32_t)divide(c0, a.group), ib = (int32_t)divide(end - 1, a.group);
@@ -362,14 +382,28 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
             continue;
         const bool whole = c0 + kCols <= c_end && mine1 <= s.last(a, ia) &&
                            (mine >= s.first(a, ib) || mine1 < a.sinks);
-        const char *qs = lds[buffer], *dys = qs + kBytes;
-        const int row_at = fresh(row_at0), column_at = fresh(column_at0);
-        f32x16 x = (f32x16)0.0f, y = (f32x16)0.0f;
-#pragma unroll
-        for (int t = 0; t < 2 * N; ++t) {
-            multiply<T>(x, Rows::row(qs, row_at, 0, t), k[t]);
-            multiply<T>(y, Rows::row(dys, row_at, 0, t), Rows::row(values, row_at, wave * 32, t));
-        }
+        const int row_at = fresh(row_at0 + buffer * (2 * kBytes));
+        const int column_at = fresh(column_at0 + buffer * (2 * kBytes));
+        const int value_at = fresh(row_at0 + wave * (32 * Rows::kStride));
+        // products take turns with what is made of the scores, operands read kAhead
+        // before they are used: scores; grad_out v^T beside the weights p; p^T grad_out
+        // beside d; d^T q. The sums start from minus lse and minus D; where a key is not
+        // seen from minus infinity, which leaves weights of zero.
+        constexpr int kAhead = 3, kHalf = 2 * N;
+        vec<T, 8> ahead[kAhead], ahead_v[2];
+        const auto read = [&](int k) {
+            const int part = k / kHalf, t = k % kHalf;
+            if (part < 2)
+                ahead[k % kAhead] = Rows::row(lds[0] + part * kBytes, row_at, 0, t);
+            else if (part < 4)
+                ahead[k % kAhead] = Rows::column(lds[0] + (3 - part) * kBytes, column_at,
+                                                 t / N * 16, t % N);
+        };
+        const auto read_v = [&](int t) {
+            if (t < kHalf)
+                ahead_v[t % 2] = Rows::row(values, value_at, 0, t);
+        };
+        f32x16 x, y;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int r = 8 * g + 4 * (lane >> 5);
@@ -377,9 +411,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
             const f32x4 d4 = *(const f32x4 *)&deltas[buffer][r];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float p = exp2_of(fmaf(x[4 * g + e], a.scale_log2, kCarry<T> - l4[e]));
-                x[4 * g + e] = p;
-                y[4 * g + e] = p * (y[4 * g + e] - d4[e]);
+                x[4 * g + e] = l4[e];
+                y[4 * g + e] = d4[e];
             }
             if (!whole) {
                 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
@@ -387,17 +420,49 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
                 const i32x4 first = *(const i32x4 *)&firsts[buffer][r];
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (!sees(j, last[e], first[e], a.sinks))
-                        x[4 * g + e] = y[4 * g + e] = 0.0f;
+                    x[4 * g + e] = sees(j, last[e], first[e], a.sinks) ? x[4 * g + e] : -INFINITY;
             }
         }
+        vec<T, 8> p[2], d[2];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const vec<T, 8> p = operand<T>(x, g), d = operand<T>(y, g);
+        for (int k = 0; k < kAhead; ++k)
+            read(k);
+        in_order();
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                multiply<T>(dv[n], Rows::column(dys, column_at, 16 * g, n), p);
-                multiply<T>(dk[n], Rows::column(qs, column_at, 16 * g, n), d);
+        for (int part = 0; part < 4; ++part) {
+#pragma unroll
+            for (int k = 0; k < kHalf; ++k) {
+                const vec<T, 8> next = ahead[(part * kHalf + k) % kAhead];
+                if (part == 0)
+                    multiply<T>(x, next, k_rows[k]);
+                else if (part == 1)
+                    multiply<T>(y, next, ahead_v[k % 2]);
+                else if (part == 2)
+                    multiply<T>(dv[k % N], next, p[k / N]);
+                else
+                    multiply<T>(dk[k % N], next, d[k / N]);
+                read(part * kHalf + k + kAhead);
+                if (part == 1)
+                    read_v(k + 2);
+#pragma unroll
+                for (int e = 16 * k / kHalf; e < 16 * (k + 1) / kHalf; ++e) {
+                    if (part == 1)
+                        x[e] = here(exp2_of(x[e] * a.scale_log2));
+                    else if (part == 2)
+                        y[e] = here(x[e] * y[e]);
+                }
+                in_order();
+            }
+            if (part == 0) {
+                read_v(0);
+                read_v(1);
+            }
+            if (part == 1) {
+                p[0] = operand<T>(x, 0);
+                p[1] = operand<T>(x, 1);
+            } else if (part == 2) {
+                d[0] = operand<T>(y, 0);
+                d[1] = operand<T>(y, 1);
             }
         }
     }

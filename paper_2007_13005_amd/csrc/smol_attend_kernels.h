@@ -207,7 +207,7 @@ template <typename T, int N>
 __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     attend_kernel(AttendArgs a)
 {
-    constexpr int kThreads = 64 * kAttendWaves, kKeys = kAttendKeys;
+    constexpr int kKeys = kAttendKeys;
     typedef LdsRows<T, N> Rows;
     constexpr int kBytes = kKeys * Rows::kStride;
     __shared__ __attribute__((aligned(512))) char lds[2][2 * kBytes];
@@ -222,20 +222,20 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     Columns<T, N> cols;
     cols.start(a, s, mine, lane);
     const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
-    Mover<T, N, kKeys, kThreads> k(a.dim, threadIdx.x), v(a.dim, threadIdx.x);
     const auto fetch = [&](int32_t n) {
         const int32_t j0 = walk.tile(n) * kKeys;
-        k.fetch(kp, a.k.row, j0, s.k_length);
-        v.fetch(vp, a.v.row, j0, s.k_length);
+        char *to = lds[(n - lo) & 1];
+        move_rows<T, N, kKeys, kAttendWaves>(kp, a.k.row, a.direct_keys, a.dim, to, wave, lane, j0,
+                                             s.k_length);
+        move_rows<T, N, kKeys, kAttendWaves>(vp, a.v.row, a.direct_keys, a.dim, to + kBytes, wave,
+                                             lane, j0, s.k_length);
     };
     if (lo < hi)
         fetch(lo);
     const int key_at0 = Rows::row_at(lane), value_at0 = Rows::column_at(lane);
     for (int32_t n = lo; n < hi; ++n) {
-        char *keys = lds[(n - lo) & 1], *values = keys + kBytes;
-        k.put(keys);
-        v.put(values);
-        // a tile is written again two turns on, behind the next turn's barrier
+        // tile n is there, for all waves; the other buffer's tile has been used by all
+        loads_done();
         __syncthreads();
         if (n + 1 < hi)
             fetch(n + 1);
@@ -319,8 +319,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     constexpr int kKeys = kAttendFewKeys;
     typedef LdsRows<T, N> Rows;
     constexpr int kBytes = kKeys * Rows::kStride;
-    static_assert(kAttendWaves * kBytes >= 2 * 64 * N * 16 * 4, "room for two waves' sums");
-    __shared__ __attribute__((aligned(512))) char lds[kAttendWaves * kBytes];
+    static_assert(kAttendWaves * 2 * kBytes >= 2 * 64 * N * 16 * 4, "room for two waves' sums");
+    __shared__ __attribute__((aligned(512))) char lds[kAttendWaves * 2 * kBytes];
     __shared__ float tops[kAttendWaves][32], sums[kAttendWaves][32];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Task task(a);
@@ -333,30 +333,31 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     Columns<T, N> cols;
     cols.start(a, s, c0, lane);
     const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
-    char *values = lds + wave * kBytes;
+    char *values = lds + wave * (2 * kBytes);
     vec<T, 8> k[2 * N];
-    Mover<T, N, kKeys, 64> v(a.dim, lane);
-    const auto fetch = [&](int32_t n) {
+    // (the keys' registers are asked for first: they are used first)
+    const auto fetch = [&](int32_t n, int buffer) {
         const int32_t j0 = walk.tile(n) * kKeys, j = j0 + (lane & 31);
         row_operands<T, N>(kp + (j < s.k_length ? j : s.k_length - 1) * a.k.row, a.dim, lane, k);
-        v.fetch(vp, a.v.row, j0, s.k_length);
+        move_rows<T, N, kKeys, 1>(vp, a.v.row, a.direct_keys, a.dim, values + buffer * kBytes, 0,
+                                  lane, j0, s.k_length);
     };
     const int32_t own = lo + wave;
     if (own < hi)
-        fetch(own);
+        fetch(own, 0);
     const int value_at0 = Rows::column_at(lane);
-    for (int32_t n = own; n < hi; n += kAttendWaves) {
+    int buffer = 0;
+    for (int32_t n = own; n < hi; n += kAttendWaves, buffer ^= 1) {
         const int32_t j0 = walk.tile(n) * kKeys;
-        const int value_at = fresh(value_at0);
+        const int value_at = fresh(value_at0 + buffer * kBytes);
         f32x16 x[1] = {(f32x16)0.0f};
 #pragma unroll
         for (int t = 0; t < 2 * N; ++t)
             multiply<T>(x[0], k[t], cols.q[t]);
-        asm volatile("" ::: "memory");  // the wave's reads of the last tile come first
-        v.put(values);
-        asm volatile("" ::: "memory");  // other lanes read what this one writes
+        loads_done();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // reads of the other buffer
         if (n + kAttendWaves < hi)
-            fetch(n + kAttendWaves);
+            fetch(n + kAttendWaves, buffer ^ 1);
         float f;
         cols.look(a, x[0], j0, lane, &f);
         cols.weigh(a, x[0], 0, 16);
@@ -375,6 +376,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         *j1 = *j0 + kKeys - 1;
         return true;
     });
+    loads_done();
     // the waves' sums at one maximum, then waves 2 and 3 into 0 and 1, 1 into 0
     const float half = both_halves(cols.l, [](float u, float v) { return u + v; });
     if (lane < 32) {
