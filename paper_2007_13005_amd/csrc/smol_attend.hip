@@ -225,14 +225,21 @@ AttendArgs args_of(const smol_attend_shape &s)
     return a;
 }
 
-// Whether `rows` rows of a matrix, and `heads` of its heads, lie within 2^31 bytes,
-// every chunk of 16 bytes aligned to 16.
-bool near(const HeadRows &m, int64_t rows, int64_t heads, int type)
+// Whether every chunk of 16 bytes is aligned to 16, and `rows` rows of a matrix and
+// `heads` of its heads lie within 2^31 bytes.
+bool near_rows(const HeadRows &m, int64_t rows, int64_t heads, int type)
 {
-    const int64_t size = elem_size(type), most = ((int64_t)1 << 31) - 256 * size;
+    const int64_t size = elem_size(type), most = ((int64_t)1 << 31) / size - 256;
     const int64_t any = (int64_t)(uintptr_t)m.p | m.batch * size | m.row * size | m.head * size;
     return any % 16 == 0 && m.row < most / rows && m.head < most / heads &&
-           (rows * m.row + heads * m.head) * size < most;
+           rows * m.row + heads * m.head < most;
+}
+
+// The same for rows of keys: what passes the last is told by its offset, so no row
+// stands within another.
+bool near_keys(const HeadRows &m, int64_t rows, int dim, int type)
+{
+    return near_rows(m, rows, 1, type) && m.row >= dim;
 }
 
 int check_workspace(const void *p, int64_t have, int64_t need)
@@ -300,7 +307,8 @@ extern "C" int smol_attend(const smol_attend_args *p, void *stream)
     const Split split = split_of(s);
     if ((st = check_workspace(p->workspace, p->workspace_bytes, part_bytes(s, split))) != SMOL_OK)
         return st;
-    a.direct_keys = near(a.k, kAttendKeys, 1, s.type) && near(a.v, kAttendKeys, 1, s.type);
+    a.direct_keys = near_keys(a.k, kAttendKeys, s.dim, s.type) &&
+                    near_keys(a.v, kAttendKeys, s.dim, s.type);
     a.lse = p->lse;
     a.rest = p->rest;
     a.part = (float *)p->workspace;
@@ -354,8 +362,9 @@ extern "C" int smol_attend_backward(const smol_attend_grad_args *p, void *stream
     if (parts.groups > kMostGroups)
         return set_error(SMOL_ERR_UNSUPPORTED, "too many rows and heads for a launch");
     // (keys of a workgroup; queries of 32 columns)
-    a.direct_keys = near(a.k, 128, 1, s.type) && near(a.v, 128, 1, s.type);
-    a.direct_rows = near(a.q, 33, a.group.d, s.type) && near(a.dout, 33, a.group.d, s.type);
+    a.direct_keys = near_keys(a.k, 128, s.dim, s.type) && near_keys(a.v, 128, s.dim, s.type);
+    a.direct_rows = near_rows(a.q, 33, a.group.d, s.type) &&
+                    near_rows(a.dout, 33, a.group.d, s.type);
     a.lse = (float *)p->lse;
     a.rest_in = p->rest;
     a.delta = (float *)p->workspace;

@@ -259,69 +259,98 @@ __device__ __forceinline__ void row_operands(const T *row, int32_t dim, int lane
 }
 
 // Moves one chunk a lane from base + offset to `to` + 16 * lane in LDS, without
-// registers between; zeros where offset is kNoChunk. Complete once loads_done says
-// so (the compiler does not count these loads).
+// registers between; zeros where it would pass `bytes` (kNoChunk always does).
+// Complete after loads_done and a barrier.
 constexpr uint32_t kNoChunk = ~15u;
-__device__ __forceinline__ void load_to_lds(const void *base, uint32_t offset, const char *to)
+__device__ __forceinline__ void load_to_lds(const void *base, uint32_t bytes, uint32_t offset,
+                                            const char *to)
 {
     typedef __attribute__((address_space(3))) void Shared;
-    // a raw buffer of 2^31 bytes: what lies past it reads as zero
-    const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x80000000u, 0x00027000);
+    const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, bytes, 0x00027000);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (Shared *)to, 16, offset, 0, 0, 0);
 }
 __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// A tile of rows on its way to LDS, by `Waves` waves. place(row, &from) gives where
-// a row stands, in elements from p, or false for none: zeros, as past the head.
-// direct: everything is aligned to 16 bytes and rows lie within 2^31 bytes of p;
-// else they go through registers, and the wave waits.
-template <typename T, int N, int Rows, int Waves, typename Place>
-__device__ __forceinline__ void move_tile(const T *p, bool direct, int32_t dim, char *tile,
-                                          int wave, int lane, Place place)
-{
-    typedef LdsRows<T, N> Layout;
-    constexpr int kTotal = Rows * Layout::kChunks, kIssues = (kTotal + 64 * Waves - 1) /
-                                                             (64 * Waves);
-    static_assert(kTotal % 64 == 0, "whole waves");
-    lane = fresh(lane);
-    const auto each = [&](auto move) {
-#pragma unroll
-        for (int n = 0; n < kIssues; ++n) {
-            const int first = (n * Waves + wave) * 64, id = first + lane;
-            if (kTotal % (64 * Waves) && first >= kTotal)
-                break;
-            const int row = id / Layout::kChunks;
-            const int at = ((id % Layout::kChunks) ^ Layout::turn(row)) * Layout::kEach;
-            int64_t from;
-            const bool some = place(row, &from) && at < dim;
-            move(tile + first * 16, some, from + at);
-        }
-    };
-    if (direct)
-        each([&](char *to, bool some, int64_t from) {
-            load_to_lds(p, some ? (uint32_t)from * (uint32_t)sizeof(T) : kNoChunk, to);
-        });
-    else
-        each([&](char *to, bool some, int64_t from) {
-            typename Layout::Chunk v = (typename Layout::Chunk)(T)0.0f;
-            if (some)
-                v = load<T, Layout::kEach>(p + from);
-            *(typename Layout::Chunk *)(to + lane * 16) = v;
-        });
-}
-
-// Rows row0 .. of `rows` rows of keys or values.
+// Which chunks of a tile in LDS a lane of `Waves` waves moves: chunk n of its own
+// comes from value at(n) of row row(n).
 template <typename T, int N, int Rows, int Waves>
-__device__ __forceinline__ void move_rows(const T *p, int64_t stride, bool direct, int32_t dim,
+struct Share {
+    typedef LdsRows<T, N> Layout;
+    static constexpr int kTotal = Rows * Layout::kChunks;
+    static constexpr int kCount = (kTotal + 64 * Waves - 1) / (64 * Waves);
+    static_assert(kTotal % 64 == 0, "whole waves");
+    static __device__ __forceinline__ int first(int n, int wave) { return (n * Waves + wave) * 64; }
+    static __device__ __forceinline__ bool has(int n, int wave)
+    {
+        return kTotal % (64 * Waves) == 0 || first(n, wave) < kTotal;
+    }
+    static __device__ __forceinline__ int row(int n, int wave, int lane)
+    {
+        return (first(n, wave) + lane) / Layout::kChunks;
+    }
+    static __device__ __forceinline__ int at(int n, int wave, int lane)
+    {
+        const int chunk = (first(n, wave) + lane) % Layout::kChunks;
+        return (chunk ^ Layout::turn(row(n, wave, lane))) * Layout::kEach;
+    }
+};
+
+// Rows of keys or values, a stride apart, on their way to tiles in LDS. direct
+// (see near_rows in smol_attend.hip): aligned to 16 bytes, no row within another,
+// a tile within 2^31 bytes; else they go through registers, and the wave waits.
+// Offsets within a tile are formed once. Where 64 * Waves chunks are rows that all
+// turn alike, one offset serves all of a lane's chunks.
+template <typename T, int N, int Rows, int Waves>
+struct RowMover {
+    typedef Share<T, N, Rows, Waves> Mine;
+    typedef LdsRows<T, N> Layout;
+    static constexpr bool kAlike = 64 * Waves % (16 * Layout::kChunks) == 0;
+    static constexpr int kStep = kAlike ? 64 * Waves / Layout::kChunks : 0;
+    uint32_t offset[kAlike ? 1 : Mine::kCount];
+    __device__ __forceinline__ RowMover(int64_t stride, int32_t dim, int wave, int lane)
+    {
+#pragma unroll
+        for (int n = 0; n < (kAlike ? 1 : Mine::kCount); ++n) {
+            const int at = Mine::at(n, wave, lane);
+            offset[n] = at < dim ? ((uint32_t)Mine::row(n, wave, lane) * (uint32_t)stride + at) *
+                                       (uint32_t)sizeof(T)
+                                 : kNoChunk;
+        }
+    }
+    // Rows row0 .. of `rows`, zeros past them and past the head.
+    __device__ __forceinline__ void fetch(const T *p, int64_t stride, bool direct, int32_t dim,
                                           char *tile, int wave, int lane, int32_t row0,
-                                          int32_t rows)
-{
-    move_tile<T, N, Rows, Waves>(p + row0 * stride, direct, dim, tile, wave, lane,
-                                 [&](int32_t row, int64_t *from) {
-                                     *from = row * stride;
-                                     return row0 + row < rows;
-                                 });
-}
+                                          int32_t rows) const
+    {
+        p += row0 * stride;
+        const int32_t left = rows - row0 < Rows ? rows - row0 : Rows;
+        if (direct) {
+#pragma unroll
+            for (int n = 0; n < Mine::kCount; ++n) {
+                const int32_t have = left - n * kStep;
+                const uint32_t bytes =
+                    have > 0 ? ((uint32_t)(have - 1) * (uint32_t)stride + dim) *
+                                   (uint32_t)sizeof(T)
+                             : 0;
+                if (Mine::has(n, wave))
+                    load_to_lds(p + n * kStep * stride, bytes, offset[kAlike ? 0 : n],
+                                tile + Mine::first(n, wave) * 16);
+            }
+            return;
+        }
+        lane = fresh(lane);
+#pragma unroll
+        for (int n = 0; n < Mine::kCount; ++n) {
+            if (!Mine::has(n, wave))
+                break;
+            const int row = Mine::row(n, wave, lane), at = Mine::at(n, wave, lane);
+            typename Layout::Chunk v = (typename Layout::Chunk)(T)0.0f;
+            if (row < left && at < dim)
+                v = load<T, Layout::kEach>(p + row * stride + at);
+            *(typename Layout::Chunk *)(tile + (Mine::first(n, wave) + lane) * 16) = v;
+        }
+    }
+};
 
 // Whether any of a result's N tiles has a value that is not finite.
 template <int N>

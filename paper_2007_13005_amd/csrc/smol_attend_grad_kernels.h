@@ -120,13 +120,13 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     for (int n = 0; n < N; ++n)
         sum[n] = (f32x16)0.0f;
     const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
+    typedef RowMover<T, N, kKeys, kAttendWaves> Moves;
+    const Moves k_moves(a.k.row, a.dim, wave, lane), v_moves(a.v.row, a.dim, wave, lane);
     const auto fetch = [&](int32_t n) {
         const int32_t j0 = walk.tile(n) * kKeys;
         char *to = lds[n & 1];
-        move_rows<T, N, kKeys, kAttendWaves>(kp, a.k.row, a.direct_keys, a.dim, to, wave, lane,
-                                             j0, s.k_length);
-        move_rows<T, N, kKeys, kAttendWaves>(vp, a.v.row, a.direct_keys, a.dim, to + kBytes, wave,
-                                             lane, j0, s.k_length);
+        k_moves.fetch(kp, a.k.row, a.direct_keys, a.dim, to, wave, lane, j0, s.k_length);
+        v_moves.fetch(vp, a.v.row, a.direct_keys, a.dim, to + kBytes, wave, lane, j0, s.k_length);
     };
     if (walk.count)
         fetch(0);
@@ -325,27 +325,69 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     if (c_begin < c_end) {
         row_operands<T, N>(kp + (j < a.keys ? j : a.keys - 1) * a.k.row, a.dim, lane,
                            k_rows);
-        move_rows<T, N, kKeys, kAttendWaves>(vp, a.v.row, a.direct_keys, a.dim, values, wave, lane,
-                                             j0, s.k_length);
+        RowMover<T, N, kKeys, kAttendWaves>(a.v.row, a.dim, wave, lane)
+            .fetch(vp, a.v.row, a.direct_keys, a.dim, values, wave, lane, j0, s.k_length);
     }
     const T *qp = s.rows<T>(a.q, head0), *dp = s.rows<T>(a.dout, head0);
     const int64_t stat0 = (int64_t)s.b * a.queries * a.heads + head0;
     // of the first 32 threads one column's numbers
     float m_lse = 0.0f, m_delta = 0.0f;
     int32_t m_last = -1, m_first = 0;
-    const auto fetch = [&](int32_t c0, int buffer) {
+    // offsets of the thread's chunks from the tile's first query: the same for all
+    // tiles where these begin with whole queries
+    typedef Share<T, N, kCols, kAttendWaves> Mine;
+    const bool whole_queries = kCols % group == 0;
+    uint32_t q_offset[Mine::kCount], d_offset[Mine::kCount];
+    const auto place = [&](int32_t c0) {
         const int32_t i0 = (int32_t)divide(c0, a.group);
-        const auto move = [&](const T *p, const HeadRows &m, char *to) {
-            move_tile<T, N, kCols, kAttendWaves>(
-                p + i0 * m.row, a.direct_rows, a.dim, to, wave, lane,
-                [&](int32_t row, int64_t *from) {
-                    const int32_t c = c0 + row, i = (int32_t)divide(c, a.group);
-                    *from = (i - i0) * m.row + (c - i * group) * m.head;
-                    return c < c_end;
-                });
-        };
-        move(qp, a.q, lds[buffer]);
-        move(dp, a.dout, lds[buffer] + kBytes);
+#pragma unroll
+        for (int n = 0; n < Mine::kCount; ++n) {
+            const int32_t c = c0 + Mine::row(n, wave, lane), i = (int32_t)divide(c, a.group);
+            const uint32_t at = Mine::at(n, wave, lane), g = c - i * group;
+            const bool some = at < (uint32_t)a.dim;
+            q_offset[n] = some ? ((uint32_t)(i - i0) * (uint32_t)a.q.row + g * (uint32_t)a.q.head +
+                                  at) * (uint32_t)sizeof(T)
+                               : kNoChunk;
+            d_offset[n] = some ? ((uint32_t)(i - i0) * (uint32_t)a.dout.row +
+                                  g * (uint32_t)a.dout.head + at) * (uint32_t)sizeof(T)
+                               : kNoChunk;
+        }
+    };
+    const auto fetch = [&](int32_t c0, int buffer) {
+        char *to = lds[buffer];
+        if (a.direct_rows) {
+            const int32_t i0 = (int32_t)divide(c0, a.group);
+            if (!whole_queries)
+                place(c0);
+#pragma unroll
+            for (int n = 0; n < Mine::kCount; ++n) {
+                const bool some = c0 + Mine::row(n, wave, lane) < c_end;
+                if (!Mine::has(n, wave))
+                    break;
+                load_to_lds(qp + i0 * a.q.row, 0x80000000u, some ? q_offset[n] : kNoChunk,
+                            to + Mine::first(n, wave) * 16);
+                load_to_lds(dp + i0 * a.dout.row, 0x80000000u, some ? d_offset[n] : kNoChunk,
+                            to + kBytes + Mine::first(n, wave) * 16);
+            }
+        } else {
+            const int l = fresh(lane);
+#pragma unroll
+            for (int n = 0; n < Mine::kCount; ++n) {
+                if (!Mine::has(n, wave))
+                    break;
+                typedef typename Rows::Chunk Chunk;
+                const int32_t c = c0 + Mine::row(n, wave, l), i = (int32_t)divide(c, a.group);
+                const int32_t g = c - i * group, at = Mine::at(n, wave, l);
+                Chunk v = (Chunk)(T)0.0f, w = v;
+                if (c < c_end && at < a.dim) {
+                    v = load<T, Rows::kEach>(qp + i * a.q.row + g * a.q.head + at);
+                    w = load<T, Rows::kEach>(dp + i * a.dout.row + g * a.dout.head + at);
+                }
+                char *here = to + (Mine::first(n, wave) + l) * 16;
+                *(Chunk *)here = v;
+                *(Chunk *)(here + kBytes) = w;
+            }
+        }
         if (threadIdx.x < kCols) {
             const int32_t c = c0 + threadIdx.x, i = (int32_t)divide(c, a.group);
             m_last = c < c_end ? s.last(a, i) : -1;
@@ -358,8 +400,10 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
             }
         }
     };
-    if (c_begin < c_end)
+    if (c_begin < c_end) {
+        place(c_begin);
         fetch(c_begin, 0);
+    }
     const int row_at0 = Rows::row_at(lane), column_at0 = Rows::column_at(lane);
     int buffer = 0;
     for (int32_t c0 = c_begin; c0 < c_end; c0 += kCols, buffer ^= 1) {

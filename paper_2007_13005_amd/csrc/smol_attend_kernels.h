@@ -222,13 +222,13 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     Columns<T, N> cols;
     cols.start(a, s, mine, lane);
     const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
+    typedef RowMover<T, N, kKeys, kAttendWaves> Moves;
+    const Moves k_moves(a.k.row, a.dim, wave, lane), v_moves(a.v.row, a.dim, wave, lane);
     const auto fetch = [&](int32_t n) {
         const int32_t j0 = walk.tile(n) * kKeys;
         char *to = lds[(n - lo) & 1];
-        move_rows<T, N, kKeys, kAttendWaves>(kp, a.k.row, a.direct_keys, a.dim, to, wave, lane, j0,
-                                             s.k_length);
-        move_rows<T, N, kKeys, kAttendWaves>(vp, a.v.row, a.direct_keys, a.dim, to + kBytes, wave,
-                                             lane, j0, s.k_length);
+        k_moves.fetch(kp, a.k.row, a.direct_keys, a.dim, to, wave, lane, j0, s.k_length);
+        v_moves.fetch(vp, a.v.row, a.direct_keys, a.dim, to + kBytes, wave, lane, j0, s.k_length);
     };
     if (lo < hi)
         fetch(lo);
@@ -335,12 +335,13 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
     char *values = lds + wave * (2 * kBytes);
     vec<T, 8> k[2 * N];
+    const RowMover<T, N, kKeys, 1> moves(a.v.row, a.dim, 0, lane);
     // (the keys' registers are asked for first: they are used first)
     const auto fetch = [&](int32_t n, int buffer) {
         const int32_t j0 = walk.tile(n) * kKeys, j = j0 + (lane & 31);
         row_operands<T, N>(kp + (j < s.k_length ? j : s.k_length - 1) * a.k.row, a.dim, lane, k);
-        move_rows<T, N, kKeys, 1>(vp, a.v.row, a.direct_keys, a.dim, values + buffer * kBytes, 0,
-                                  lane, j0, s.k_length);
+        moves.fetch(vp, a.v.row, a.direct_keys, a.dim, values + buffer * kBytes, 0, lane, j0,
+                    s.k_length);
     };
     const int32_t own = lo + wave;
     if (own < hi)
