@@ -37,7 +37,7 @@ struct AttendArgs {
     // gradients of keys: tiles of keys that hold sinks, and columns of a part of
     // these and of the other tiles (as many parts: the two divisors)
     int32_t sink_tiles, sink_part, tile_part;
-    Divisor group, pair_div, kv_heads, tile_div, sink_div;
+    Divisor group, pair_div, kv_heads, tile_div, sink_div, split_div;
 };
 
 constexpr int kAttendKeys = 64;     // of a tile that four waves share

@@ -315,6 +315,7 @@ extern "C" int smol_attend(const smol_attend_args *p, void *stream)
     a.tiles = split.tiles;
     a.tile_div = make_divisor(split.tiles);
     a.splits = split.splits;
+    a.split_div = make_divisor(split.splits);
     int e = launch(a, split.few ? kAttendFew : kAttendMany, s.type, s.dim,
                    (int64_t)split.tiles * a.pairs * split.splits, stream);
     if (e == hipSuccess && split.splits > 1)

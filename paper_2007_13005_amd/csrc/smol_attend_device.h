@@ -79,6 +79,23 @@ __device__ __forceinline__ int fresh(int x)
     return x;
 }
 
+// The same for a value that the wave shares.
+__device__ __forceinline__ int64_t fresh_scalar(int64_t x)
+{
+    asm volatile("" : "+s"(x));
+    return x;
+}
+
+// The kernel's arguments (its only parameter) read again: those that its end alone
+// needs would else take scalar registers through its loop.
+__device__ __forceinline__ const AttendArgs &args_again()
+{
+    auto p = (const __attribute__((address_space(4))) AttendArgs *)
+        __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const AttendArgs *)p;
+}
+
 // Nothing moves past this: the compiler keeps the order that is written.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
@@ -221,6 +238,47 @@ struct Column {
     }
 };
 
+// What 32 columns from c0 on see, as a wave has to know it for a tile of keys.
+// Columns that do not exist, or see nothing, count for neither: whatever comes of
+// them is not kept.
+struct Sight {
+    int32_t last, first;  // of the lane's column
+    int32_t last_min, last_max, first_min, first_max;  // over the columns
+    __device__ __forceinline__ void start(const AttendArgs &a, const Sequence &s, int32_t c0,
+                                          const Column &c)
+    {
+        last = c.exists ? s.last(a, c.i) : -1;
+        first = s.first(a, c.i);
+        const Column lo(a, s, c0), hi(a, s, c0 + 31);
+        const int32_t end = hi.i < s.q_length ? hi.i : s.q_length - 1;
+        last_max = lo.i < s.q_length ? s.last(a, end) : -1;
+        last_min = s.last(a, lo.i) > 0 ? s.last(a, lo.i) : 0;
+        first_min = s.first(a, lo.i);
+        first_max = s.first(a, end);
+    }
+    // Whether any column sees a key of j0 .. j1.
+    __device__ __forceinline__ bool any(const AttendArgs &a, int32_t j0, int32_t j1) const
+    {
+        return j0 <= last_max && (j1 >= first_min || j0 < a.sinks);
+    }
+    // x[e] for keys j0 + 8 (e / 4) + 4 (lane / 32) + e % 4, e = 0 .. 15: `hidden` where the
+    // lane's column does not see the key.
+    __device__ __forceinline__ void hide(const AttendArgs &a, f32x16 &x, int32_t j0, int lane,
+                                         float hidden) const
+    {
+        const bool end = j0 + 31 > last_min, begin = j0 < first_max && j0 + 31 >= a.sinks;
+        if (!end && !begin)
+            return;
+        const int32_t base = fresh(j0 + 4 * (lane >> 5));
+        const int32_t to = last - base, from = begin ? first - base : -64, sinks = a.sinks - base;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int32_t j = 8 * (e >> 2) + (e & 3);
+            x[e] = j <= to && (j >= from || j < sinks) ? x[e] : hidden;
+        }
+    }
+};
+
 // The tiles of `Keys` keys that any of queries i0 .. i1 sees: those of the first
 // keys (sinks), then a run.
 template <int Keys>
@@ -322,6 +380,7 @@ struct RowMover {
                                           char *tile, int wave, int lane, int32_t row0,
                                           int32_t rows) const
     {
+        stride = fresh_scalar(stride);
         p += row0 * stride;
         const int32_t left = rows - row0 < Rows ? rows - row0 : Rows;
         if (direct) {

@@ -83,12 +83,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     const Walk<kKeys> walk(a, s, c_first.i, c_last.i);
     const Column c(a, s, mine + (lane & 31));
     const int64_t at = ((int64_t)s.b * a.queries + c.i) * a.heads + c.head;
-    const int32_t last = c.exists ? s.last(a, c.i) : -1, first = s.first(a, c.i);
-    const Column lo(a, s, mine), hi(a, s, mine + 31);
-    const int32_t last_max =
-        lo.i < s.q_length ? s.last(a, hi.i < s.q_length ? hi.i : s.q_length - 1) : -1;
-    const int32_t last_min = mine + 31 < a.columns && hi.i < s.q_length ? s.last(a, lo.i) : -1;
-    const int32_t first_min = s.first(a, lo.i), first_max = s.first(a, hi.i);
+    Sight sight;
+    sight.start(a, s, mine, c);
     vec<T, 8> q[2 * N], dy[2 * N];
     const T *qp = s.rows<T>(a.q, c.head) + c.i * a.q.row;
     const T *dyp = s.rows<T>(a.dout, c.head) + c.i * a.dout.row;
@@ -112,7 +108,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         }
         delta = both_halves(delta, [](float u, float v) { return u + v; });
     }
-    const float lse2 = last < 0 ? 0.0f : a.lse[at] * kLog2e, minus_lse = kCarry<T> - lse2;
+    const float lse2 = sight.last < 0 ? 0.0f : a.lse[at] * kLog2e, minus_lse = kCarry<T> - lse2;
     if (c.exists && lane < 32)
         a.delta[at] = delta;
     f32x16 sum[N];
@@ -138,7 +134,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         if (n + 1 < walk.count)
             fetch(n + 1);
         const int32_t j0 = walk.tile(n) * kKeys;
-        if (j0 > last_max || (j0 + kKeys - 1 < first_min && j0 >= a.sinks))
+        if (!sight.any(a, j0, j0 + kKeys - 1))
             continue;
         const int at_keys = (n & 1) * (2 * kBytes);
         const int row_at = fresh(row_at0 + at_keys), column_at = fresh(column_at0 + at_keys);
@@ -159,12 +155,9 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         // weights of zero
         f32x16 x[2] = {(f32x16)0.0f, (f32x16)0.0f}, y[2] = {(f32x16)0.0f, (f32x16)0.0f};
         vec<T, 8> d[4];
-        if (!(j0 + kKeys - 1 <= last_min && (j0 >= first_max || j0 + kKeys - 1 < a.sinks)))
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                const int32_t j = j0 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
-                x[e >> 4][e & 15] = sees(j, last, first, a.sinks) ? 0.0f : -INFINITY;
-            }
+        for (int h = 0; h < 2; ++h)
+            sight.hide(a, x[h], j0 + 32 * h, lane, -INFINITY);
         const auto weigh = [&](int h, int k) {
 #pragma unroll
             for (int e = 16 * k / kHalf; e < 16 * (k + 1) / kHalf; ++e)
@@ -203,15 +196,15 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
             }
         }
     }
-    const bool bad = any_not_finite(sum) && last >= 0 && fabsf(lse2) < INFINITY &&
+    const bool bad = any_not_finite(sum) && sight.last >= 0 && fabsf(lse2) < INFINITY &&
                      fabsf(delta) < INFINITY;
     uint64_t which = __ballot(bad);
     which = (which | which >> 32) & 0xffffffffu;
     while (which) {
         const int col = __builtin_ctzll(which);
         which &= which - 1;
-        const int32_t to = __builtin_amdgcn_readlane(last, col);
-        const int32_t from = __builtin_amdgcn_readlane(first, col);
+        const int32_t to = __builtin_amdgcn_readlane(sight.last, col);
+        const int32_t from = __builtin_amdgcn_readlane(sight.first, col);
         const float l2 = __shfl(lse2, col), dl = __shfl(delta, col);
         const Column cc(a, s, mine + col);
         const Spread qs = Spread::of(s.rows<T>(a.q, cc.head) + cc.i * a.q.row, a.dim, lane);
@@ -235,7 +228,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     }
     if (c.exists)
         write_row<T, N>((T *)s.rows<T>(a.dq, c.head) + c.i * a.dq.row, sum,
-                        a.scale * kCarried<T>, last < 0, a.dim, lane);
+                        a.scale * kCarried<T>, sight.last < 0, a.dim, lane);
 }
 
 // The queries that see any of keys j0 .. j1, and their columns.
@@ -418,14 +411,15 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         __syncthreads();
         if (c0 + kCols < c_end)
             fetch(c0 + kCols, buffer ^ 1);
-        // the wave's keys against the tile's first and last query
+        // the wave's keys (those that exist) against the tile's first and last query;
+        // columns past the last are zeros
         const int32_t end = c0 + kCols < c_end ? c0 + kCols : c_end;
         const int32_t ia = (int32_t)divide(c0, a.group), ib = (int32_t)divide(end - 1, a.group);
-        const int32_t mine1 = mine + 31;
+        const int32_t mine1 = mine + 31 < s.k_length ? mine + 31 : s.k_length - 1;
         if (mine > s.last(a, ib) || (mine1 < s.first(a, ia) && mine >= a.sinks))
             continue;
-        const bool whole = c0 + kCols <= c_end && mine1 <= s.last(a, ia) &&
-                           (mine >= s.first(a, ib) || mine1 < a.sinks);
+        const bool whole =
+            mine1 <= s.last(a, ia) && (mine >= s.first(a, ib) || mine1 < a.sinks);
         const int row_at = fresh(row_at0 + buffer * (2 * kBytes));
         const int column_at = fresh(column_at0 + buffer * (2 * kBytes));
         const int value_at = fresh(row_at0 + wave * (32 * Rows::kStride));

@@ -28,36 +28,19 @@ struct Columns {
     vec<T, 8> q[2 * N];
     f32x16 sum[N];   // [values x columns]
     float m, l;      // l: of this half of the wave
-    int32_t last, first;
-    int32_t last_min, last_max, first_min, first_max;  // over the wave's columns
+    Sight sight;
 
     __device__ __forceinline__ void start(const AttendArgs &a, const Sequence &s, int32_t c0,
                                           int lane)
     {
         const Column c(a, s, c0 + (lane & 31));
         row_operands<T, N>(s.rows<T>(a.q, c.head) + c.i * a.q.row, a.dim, lane, q);
-        last = c.exists ? s.last(a, c.i) : -1;
-        first = s.first(a, c.i);
+        sight.start(a, s, c0, c);
 #pragma unroll
         for (int n = 0; n < N; ++n)
             sum[n] = (f32x16)0.0f;
         m = kLowest;
         l = 0.0f;
-        const Column lo(a, s, c0), hi(a, s, c0 + 31);
-        last_max = s.last(a, hi.i < s.q_length ? hi.i : s.q_length - 1);
-        last_max = lo.i < s.q_length ? last_max : -1;
-        last_min = c0 + 31 < a.columns && hi.i < s.q_length ? s.last(a, lo.i) : -1;
-        first_min = s.first(a, lo.i);
-        first_max = s.first(a, hi.i);
-    }
-    // Whether any column sees a key of j0 .. j1; whether all see all.
-    __device__ __forceinline__ bool any(const AttendArgs &a, int32_t j0, int32_t j1) const
-    {
-        return j0 <= last_max && (j1 >= first_min || j0 < a.sinks);
-    }
-    __device__ __forceinline__ bool all(const AttendArgs &a, int32_t j0, int32_t j1) const
-    {
-        return j1 <= last_min && (j0 >= first_max || j1 < a.sinks);
     }
     // Scores x of 32 keys from j0 on (register rows): what is not seen leaves, and
     // the maximum follows. True (and f) where what was summed, and weights formed
@@ -66,12 +49,7 @@ struct Columns {
     __device__ __forceinline__ bool look(const AttendArgs &a, f32x16 &x, int32_t j0, int lane,
                                          float *f)
     {
-        if (!all(a, j0, j0 + 31))
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int32_t j = j0 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
-                x[e] = sees(j, last, first, a.sinks) ? x[e] : -INFINITY;
-            }
+        sight.hide(a, x, j0, lane, -INFINITY);
         float top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -104,14 +82,14 @@ struct Columns {
     __device__ __forceinline__ void mend(const AttendArgs &a, const Sequence &s, int32_t c0,
                                          int lane, Next next)
     {
-        const bool bad = any_not_finite(sum) && fabsf(l) < INFINITY && last >= 0;
+        const bool bad = any_not_finite(sum) && fabsf(l) < INFINITY && sight.last >= 0;
         uint64_t which = __ballot(bad);
         which = (which | which >> 32) & 0xffffffffu;
         while (which) {
             const int col = __builtin_ctzll(which);
             which &= which - 1;
-            const int32_t to = __builtin_amdgcn_readlane(last, col);
-            const int32_t from = __builtin_amdgcn_readlane(first, col);
+            const int32_t to = __builtin_amdgcn_readlane(sight.last, col);
+            const int32_t from = __builtin_amdgcn_readlane(sight.first, col);
             const float top = __builtin_bit_cast(
                 float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), col));
             const Column c(a, s, c0 + col);
@@ -161,7 +139,7 @@ struct Columns {
             return;
         }
         const Column c(a, s, at);
-        const float f = last < 0 ? 0.0f : 1.0f / l;
+        const float f = sight.last < 0 ? 0.0f : 1.0f / l;
         T *out = (T *)s.rows<T>(a.out, c.head) + c.i * a.out.row;
         const int64_t row = ((int64_t)s.b * a.queries + c.i) * a.heads + c.head;
         T *rest = a.rest ? (T *)a.rest + row * a.dim : nullptr;
@@ -175,14 +153,14 @@ struct Columns {
                 vec<float, 4> y;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    y[e] = last < 0 ? 0.0f : sum[n][4 * g + e] * f;
+                    y[e] = sight.last < 0 ? 0.0f : sum[n][4 * g + e] * f;
                 const vec<T, 4> z = from_f32<T, 4>(y);
                 store<T, 4>(out + d, z);
                 if (rest)
                     store<T, 4>(rest + d, from_f32<T, 4>(y - to_f32<4, T>(z)));
             }
         if (a.lse && lane < 32)
-            a.lse[row] = last < 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+            a.lse[row] = sight.last < 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
     }
 };
 
@@ -217,8 +195,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     const int32_t c0 = task.tile * (kAttendWaves * 32), mine = c0 + wave * 32;
     const Column c_first(a, s, c0), c_last(a, s, c0 + kAttendWaves * 32 - 1);
     const Walk<kKeys> walk(a, s, c_first.i, c_last.i);
-    const int32_t lo = (int32_t)((int64_t)walk.count * task.split / a.splits);
-    const int32_t hi = (int32_t)((int64_t)walk.count * (task.split + 1) / a.splits);
+    const int32_t lo = (int32_t)divide(walk.count * task.split, a.split_div);
+    const int32_t hi = (int32_t)divide(walk.count * (task.split + 1), a.split_div);
     Columns<T, N> cols;
     cols.start(a, s, mine, lane);
     const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
@@ -240,7 +218,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         if (n + 1 < hi)
             fetch(n + 1);
         const int32_t j0 = walk.tile(n) * kKeys;
-        if (!cols.any(a, j0, j0 + kKeys - 1))
+        if (!cols.sight.any(a, j0, j0 + kKeys - 1))
             continue;
         const int key_at = fresh(key_at0 + (n - lo & 1) * (2 * kBytes));
         const int value_at = fresh(value_at0 + (n - lo & 1) * (2 * kBytes) + kBytes);
@@ -300,14 +278,15 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
             in_order();
         }
     }
-    cols.mend(a, s, mine, lane, [&](int32_t n, int32_t *j0, int32_t *j1) {
+    const AttendArgs &late = args_again();
+    cols.mend(late, s, mine, lane, [&](int32_t n, int32_t *j0, int32_t *j1) {
         if (lo + n >= hi)
             return false;
         *j0 = walk.tile(lo + n) * kKeys;
         *j1 = *j0 + kKeys - 1;
         return true;
     });
-    cols.finish(a, s, mine, task.pair, task.split, lane);
+    cols.finish(late, s, mine, task.pair, task.split, lane);
 }
 
 // 32 columns a workgroup: its four waves take tiles of 32 keys in turn, each
@@ -328,8 +307,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     const int32_t c0 = task.tile * 32;
     const Column c_first(a, s, c0), c_last(a, s, c0 + 31);
     const Walk<kKeys> walk(a, s, c_first.i, c_last.i);
-    const int32_t lo = (int32_t)((int64_t)walk.count * task.split / a.splits);
-    const int32_t hi = (int32_t)((int64_t)walk.count * (task.split + 1) / a.splits);
+    const int32_t lo = (int32_t)divide(walk.count * task.split, a.split_div);
+    const int32_t hi = (int32_t)divide(walk.count * (task.split + 1), a.split_div);
     Columns<T, N> cols;
     cols.start(a, s, c0, lane);
     const T *kp = s.rows<T>(a.k, s.kv), *vp = s.rows<T>(a.v, s.kv);
@@ -370,7 +349,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
                 multiply<T>(cols.sum[n2], Rows::column(values, value_at, 16 * g, n2), w);
         }
     }
-    cols.mend(a, s, c0, lane, [&](int32_t n, int32_t *j0, int32_t *j1) {
+    const AttendArgs &late = args_again();
+    cols.mend(late, s, c0, lane, [&](int32_t n, int32_t *j0, int32_t *j1) {
         if (own + n * kAttendWaves >= hi)
             return false;
         *j0 = walk.tile(own + n * kAttendWaves) * kKeys;
@@ -418,7 +398,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     if (wave != 0)
         return;
     cols.l = lane < 32 ? total : 0.0f;  // finish adds the halves
-    cols.finish(a, s, c0, task.pair, task.split, lane);
+    cols.finish(late, s, c0, task.pair, task.split, lane);
 }
 
 // Joins the parts of the keys: a workgroup a column, each wave a quarter of the
