@@ -13,37 +13,44 @@
 namespace smol {
 namespace {
 
-// Joins the workgroups' sums in order: 16 columns a workgroup, 16 threads a
-// column each taking every 16th workgroup's, eight loads at once.
+// Joins the workgroups' sums in order: 16 columns a workgroup, 64 threads a
+// column each taking every 64th workgroup's, eight loads at once (all there are:
+// 512 workgroups), then four threads a column, then one.
 template <typename P>
-__global__ void __launch_bounds__(256) head_join_kernel(const float *sums, P *q, P *k,
-                                                        int32_t dim, int32_t groups,
-                                                        int32_t accumulate)
+__global__ void __launch_bounds__(1024) head_join_kernel(const float *sums, P *q, P *k,
+                                                         int32_t dim, int32_t groups,
+                                                         int32_t accumulate)
 {
+    constexpr int kAhead = 8;
     const int32_t c = blockIdx.x * 16 + (threadIdx.x & 15), first = threadIdx.x >> 4;
-    __shared__ float part[16][17];
+    __shared__ float part[64][17];
     float s = 0.0f;
-    if (c < 2 * dim) {
-        constexpr int kAhead = 8;
-        for (int32_t g = first; g < groups; g += 16 * kAhead) {
+    if (c < 2 * dim)
+        for (int32_t g = first; g < groups; g += 64 * kAhead) {
             float x[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int32_t at = g + 16 * u;
+                const int32_t at = g + 64 * u;
                 x[u] = sums[(int64_t)(at < groups ? at : first) * 2 * dim + c];
             }
             asm volatile("" ::: "memory");
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
-                s += g + 16 * u < groups ? x[u] : 0.0f;
+                s += g + 64 * u < groups ? x[u] : 0.0f;
         }
-    }
     part[first][threadIdx.x & 15] = s;
     __syncthreads();
+    if (first >= 4)
+        return;
+    // (one wave from here on)
+    s = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 16; ++t)
+        s += part[first * 16 + t][threadIdx.x & 15];
+    const float s1 = __shfl_down(s, 16), s2 = __shfl_down(s, 32), s3 = __shfl_down(s, 48);
     if (first != 0 || c >= 2 * dim)
         return;
-    for (int t = 1; t < 16; ++t)
-        s += part[t][threadIdx.x];
+    s = s + s1 + s2 + s3;
     P *out = c < dim ? q : k;
     if (!out)
         return;
@@ -53,7 +60,10 @@ __global__ void __launch_bounds__(256) head_join_kernel(const float *sums, P *q,
 
 constexpr int kWaves = 4;             // of a workgroup (kHeadWaves)
 constexpr int64_t kFewItems = 8192;   // waves that the chip holds at once
-constexpr int kGradGroups = 1024;     // workgroups of the backward pass at most
+// of the backward pass, whose waves' angles, weights and sums serve more heads so
+// (2048 rows of 32 and 8 heads of 128 bf16 values: 27 us with 8192 waves, 19)
+constexpr int64_t kFewGradItems = 2048;
+constexpr int kGradGroups = 512;      // workgroups of the backward pass at most
 
 int floor_log2(int v)
 {
@@ -64,7 +74,7 @@ int floor_log2(int v)
 }
 
 // Chunks, lanes, rows and parts for heads of this width.
-void plan(HeadArgs *a, HeadForm *f, int type)
+void plan(HeadArgs *a, HeadForm *f, int type, int64_t few = kFewItems)
 {
     const int dim = a->dim, half = a->half, rot = 2 * half;
     // the widest chunk of 16 bytes or less of which every run is whole: the
@@ -99,7 +109,7 @@ void plan(HeadArgs *a, HeadForm *f, int type)
     const int64_t blocks = ((int64_t)a->rows + (1 << a->rows_log2) - 1) >> a->rows_log2;
     // a wave takes all of a block's steps, so that angles and weights are formed
     // once, unless there would be too few waves
-    int64_t per = blocks * steps / kFewItems;
+    int64_t per = blocks * steps / few;
     per = per < 1 ? 1 : per < steps ? per : steps;
     a->per = (int)per;
     a->parts = (int)((steps + per - 1) / per);
@@ -450,7 +460,7 @@ extern "C" int smol_head_norm_backward(const smol_head_norm_grad_args *p, void *
     if (s.rows > 0 && p->q.heads + p->k.heads > 0) {
         fill_shape(&a, &f, s);
         a.sign = -1.0f;
-        plan(&a, &f, s.type);
+        plan(&a, &f, s.type, kFewGradItems);
         const int64_t groups = (a.items + kWaves - 1) / kWaves;
         a.groups = (int32_t)(groups < kGradGroups ? groups : kGradGroups);
         e = launch(a, f, s.type, true, a.groups, stream);
@@ -458,7 +468,7 @@ extern "C" int smol_head_norm_backward(const smol_head_norm_grad_args *p, void *
     if (e == hipSuccess && (p->q.grad_weight || p->k.grad_weight)) {
         with_type(s.weight_type, [&](auto t) {
             typedef decltype(t) P;
-            hipLaunchKernelGGL((head_join_kernel<P>), dim3((2 * s.dim + 15) / 16), dim3(256), 0,
+            hipLaunchKernelGGL((head_join_kernel<P>), dim3((2 * s.dim + 15) / 16), dim3(1024), 0,
                                (hipStream_t)stream, a.part, (P *)p->q.grad_weight,
                                (P *)p->k.grad_weight, s.dim, a.groups, p->accumulate);
         });
