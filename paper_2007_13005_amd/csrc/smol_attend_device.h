@@ -411,17 +411,52 @@ struct RowMover {
     }
 };
 
-// Whether any of a result's N tiles has a value that is not finite.
+// Whether any of a result's N tiles has a value that is not finite: the only ones
+// that 0 times does not make 0.
 template <int N>
 __device__ __forceinline__ bool any_not_finite(const f32x16 (&x)[N])
 {
-    bool bad = false;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-            bad |= !(fabsf(x[n][e]) < INFINITY);
-    return bad;
+            s[e & 3] = fmaf(x[n][e], 0.0f, s[e & 3]);
+    const float all = (s[0] + s[1]) + (s[2] + s[3]);
+    return all != all;
+}
+
+// Writes a result [values x rows]: the lane's row at p, times f, and what rounding
+// takes from it at rest (or null); zeros for a row that has no pair (its sums may
+// hold 0 times a NaN). dim is a multiple of 8, so both halves of the wave write.
+template <typename T, int N>
+__device__ __forceinline__ void write_row(T *p, T *rest, f32x16 (&sum)[N], float f, bool none,
+                                          int32_t dim, int lane)
+{
+    if (__any(none))
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                sum[n][e] = none ? 0.0f : sum[n][e];
+    f = none ? 0.0f : f;
+    p += 4 * (lane >> 5);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = 32 * n + 8 * g;
+            if (d >= dim)
+                return;
+            vec<float, 4> y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                y[e] = sum[n][4 * g + e] * f;
+            const vec<T, 4> z = from_f32<T, 4>(y);
+            store<T, 4>(p + d, z);
+            if (rest)
+                store<T, 4>(rest + 4 * (lane >> 5) + d, from_f32<T, 4>(y - to_f32<4, T>(z)));
+        }
 }
 
 // A row of up to 128 values over the wave: values lane and lane + 64.

@@ -31,27 +31,6 @@ constexpr float kCarry = std::is_same<T, f16>::value ? 6.0f : 0.0f;  // log2
 template <typename T>
 constexpr float kCarried = std::is_same<T, f16>::value ? 1.0f / 64.0f : 1.0f;
 
-// Writes a result [values x rows]: the lane's row at p, times f; zeros for a row
-// that has no pair (its sums may hold 0 times a NaN).
-template <typename T, int N>
-__device__ __forceinline__ void write_row(T *p, const f32x16 (&sum)[N], float f, bool none,
-                                          int32_t dim, int lane)
-{
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int32_t d = 32 * n + 8 * g + 4 * (lane >> 5);
-            if (d >= dim)
-                continue;
-            vec<float, 4> y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                y[e] = none ? 0.0f : sum[n][4 * g + e] * f;
-            store<T, 4>(p + d, from_f32<T, 4>(y));
-        }
-}
-
 // The weight of one pair and its d, over the wave.
 struct PairOf {
     float p, d;
@@ -227,7 +206,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         set_column(sum, y, col, lane);
     }
     if (c.exists)
-        write_row<T, N>((T *)s.rows<T>(a.dq, c.head) + c.i * a.dq.row, sum,
+        write_row<T, N>((T *)s.rows<T>(a.dq, c.head) + c.i * a.dq.row, nullptr, sum,
                         a.scale * kCarried<T>, sight.last < 0, a.dim, lane);
 }
 
@@ -538,14 +517,14 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     const float fk = a.scale * kCarried<T>, fv = kCarried<T>;
     if (!task.whole) {
         float *p = a.part + ((int64_t)blockIdx.x * 2 * kKeys + wave * 32 + (lane & 31)) * (N * 32);
-        write_row<float, N>(p, dk, fk, none, N * 32, lane);
-        write_row<float, N>(p + kKeys * (N * 32), dv, fv, none, N * 32, lane);
+        write_row<float, N>(p, nullptr, dk, fk, none, N * 32, lane);
+        write_row<float, N>(p + kKeys * (N * 32), nullptr, dv, fv, none, N * 32, lane);
         return;
     }
     if (j >= a.keys)
         return;
-    write_row<T, N>((T *)s.rows<T>(a.dk, s.kv) + j * a.dk.row, dk, fk, none, a.dim, lane);
-    write_row<T, N>((T *)s.rows<T>(a.dv, s.kv) + j * a.dv.row, dv, fv, none, a.dim, lane);
+    write_row<T, N>((T *)s.rows<T>(a.dk, s.kv) + j * a.dk.row, nullptr, dk, fk, none, a.dim, lane);
+    write_row<T, N>((T *)s.rows<T>(a.dv, s.kv) + j * a.dv.row, nullptr, dv, fv, none, a.dim, lane);
 }
 
 // Joins the parts of the keys' gradients, in order: four keys a workgroup, four

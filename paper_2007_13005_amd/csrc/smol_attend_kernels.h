@@ -139,26 +139,10 @@ struct Columns {
             return;
         }
         const Column c(a, s, at);
-        const float f = sight.last < 0 ? 0.0f : 1.0f / l;
         T *out = (T *)s.rows<T>(a.out, c.head) + c.i * a.out.row;
         const int64_t row = ((int64_t)s.b * a.queries + c.i) * a.heads + c.head;
-        T *rest = a.rest ? (T *)a.rest + row * a.dim : nullptr;
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int32_t d = 32 * n + 8 * g + 4 * (lane >> 5);
-                if (d >= a.dim)
-                    continue;
-                vec<float, 4> y;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    y[e] = sight.last < 0 ? 0.0f : sum[n][4 * g + e] * f;
-                const vec<T, 4> z = from_f32<T, 4>(y);
-                store<T, 4>(out + d, z);
-                if (rest)
-                    store<T, 4>(rest + d, from_f32<T, 4>(y - to_f32<4, T>(z)));
-            }
+        write_row<T, N>(out, a.rest ? (T *)a.rest + row * a.dim : nullptr, sum, 1.0f / l,
+                        sight.last < 0, a.dim, lane);
         if (a.lse && lane < 32)
             a.lse[row] = sight.last < 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
     }
@@ -182,7 +166,7 @@ struct Task {
 
 // Four waves of 32 columns each over shared tiles of 64 keys.
 template <typename T, int N>
-__global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
+__global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 4 ? 1 : N <= 2 ? 4 : 2)
     attend_kernel(AttendArgs a)
 {
     constexpr int kKeys = kAttendKeys;
@@ -222,6 +206,21 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
             continue;
         const int key_at = fresh(key_at0 + (n - lo & 1) * (2 * kBytes));
         const int value_at = fresh(value_at0 + (n - lo & 1) * (2 * kBytes) + kBytes);
+        if (!cols.sight.any(a, j0 + 32, j0 + kKeys - 1)) {
+            // the tile's first 32 keys alone (the last of 197 keys: 5 of them)
+            f32x16 x = (f32x16)0.0f;
+            float f;
+#pragma unroll
+            for (int k = 0; k < 2 * N; ++k)
+                multiply<T>(x, Rows::row(lds[0], key_at, 0, k), cols.q[k]);
+            cols.look(a, x, j0, lane, &f);
+            cols.weigh(a, x, 0, 16);
+#pragma unroll
+            for (int k = 0; k < 2 * N; ++k)
+                multiply<T>(cols.sum[k % N], Rows::column(lds[0], value_at, k / N * 16, k % N),
+                            operand<T>(x, k / N));
+            continue;
+        }
         // operands in the order of their products, kAhead read before they are used:
         // scores of the first 32 keys, of the second, values with the first 32 keys'
         // weights, with the second's
