@@ -540,6 +540,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves) attend_grad_join_kernel(Att
     const Sequence s(a, pair);
     const KeySpan span(a, s, tile * kKeys, tile * kKeys + kKeys - 1);
     const bool sink = tile < (uint32_t)a.sink_tiles;
+    if (sink && a.sink_div.d == 1)
+        return;  // its only part is written whole
     const int32_t size = sink ? a.sink_part : a.tile_part;
     const int32_t parts = (int32_t)(((int64_t)span.end - span.begin + size - 1) / size);
     // the first part's place among the workgroups' sums

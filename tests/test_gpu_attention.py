@@ -338,6 +338,39 @@ def test_attend_shapes(shape, dtype):
     check(q, k, v, dy, f"{shape}", **mask(shape))
 
 
+PARTS = [
+    # batch, queries, keys, heads, kv_heads, dim, causal, window, sinks
+    (129, 100, 100, 8, 1, 40, True, 20, 4),   # sinks in one part, the rest could have more
+    (2, 150, 260, 8, 1, 24, True, 40, 150),   # two tiles of sinks
+    (1, 700, 700, 8, 2, 64, False, 0, 0),
+    (1, 515, 300, 6, 2, 72, True, 100, 130),  # queries before the first key
+    (2, 333, 401, 5, 1, 128, True, 64, 3),    # columns of a query across tiles
+]
+
+
+@pytest.mark.parametrize("shape", PARTS)
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_attend_parts(shape, dtype):
+    """Gradients of keys whose columns are taken in parts, over whole and ragged
+    sequences, from tensors that load as they are and from misaligned ones."""
+    note(f"attend parts {shape} {dtype}")
+    b, lq, lk = shape[:3]
+    q, k, v, dy = inputs(shape, dtype, sum(shape[:6]))
+    if b == 1 or b > 2:
+        out, lse, rest, grads = check(q, k, v, dy, f"{shape}", **mask(shape))
+        lengths = {}
+    else:
+        ql, kl = (torch.tensor([n, n // 2 + 7], dtype=torch.int32) for n in (lq, lk))
+        out, lse, rest, grads = check(q, k, v, dy, f"{shape}", (ql, kl), **mask(shape))
+        lengths = {"q_lengths": dev(ql), "k_lengths": dev(kl)}
+    (sq, _), (sk, _), (sv, _), (sy, _) = spread(q), spread(k, 1, 3), spread(v, 5), spread(dy, 7, 5)
+    same = attention.attend(sq, sk, sv, **lengths, **mask(shape))
+    assert torch.equal(same[0], out) and torch.equal(same[1], lse)
+    got = attention.attend_backward(sy, sq, sk, sv, out, lse, rest, **lengths, **mask(shape))
+    for x, y in zip(got, grads):
+        assert torch.equal(x, y)
+
+
 @pytest.mark.parametrize("dim", list(range(8, 129, 8)))
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_attend_widths(dim, dtype):
@@ -683,6 +716,45 @@ def test_graphs_share_a_workspace():
             for a, c in zip(got, want):
                 assert torch.equal(a, c)
             room.fill_(turn)  # the program's own work on the same memory
+
+
+def test_heads_in_a_graph():
+    """Norm, rotation and their gradients captured in one graph: every replay
+    takes the positions that stand there then."""
+    note("heads graph")
+    rows, h, d = 300, 5, 64
+    g = gen(12)
+    x, dy = (dev(randn(g, rows, h, d, dtype=BF16)) for _ in range(2))
+    w, freqs = dev(1 + randn(g, d, scale=0.1)), dev(ref.frequencies(d)[0])
+    pos = torch.zeros(rows, dtype=torch.int64, device="cuda")
+    gw = torch.empty(d, device="cuda")
+
+    def call():
+        y = attention.head_norm(x, None, w, None, pos, freqs)[0]
+        z = attention.rotate(x, pos, freqs)
+        dz = attention.rotate_backward(dy, pos, freqs)
+        dx = attention.head_norm_backward(dy, None, x, None, w, None, pos, freqs,
+                                          grad_q_weight=gw)[0]
+        return y, z, dz, dx, gw
+
+    call()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call()
+    for start in (0, 17, 100000):
+        pos.copy_(torch.arange(rows) + start)
+        want = [t.clone() for t in call()]
+        for t in got:
+            t.fill_(SENTINEL)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, c in zip(got, want):
+            assert torch.equal(a, c)
 
 
 def test_two_streams_and_repeats():
