@@ -96,8 +96,14 @@ int64_t part_bytes(const smol_attend_shape &s, const Split &p)
     return p.splits * rows * (wide_of(s.dim) * 32 + 2) * 4;
 }
 
+// Parts of the columns of the keys' gradients. They make two workgroups a compute
+// unit; a part has at least 128 columns (against 512: 1 x 399 rows of 14 heads
+// of 128 over 2 keys' 52 -> 42 us, 2 x 148 of 16 of 80 over 4 31 -> 24), one of a
+// tile of sinks 512, as the others' workgroups run along (18 x 4422 rows of a head
+// of 128, a window of 15: 92 us against 100 with 256).
 constexpr int64_t kTileGroups = 512, kSinkGroups = 256;  // workgroups that parts make
-constexpr int64_t kKeyParts = 64, kLeastColumns = 512;   // of a tile; of a part
+constexpr int64_t kKeyParts = 64;                        // of a tile at most
+constexpr int64_t kLeastColumns = 128, kLeastSinkColumns = 512;
 
 // The parts in which the gradients of keys are formed: a tile of 128 keys takes
 // the columns of all queries that see it, or a part of them.
@@ -119,7 +125,6 @@ KeyParts key_parts_of(const smol_attend_shape &s)
         window ? std::min<int64_t>(s.queries, (int64_t)s.window + kKeys - 1) * group : all;
     p.tiles = (int32_t)ceil_div(s.keys, kKeys);
     p.sink_tiles = window ? (int32_t)std::min<int64_t>(ceil_div(s.sinks, kKeys), p.tiles) : 0;
-    // two workgroups a compute unit, each with 512 columns or more
     const auto parts = [&](int64_t groups, int64_t tiles, int64_t columns, int64_t least) {
         const int64_t n = std::min(groups / std::max<int64_t>(1, tiles * pairs),
                                    ceil_div(columns, least));
@@ -129,7 +134,7 @@ KeyParts key_parts_of(const smol_attend_shape &s)
     p.tile_part = (int32_t)(ceil_div(ceil_div(seen, p.tile_parts), 32) * 32);
     // those of sinks as long as the others' columns
     p.sink_parts =
-        parts(kSinkGroups, p.sink_tiles, all, std::max<int64_t>(p.tile_part, kLeastColumns));
+        parts(kSinkGroups, p.sink_tiles, all, std::max<int64_t>(p.tile_part, kLeastSinkColumns));
     p.sink_part = (int32_t)(ceil_div(ceil_div(all, p.sink_parts), 32) * 32);
     const int64_t first = (int64_t)p.sink_tiles * p.sink_parts;
     const int64_t rest = (int64_t)(p.tiles - p.sink_tiles) * p.tile_parts;

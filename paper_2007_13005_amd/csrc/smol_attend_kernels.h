@@ -357,7 +357,9 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         return true;
     });
     loads_done();
-    // the waves' sums at one maximum, then waves 2 and 3 into 0 and 1, 1 into 0
+    // the waves' sums at one maximum, then waves 2 and 3 into 0 and 1, 1 into 0:
+    // of those that had a tile
+    const int32_t busy = hi - lo;
     const float half = both_halves(cols.l, [](float u, float v) { return u + v; });
     if (lane < 32) {
         tops[wave][lane] = cols.m;
@@ -379,6 +381,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     float *room = (float *)lds;
 #pragma unroll
     for (int step = 2; step >= 1; step >>= 1) {
+        if (busy <= step)
+            continue;
         if (wave >= step && wave < 2 * step)
 #pragma unroll
             for (int n = 0; n < N; ++n)
