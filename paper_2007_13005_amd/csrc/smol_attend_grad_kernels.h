@@ -234,8 +234,6 @@ struct KeySpan {
 // size.
 struct KeyTask {
     uint32_t pair, tile, part;
-    bool whole;  // the only part
-    int32_t begin, end;
     __device__ __forceinline__ KeyTask(const AttendArgs &a)
     {
         const uint32_t unit = divide(blockIdx.x, a.pair_div);
@@ -244,12 +242,10 @@ struct KeyTask {
         if (unit < first) {
             tile = divide(unit, a.sink_div);
             part = unit - tile * a.sink_div.d;
-            whole = a.sink_div.d == 1;
         } else {
             const uint32_t n = divide(unit - first, a.tile_div);
             tile = a.sink_tiles + n;
             part = unit - first - n * a.tile_div.d;
-            whole = a.tile_div.d == 1;
         }
     }
     __device__ __forceinline__ int32_t size(const AttendArgs &a) const
@@ -280,14 +276,15 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     const int32_t group = (int32_t)a.group.d, head0 = s.kv * group;
     const KeySpan span(a, s, j0, j0 + kKeys - 1);
     int32_t c_begin = span.begin, c_end = span.end;
-    if (!task.whole) {
-        const int32_t size = task.size(a);
+    const int32_t size = task.size(a);
+    const bool whole = c_end - c_begin <= size;  // one part, which may be empty
+    if (task.part) {
         const int64_t from = (int64_t)c_begin + (int64_t)task.part * size;
-        c_begin = from < c_end ? (int32_t)from : c_end;
-        c_end = c_end - c_begin < size ? c_end : c_begin + size;
-        if (c_begin >= c_end)
-            return;  // the join knows that this part is empty
+        if (from >= c_end)
+            return;  // the join knows that there is no such part
+        c_begin = (int32_t)from;
     }
+    c_end = c_end - c_begin < size ? c_end : c_begin + size;
     f32x16 dk[N], dv[N];
 #pragma unroll
     for (int n = 0; n < N; ++n)
@@ -515,7 +512,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     }
     const bool none = j >= s.k_length;
     const float fk = a.scale * kCarried<T>, fv = kCarried<T>;
-    if (!task.whole) {
+    if (!whole) {
         float *p = a.part + ((int64_t)blockIdx.x * 2 * kKeys + wave * 32 + (lane & 31)) * (N * 32);
         write_row<float, N>(p, nullptr, dk, fk, none, N * 32, lane);
         write_row<float, N>(p + kKeys * (N * 32), nullptr, dv, fv, none, N * 32, lane);
@@ -540,10 +537,10 @@ __global__ void __launch_bounds__(64 * kAttendWaves) attend_grad_join_kernel(Att
     const Sequence s(a, pair);
     const KeySpan span(a, s, tile * kKeys, tile * kKeys + kKeys - 1);
     const bool sink = tile < (uint32_t)a.sink_tiles;
-    if (sink && a.sink_div.d == 1)
-        return;  // its only part is written whole
     const int32_t size = sink ? a.sink_part : a.tile_part;
     const int32_t parts = (int32_t)(((int64_t)span.end - span.begin + size - 1) / size);
+    if (parts <= 1)
+        return;  // written whole
     // the first part's place among the workgroups' sums
     const int64_t first = sink ? (int64_t)tile * a.sink_div.d
                                : (int64_t)a.sink_tiles * a.sink_div.d +
