@@ -203,7 +203,7 @@ typedef struct smol_attend_shape {
     int32_t type;             /* of all matrices                               */
     int32_t causal;
     int32_t window, sinks;    /* >= 0; 0 unless causal                         */
-    float scale;              /* > 0, finite                                   */
+    float scale;              /* 2^-60 .. 2^60                                 */
     int32_t reserved;
 } smol_attend_shape;
 

@@ -39,6 +39,9 @@ int check_shape(const smol_attend_shape &s)
                          s.sinks);
     if (!(s.scale > 0.0f) || isinf(s.scale))
         return set_error(SMOL_ERR_INVALID_ARG, "scale is not positive and finite");
+    // (it and its inverse are factors of what is far from 1 too)
+    if (s.scale < 0x1p-60f || s.scale > 0x1p60f)
+        return set_error(SMOL_ERR_UNSUPPORTED, "scale %g is not within 2^-60 .. 2^60", s.scale);
     if (s.reserved)
         return set_error(SMOL_ERR_INVALID_ARG, "reserved field is not zero");
     if ((uintptr_t)s.q_lengths % 4 || (uintptr_t)s.k_lengths % 4)

@@ -135,6 +135,7 @@ ATTEND_SHAPE = [({f"shape__{k}": v for k, v in d.items()}, s) for d, s in [
     (dict(window=-1), INVALID), (dict(sinks=-1), INVALID), (dict(causal=0, window=4), INVALID),
     (dict(causal=0, sinks=4), INVALID), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID),
     (dict(scale=NAN), INVALID), (dict(scale=INF), INVALID), (dict(reserved=1), INVALID),
+    (dict(scale=8e-19), UNSUPPORTED), (dict(scale=1.2e18), UNSUPPORTED),
     (dict(q_lengths=AT + 2), INVALID), (dict(k_lengths=AT + 1), INVALID),
     (dict(dim=60), UNSUPPORTED), (dict(dim=136), UNSUPPORTED), (dict(batch=65537), UNSUPPORTED),
     (dict(queries=2 ** 24 + 1), UNSUPPORTED), (dict(keys=2 ** 24 + 1), UNSUPPORTED),

@@ -511,6 +511,53 @@ def test_attend_strides(dtype):
     assert torch.equal(same, attention.attend(dev(q), both, both)[0])
 
 
+@pytest.mark.parametrize("dim", [8, 24, 40, 72, 104])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_attend_gaps_hold_anything(dim, dtype):
+    """Heads with NaN between them, aligned (tiles then load as they are) and not,
+    give what dense ones give."""
+    note(f"attend gaps {dim} {dtype}")
+    for shape in ((2, 140, 150, 6, 2, dim, True, 60, 3), (3, 1, 333, 4, 2, dim, True, 0, 0)):
+        q, k, v, dy = inputs(shape, dtype, dim)
+        plain = attention.attend(dev(q), dev(k), dev(v), **mask(shape))
+        grads = attention.attend_backward(dev(dy), dev(q), dev(k), dev(v), *plain, **mask(shape))
+        for pad in (24, 3):
+            at = []
+            for t in (q, k, v, dy):
+                b, n, h, d = t.shape
+                buf = torch.full((b, n, h, d + pad), NAN, dtype=dtype, device="cuda")
+                at.append(buf[..., :d])
+                at[-1].copy_(t)
+            out, lse = attention.attend(*at[:3], **mask(shape))
+            assert torch.equal(out, plain[0]) and torch.equal(lse, plain[1])
+            got = attention.attend_backward(at[3], *at[:3], out, lse, **mask(shape))
+            for x, y in zip(got, grads):
+                assert torch.equal(x, y)
+
+
+def test_attend_parts_of_no_weight():
+    """A long cache taken in parts, of which some have no finite score."""
+    note("attend parts of no weight")
+    q, k, v, _ = inputs((1, 1, 3000, 1, 1, 16, True, 0, 0), BF16, 6)
+    q[..., 0] = 1.0
+    k[..., 0] = 0.0
+    k[:, 200:2100, :, 0] = -INF
+    keep = [j for j in range(3000) if not 200 <= j < 2100]
+    out, lse = attention.attend(dev(q), dev(k), dev(v))
+    (want, bound), (wl, bl) = ref.attend(q, k[:, keep], v[:, keep])
+    close(out, want, bound, "out")
+    close(lse, wl, bl, "lse")
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -60, 1e-9, 2.0 ** 60])
+def test_attend_extreme_scales(scale):
+    note(f"attend scale {scale}")
+    shape = (1, 40, 50, 2, 1, 16, True, 0, 0)
+    q, k, v, dy = inputs(shape, F32, 3)
+    q, k = (q, k) if scale < 1 else (q * 2.0 ** -30, k * 2.0 ** -30)
+    check(q, k, v, dy, f"scale {scale}", scale=scale)
+
+
 def test_attend_offsets_past_32_bits():
     """Rows of keys and values that far apart that offsets pass 2^31 elements."""
     note("attend far rows")
