@@ -37,7 +37,10 @@ struct AttendArgs {
     // gradients of keys: tiles of keys that hold sinks, and columns of a part of
     // these and of the other tiles (as many parts: the two divisors)
     int32_t sink_tiles, sink_part, tile_part;
+    uint32_t batch, delta_groups;  // rows that workgroups form D of
+    uint32_t key_groups;           // workgroups of keys: the first
     Divisor group, pair_div, kv_heads, tile_div, sink_div, split_div;
+    Divisor heads_div, queries_div;
 };
 
 constexpr int kAttendKeys = 64;     // of a tile that four waves share
@@ -47,10 +50,13 @@ constexpr int kAttendFewKeys = 32;  // of a tile of one wave (few columns)
 constexpr int kAttendSplits = 64;   // parts of the keys at most
 constexpr int kAttendJoinKeys = 4;  // of a workgroup that joins gradients of keys
 
+// Lanes that form a row's D, eight values each.
+constexpr int attend_delta_lanes(int wide) { return wide == 1 ? 4 : wide == 2 ? 8 : 16; }
+
 // Kernels: the forward pass with the waves over columns, or over keys (few
-// columns); the join of its splits; the gradients of queries, and of keys and
-// values; the join of the latter's parts.
-enum { kAttendMany, kAttendFew, kAttendJoin, kAttendGradQ, kAttendGradK, kAttendGradJoin };
+// columns); the join of its splits; the sums D of the backward pass; its gradients;
+// the join of the parts of those of keys.
+enum { kAttendMany, kAttendFew, kAttendJoin, kAttendDelta, kAttendGrad, kAttendGradJoin };
 
 // wide: values of a head in 32s, rounded up.
 int launch_attend_f32(const AttendArgs &a, int kernel, int wide, unsigned grid, void *s);

@@ -261,7 +261,7 @@ int check_workspace(const void *p, int64_t have, int64_t need)
 
 int launch(const AttendArgs &a, int kernel, int type, int dim, int64_t grid, void *s)
 {
-    const bool grad = kernel >= kAttendGradQ;
+    const bool grad = kernel >= kAttendDelta;
     const auto f = type == SMOL_ELEM_F32   ? grad ? launch_attend_grad_f32 : launch_attend_f32
                    : type == SMOL_ELEM_F16 ? grad ? launch_attend_grad_f16 : launch_attend_f16
                    : grad                  ? launch_attend_grad_bf16
@@ -368,7 +368,10 @@ extern "C" int smol_attend_backward(const smol_attend_grad_args *p, void *stream
     if ((st = check_workspace(p->workspace, p->workspace_bytes, grad_bytes(s))) != SMOL_OK)
         return st;
     const KeyParts parts = key_parts_of(s);
-    if (parts.groups > kMostGroups)
+    a.tiles = (int32_t)ceil_div(a.columns, kAttendColumns * kAttendWaves);
+    const int64_t key_groups = s.keys > 0 ? parts.groups : 0;
+    const int64_t groups = key_groups + (int64_t)a.tiles * a.pairs;
+    if (groups > kMostGroups)
         return set_error(SMOL_ERR_UNSUPPORTED, "too many rows and heads for a launch");
     // (keys of a workgroup; queries of 32 columns)
     a.direct_keys = near_keys(a.k, 128, s.dim, s.type) && near_keys(a.v, 128, s.dim, s.type);
@@ -377,26 +380,33 @@ extern "C" int smol_attend_backward(const smol_attend_grad_args *p, void *stream
     a.lse = (float *)p->lse;
     a.rest_in = p->rest;
     a.delta = (float *)p->workspace;
+    a.part = (float *)((char *)p->workspace + delta_bytes(s));
+    a.sink_tiles = parts.sink_tiles;
+    a.sink_part = parts.sink_part;
+    a.tile_part = parts.tile_part;
+    a.sink_div = make_divisor(parts.sink_parts);
+    a.tile_div = make_divisor(parts.tile_parts);
+    a.key_groups = (uint32_t)key_groups;
     int e = hipSuccess;
     if (s.queries > 0) {
-        a.tiles = (int32_t)ceil_div(a.columns, kAttendColumns * kAttendWaves);
-        e = launch(a, kAttendGradQ, s.type, s.dim, (int64_t)a.tiles * a.pairs, stream);
+        const int64_t lanes = attend_delta_lanes(wide_of(s.dim));
+        const int64_t delta_groups = ceil_div(
+            (int64_t)s.batch * s.queries * s.heads * lanes, 64 * kAttendWaves);
+        a.delta_groups = (uint32_t)delta_groups;
+        a.batch = s.batch;
+        a.heads_div = make_divisor(s.heads);
+        a.queries_div = make_divisor(s.queries);
+        e = launch(a, kAttendDelta, s.type, s.dim, std::min(delta_groups, kMostGroups), stream);
     }
-    if (e == hipSuccess && s.keys > 0) {
-        a.part = (float *)((char *)p->workspace + delta_bytes(s));
-        a.sink_tiles = parts.sink_tiles;
-        a.sink_part = parts.sink_part;
-        a.tile_part = parts.tile_part;
-        a.sink_div = make_divisor(parts.sink_parts);
-        a.tile_div = make_divisor(parts.tile_parts);
-        e = launch(a, kAttendGradK, s.type, s.dim, parts.groups, stream);
-        const int64_t joined = parts.tile_parts > 1   ? parts.tiles
-                               : parts.sink_parts > 1 ? parts.sink_tiles
-                                                      : 0;
-        if (e == hipSuccess && joined)
-            e = launch(a, kAttendGradJoin, s.type, s.dim,
-                       joined * (kAttendColumns * kAttendWaves / kAttendJoinKeys) * a.pairs, stream);
-    }
+    if (e == hipSuccess)
+        e = launch(a, kAttendGrad, s.type, s.dim, groups, stream);
+    const int64_t joined = s.keys == 0            ? 0
+                           : parts.tile_parts > 1 ? parts.tiles
+                           : parts.sink_parts > 1 ? parts.sink_tiles
+                                                  : 0;
+    if (e == hipSuccess && joined)
+        e = launch(a, kAttendGradJoin, s.type, s.dim,
+                   joined * (kAttendColumns * kAttendWaves / kAttendJoinKeys) * a.pairs, stream);
     if (e != hipSuccess)
         return set_error(SMOL_ERR_HIP, "attention backward launch: %s",
                          hipGetErrorString((hipError_t)e));

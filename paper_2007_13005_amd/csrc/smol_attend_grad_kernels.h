@@ -43,18 +43,55 @@ struct PairOf {
     }
 };
 
+// D of every row of queries that exists: a group of lanes a row, eight values a
+// lane.
+template <typename T, int N>
+__global__ void __launch_bounds__(64 * kAttendWaves) attend_delta_kernel(AttendArgs a)
+{
+    constexpr int kLanes = attend_delta_lanes(N);
+    const int32_t d = threadIdx.x % kLanes * 8;
+    for (uint32_t block = blockIdx.x; block < a.delta_groups; block += gridDim.x) {
+        const uint32_t r = block * (64 * kAttendWaves / kLanes) + threadIdx.x / kLanes;
+        const uint32_t row = divide(r, a.heads_div), b = divide(row, a.queries_div);
+        const int32_t head = r - row * a.heads_div.d, i = row - b * a.queries_div.d;
+        const bool some = b < a.batch;
+        float delta = 0.0f;
+        if (some && d < a.dim && (!a.q_lengths || i < a.q_lengths[b])) {
+            const auto at = [&](const HeadRows &m) {
+                return (const T *)m.p + b * m.batch + i * m.row + head * m.head + d;
+            };
+            vec<float, 8> y = to_f32<8, T>(load<T, 8>(at(a.out)));
+            const vec<float, 8> dy = to_f32<8, T>(load<T, 8>(at(a.dout)));
+            if (a.rest_in)
+                y += to_f32<8, T>(load<T, 8>((const T *)a.rest_in + (int64_t)r * a.dim + d));
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                delta = fmaf(dy[e], y[e], delta);
+        }
+#pragma unroll
+        for (int step = 1; step < kLanes; step <<= 1)
+            delta += __shfl_xor(delta, step);
+        if (some && d == 0)
+            a.delta[r] = delta;
+    }
+}
+
 // Gradients of queries: four waves of 32 columns over shared tiles of 64 keys.
 template <typename T, int N>
-__global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
-    attend_grad_q_kernel(AttendArgs a)
-{
-    constexpr int kKeys = kAttendKeys;
+struct GradQ {
+    static constexpr int kKeys = kAttendKeys;
     typedef LdsRows<T, N> Rows;
-    constexpr int kBytes = kKeys * Rows::kStride;
-    __shared__ __attribute__((aligned(512))) char lds[2][2 * kBytes];
+    static constexpr int kBytes = kKeys * Rows::kStride;
+    static constexpr int kLds = 4 * kBytes;
+    static __device__ __forceinline__ void run(const AttendArgs &a, uint32_t group, char *lds);
+};
+
+template <typename T, int N>
+__device__ __forceinline__ void GradQ<T, N>::run(const AttendArgs &a, uint32_t group, char *lds)
+{
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t turn = divide(blockIdx.x, a.pair_div);
-    const uint32_t pair = blockIdx.x - turn * a.pair_div.d;
+    const uint32_t turn = divide(group, a.pair_div);
+    const uint32_t pair = group - turn * a.pair_div.d;
     const uint32_t tile = a.causal ? a.tiles - 1 - turn : turn;
     const Sequence s(a, pair);
     const int32_t c0 = tile * (kAttendWaves * 32), mine = c0 + wave * 32;
@@ -69,27 +106,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     const T *dyp = s.rows<T>(a.dout, c.head) + c.i * a.dout.row;
     row_operands<T, N>(qp, a.dim, lane, q);
     row_operands<T, N>(dyp, a.dim, lane, dy);
-    float delta = 0.0f;
-    {
-        const T *op = s.rows<T>(a.out, c.head) + c.i * a.out.row;
-        const T *rp = a.rest_in ? (const T *)a.rest_in + at * a.dim : nullptr;
-#pragma unroll
-        for (int t = 0; t < 2 * N; ++t) {
-            const int32_t d = 16 * t + 8 * (lane >> 5);
-            if (d >= a.dim)
-                continue;
-            vec<float, 8> y = to_f32<8, T>(load<T, 8>(op + d));
-            if (rp)
-                y += to_f32<8, T>(load<T, 8>(rp + d));
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                delta = fmaf((float)dy[t][e], y[e], delta);
-        }
-        delta = both_halves(delta, [](float u, float v) { return u + v; });
-    }
     const float lse2 = sight.last < 0 ? 0.0f : a.lse[at] * kLog2e, minus_lse = kCarry<T> - lse2;
-    if (c.exists && lane < 32)
-        a.delta[at] = delta;
+    const float delta = sight.last < 0 ? 0.0f : a.delta[at];
     f32x16 sum[N];
 #pragma unroll
     for (int n = 0; n < N; ++n)
@@ -99,7 +117,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     const Moves k_moves(a.k.row, a.dim, wave, lane), v_moves(a.v.row, a.dim, wave, lane);
     const auto fetch = [&](int32_t n) {
         const int32_t j0 = walk.tile(n) * kKeys;
-        char *to = lds[n & 1];
+        char *to = lds + (n & 1) * (2 * kBytes);
         k_moves.fetch(kp, a.k.row, a.direct_keys, a.dim, to, wave, lane, j0, s.k_length);
         v_moves.fetch(vp, a.v.row, a.direct_keys, a.dim, to + kBytes, wave, lane, j0, s.k_length);
     };
@@ -125,10 +143,10 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
             const int part = k / kHalf, t = k % kHalf;
             if (part < 4)
                 ahead[k % kAhead] =
-                    Rows::row(lds[0] + (part & 1) * kBytes, row_at, (part >> 1) * 32, t);
+                    Rows::row(lds + (part & 1) * kBytes, row_at, (part >> 1) * 32, t);
             else if (part < 6)
                 ahead[k % kAhead] =
-                    Rows::column(lds[0], column_at, (part - 4) * 32 + t / N * 16, t % N);
+                    Rows::column(lds, column_at, (part - 4) * 32 + t / N * 16, t % N);
         };
         // scores start from minus infinity where a key is not seen, which leaves
         // weights of zero
@@ -234,10 +252,10 @@ struct KeySpan {
 // size.
 struct KeyTask {
     uint32_t pair, tile, part;
-    __device__ __forceinline__ KeyTask(const AttendArgs &a)
+    __device__ __forceinline__ KeyTask(const AttendArgs &a, uint32_t group)
     {
-        const uint32_t unit = divide(blockIdx.x, a.pair_div);
-        pair = blockIdx.x - unit * a.pair_div.d;
+        const uint32_t unit = divide(group, a.pair_div);
+        pair = group - unit * a.pair_div.d;
         const uint32_t first = a.sink_tiles * a.sink_div.d;
         if (unit < first) {
             tile = divide(unit, a.sink_div);
@@ -259,18 +277,27 @@ struct KeyTask {
 // them. Keys stay in registers and values in LDS, which leaves room for two waves
 // a SIMD.
 template <typename T, int N>
-__global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
-    attend_grad_k_kernel(AttendArgs a)
-{
-    constexpr int kCols = 32, kKeys = kAttendWaves * 32;
+struct GradK {
+    static constexpr int kCols = 32, kKeys = kAttendWaves * 32;
     typedef LdsRows<T, N> Rows;
-    constexpr int kBytes = kCols * Rows::kStride;
-    __shared__ __attribute__((aligned(512))) char lds[2][2 * kBytes];
-    __shared__ __attribute__((aligned(512))) char values[kKeys * Rows::kStride];
-    __shared__ __attribute__((aligned(16))) float lses[2][kCols], deltas[2][kCols];
-    __shared__ __attribute__((aligned(16))) int32_t lasts[2][kCols], firsts[2][kCols];
+    static constexpr int kBytes = kCols * Rows::kStride;
+    // one column's numbers, of two tiles
+    struct Stats {
+        float lses[2][kCols], deltas[2][kCols];
+        int32_t lasts[2][kCols], firsts[2][kCols];
+    };
+    static constexpr int kValues = 4 * kBytes, kStats = kValues + kKeys * Rows::kStride;
+    static constexpr int kLds = kStats + sizeof(Stats);
+    static __device__ __forceinline__ void run(const AttendArgs &a, uint32_t block, char *lds);
+};
+
+template <typename T, int N>
+__device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t block, char *lds)
+{
+    char *values = lds + kValues;
+    Stats &stats = *(Stats *)(lds + kStats);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const KeyTask task(a);
+    const KeyTask task(a, block);
     const Sequence s(a, task.pair);
     const int32_t j0 = task.tile * kKeys, mine = j0 + wave * 32, j = mine + (lane & 31);
     const int32_t group = (int32_t)a.group.d, head0 = s.kv * group;
@@ -323,7 +350,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         }
     };
     const auto fetch = [&](int32_t c0, int buffer) {
-        char *to = lds[buffer];
+        char *to = lds + buffer * (2 * kBytes);
         if (a.direct_rows) {
             const int32_t i0 = (int32_t)divide(c0, a.group);
             if (!whole_queries)
@@ -377,10 +404,10 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     int buffer = 0;
     for (int32_t c0 = c_begin; c0 < c_end; c0 += kCols, buffer ^= 1) {
         if (threadIdx.x < kCols) {
-            lses[buffer][threadIdx.x] = m_lse;
-            deltas[buffer][threadIdx.x] = m_delta;
-            lasts[buffer][threadIdx.x] = m_last;
-            firsts[buffer][threadIdx.x] = m_first;
+            stats.lses[buffer][threadIdx.x] = m_lse;
+            stats.deltas[buffer][threadIdx.x] = m_delta;
+            stats.lasts[buffer][threadIdx.x] = m_last;
+            stats.firsts[buffer][threadIdx.x] = m_first;
         }
         // the tile is there, for all waves; the other buffer's tile has been used by all
         loads_done();
@@ -408,9 +435,9 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         const auto read = [&](int k) {
             const int part = k / kHalf, t = k % kHalf;
             if (part < 2)
-                ahead[k % kAhead] = Rows::row(lds[0] + part * kBytes, row_at, 0, t);
+                ahead[k % kAhead] = Rows::row(lds + part * kBytes, row_at, 0, t);
             else if (part < 4)
-                ahead[k % kAhead] = Rows::column(lds[0] + (3 - part) * kBytes, column_at,
+                ahead[k % kAhead] = Rows::column(lds + (3 - part) * kBytes, column_at,
                                                  t / N * 16, t % N);
         };
         const auto read_v = [&](int t) {
@@ -421,8 +448,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int r = 8 * g + 4 * (lane >> 5);
-            const f32x4 l4 = *(const f32x4 *)&lses[buffer][r];
-            const f32x4 d4 = *(const f32x4 *)&deltas[buffer][r];
+            const f32x4 l4 = *(const f32x4 *)&stats.lses[buffer][r];
+            const f32x4 d4 = *(const f32x4 *)&stats.deltas[buffer][r];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 x[4 * g + e] = l4[e];
@@ -430,8 +457,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
             }
             if (!whole) {
                 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-                const i32x4 last = *(const i32x4 *)&lasts[buffer][r];
-                const i32x4 first = *(const i32x4 *)&firsts[buffer][r];
+                const i32x4 last = *(const i32x4 *)&stats.lasts[buffer][r];
+                const i32x4 first = *(const i32x4 *)&stats.firsts[buffer][r];
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     x[4 * g + e] = sees(j, last[e], first[e], a.sinks) ? x[4 * g + e] : -INFINITY;
@@ -513,7 +540,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     const bool none = j >= s.k_length;
     const float fk = a.scale * kCarried<T>, fv = kCarried<T>;
     if (!whole) {
-        float *p = a.part + ((int64_t)blockIdx.x * 2 * kKeys + wave * 32 + (lane & 31)) * (N * 32);
+        float *p = a.part + ((int64_t)block * 2 * kKeys + wave * 32 + (lane & 31)) * (N * 32);
         write_row<float, N>(p, nullptr, dk, fk, none, N * 32, lane);
         write_row<float, N>(p + kKeys * (N * 32), nullptr, dv, fv, none, N * 32, lane);
         return;
@@ -522,6 +549,22 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         return;
     write_row<T, N>((T *)s.rows<T>(a.dk, s.kv) + j * a.dk.row, nullptr, dk, fk, none, a.dim, lane);
     write_row<T, N>((T *)s.rows<T>(a.dv, s.kv) + j * a.dv.row, nullptr, dv, fv, none, a.dim, lane);
+}
+
+// Workgroups of keys, then those of queries: either's last run beside the other's.
+template <typename T, int N>
+__global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
+    attend_grad_kernel(AttendArgs a)
+{
+    typedef GradK<T, N> Keys;
+    typedef GradQ<T, N> Queries;
+    __shared__ __attribute__((aligned(
+        512))) char lds[Keys::kLds > Queries::kLds ? Keys::kLds : Queries::kLds];
+    const uint32_t block = blockIdx.x;
+    if (block < a.key_groups)
+        Keys::run(a, block, lds);
+    else
+        Queries::run(a, block - a.key_groups, lds);
 }
 
 // Joins the parts of the keys' gradients, in order: four keys a workgroup, four
@@ -568,10 +611,10 @@ int launch_attend_grad(const AttendArgs &a, int kernel, int wide, unsigned grid,
         constexpr int N = decltype(n)::value;
         const dim3 g(grid), b(64 * kAttendWaves);
         hipStream_t st = (hipStream_t)s;
-        if (kernel == kAttendGradQ)
-            hipLaunchKernelGGL((attend_grad_q_kernel<T, N>), g, b, 0, st, a);
-        else if (kernel == kAttendGradK)
-            hipLaunchKernelGGL((attend_grad_k_kernel<T, N>), g, b, 0, st, a);
+        if (kernel == kAttendDelta)
+            hipLaunchKernelGGL((attend_delta_kernel<T, N>), g, b, 0, st, a);
+        else if (kernel == kAttendGrad)
+            hipLaunchKernelGGL((attend_grad_kernel<T, N>), g, b, 0, st, a);
         else
             hipLaunchKernelGGL((attend_grad_join_kernel<T, N>), g, b, 0, st, a);
     };
