@@ -48,6 +48,7 @@ constexpr int kAttendColumns = 32;  // of a wave
 constexpr int kAttendWaves = 4;     // of a workgroup
 constexpr int kAttendFewKeys = 32;  // of a tile of one wave (few columns)
 constexpr int kAttendSplits = 64;   // parts of the keys at most
+constexpr int kAttendJoinParts = 16;  // that a wave joins
 constexpr int kAttendJoinKeys = 4;  // of a workgroup that joins gradients of keys
 
 // Lanes that form a row's D, eight values each.

@@ -64,6 +64,14 @@ int check_shape(const smol_attend_shape &s)
     return SMOL_OK;
 }
 
+// Parts of the keys make a workgroup a compute unit (two, where that kernel holds
+// two: 28.4 -> 29.7 us for one token over 32768 keys of 8 heads of 128 in fp16, 32
+// -> 42 for four over 3000 in fp32, the sums of all parts being written and read;
+// 64 tokens over 8192 25 -> 30). A part has 128 keys or more (256: a token over
+// 1000 keys 11.2 -> 12.3 us), and up to 512 keys stay whole: the join takes 3 to 4
+// us (300 keys: 10.1 us whole, 11 to 12 in parts; 600: 12.6 and 11.2).
+constexpr int64_t kSplitGroups = 256, kSplitKeys = 128, kWholeKeys = 512;
+
 // How the forward pass is split.
 struct Split {
     bool few;
@@ -78,13 +86,14 @@ Split split_of(const smol_attend_shape &s)
     // a tile of columns that one wave holds: the waves then share the keys
     p.few = columns <= kAttendColumns;
     p.tiles = (int32_t)ceil_div(columns, p.few ? kAttendColumns : kAttendColumns * kAttendWaves);
-    // two workgroups a compute unit, each with 256 keys or more
     int64_t keys = s.keys;
     if (s.causal && s.window)
         keys = std::min<int64_t>(keys, (int64_t)s.window + s.sinks + s.queries);
     const int64_t groups = std::max<int64_t>(1, p.tiles * pairs);
-    int64_t splits = std::min<int64_t>(512 / groups, ceil_div(keys, 256));
+    int64_t splits = std::min<int64_t>(kSplitGroups / groups, ceil_div(keys, kSplitKeys));
     splits = std::max<int64_t>(1, std::min<int64_t>(splits, kAttendSplits));
+    if (keys <= kWholeKeys)
+        splits = 1;
     p.splits = (int32_t)splits;
     return p;
 }
@@ -327,7 +336,11 @@ extern "C" int smol_attend(const smol_attend_args *p, void *stream)
     int e = launch(a, split.few ? kAttendFew : kAttendMany, s.type, s.dim,
                    (int64_t)split.tiles * a.pairs * split.splits, stream);
     if (e == hipSuccess && split.splits > 1)
-        e = launch(a, kAttendJoin, s.type, s.dim, (int64_t)a.pairs * a.columns, stream);
+        e = launch(a, kAttendJoin, s.type, s.dim,
+                   split.splits <= kAttendJoinParts
+                       ? ceil_div((int64_t)a.pairs * a.columns, kAttendWaves)
+                       : (int64_t)a.pairs * a.columns,
+                   stream);
     if (e != hipSuccess)
         return set_error(SMOL_ERR_HIP, "attention launch: %s", hipGetErrorString((hipError_t)e));
     return SMOL_OK;

@@ -404,31 +404,39 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     cols.finish(late, s, c0, task.pair, task.split, lane);
 }
 
-// Joins the parts of the keys: a workgroup a column, each wave a quarter of the
-// parts in order (all their loads at once), then the four waves' sums in order.
+// Joins the parts of the keys: a wave a column, all its parts' loads at once; past
+// 16 parts a workgroup a column, each wave a quarter of the parts in order, then
+// the four waves' sums in order.
 template <typename T, int N>
 __global__ void __launch_bounds__(64 * kAttendWaves) attend_join_kernel(AttendArgs a)
 {
-    constexpr int kParts = kAttendSplits / kAttendWaves;
+    constexpr int kParts = kAttendJoinParts;
+    static_assert(kAttendSplits <= kParts * kAttendWaves, "parts that the waves hold");
     __shared__ Spread quarter[kAttendWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t pair = blockIdx.x / (uint32_t)a.columns;
+    const bool alone = a.splits <= kParts;
+    const uint32_t at = alone ? blockIdx.x * kAttendWaves + wave : blockIdx.x;
+    const uint32_t rows = (uint32_t)a.pairs * (uint32_t)a.columns;  // of a part
+    if (at >= rows)
+        return;
+    const uint32_t pair = at / (uint32_t)a.columns;
     const Sequence s(a, pair);
-    const Column c(a, s, (int32_t)(blockIdx.x - pair * (uint32_t)a.columns));
-    const int64_t rows = (int64_t)a.pairs * a.columns;
-    const int per = (a.splits + kAttendWaves - 1) / kAttendWaves;
-    const float *p = a.part + (wave * per * rows + blockIdx.x) * (N * 32);
+    const Column c(a, s, (int32_t)(at - pair * (uint32_t)a.columns));
+    const int per = alone ? a.splits : (a.splits + kAttendWaves - 1) / kAttendWaves;
+    const int first = alone ? 0 : wave * per;
+    const float *p = a.part + ((int64_t)first * rows + at) * (N * 32);
     Spread x[kParts];
 #pragma unroll
     for (int k = 0; k < kParts; ++k) {
-        const bool own = k < per && wave * per + k < a.splits;
-        const float *at = p + k * rows * (N * 32);
-        x[k].x = own && lane < N * 32 ? at[lane] : 0.0f;
-        x[k].y = own && lane + 64 < N * 32 ? at[lane + 64] : 0.0f;
+        const bool own = k < per && first + k < a.splits;
+        const float *from = p + (int64_t)k * rows * (N * 32);
+        x[k].x = own && lane < N * 32 ? from[lane] : 0.0f;
+        x[k].y = own && lane + 64 < N * 32 ? from[lane + 64] : 0.0f;
     }
-    const float *ml = a.part + (int64_t)a.splits * rows * (N * 32) + 2 * (int64_t)blockIdx.x;
+    const float *ml = a.part + (int64_t)a.splits * rows * (N * 32) + 2 * (int64_t)at;
     const bool own = lane < a.splits;  // splits <= 64
-    const float m = own ? ml[2 * lane * rows] : kLowest, l = own ? ml[2 * lane * rows + 1] : 0.0f;
+    const float m = own ? ml[2 * (int64_t)lane * rows] : kLowest;
+    const float l = own ? ml[2 * (int64_t)lane * rows + 1] : 0.0f;
     float top = m;
 #pragma unroll
     for (int step = 32; step; step >>= 1)
@@ -439,18 +447,20 @@ __global__ void __launch_bounds__(64 * kAttendWaves) attend_join_kernel(AttendAr
 #pragma unroll
     for (int k = 0; k < kParts; ++k)
         if (k < per) {
-            const float w = __shfl(f, (wave * per + k) & 63);
+            const float w = __shfl(f, (first + k) & 63);
             y.x = fmaf(w, x[k].x, y.x);
             y.y = fmaf(w, x[k].y, y.y);
         }
-    quarter[wave][lane] = y;
-    __syncthreads();
-    if (wave != 0)
-        return;
+    if (!alone) {
+        quarter[wave][lane] = y;
+        __syncthreads();
+        if (wave != 0)
+            return;
 #pragma unroll
-    for (int w = 1; w < kAttendWaves; ++w) {
-        y.x += quarter[w][lane].x;
-        y.y += quarter[w][lane].y;
+        for (int w = 1; w < kAttendWaves; ++w) {
+            y.x += quarter[w][lane].x;
+            y.y += quarter[w][lane].y;
+        }
     }
     const bool none = s.last(a, c.i) < 0;
     const float inv = 1.0f / total;

@@ -294,6 +294,8 @@ SHAPES = [
     (1, 4, 1000, 12, 4, 120, False, 0, 0),
     (1, 30, 2100, 4, 1, 64, True, 0, 0),
     (1, 12, 40, 1, 1, 104, True, 100, 4),   # a window past all keys
+    (1, 2, 5000, 4, 1, 72, True, 0, 0),     # the most parts of keys
+    (2, 70, 1100, 2, 1, 96, False, 0, 0),
 ]
 
 
