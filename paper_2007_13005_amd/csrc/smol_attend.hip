@@ -109,10 +109,11 @@ int64_t part_bytes(const smol_attend_shape &s, const Split &p)
 }
 
 // Parts of the columns of the keys' gradients. They make two workgroups a compute
-// unit; a part has at least 128 columns (against 512: 1 x 399 rows of 14 heads
-// of 128 over 2 keys' 52 -> 42 us, 2 x 148 of 16 of 80 over 4 31 -> 24), one of a
-// tile of sinks 512, as the others' workgroups run along (18 x 4422 rows of a head
-// of 128, a window of 15: 92 us against 100 with 256).
+// unit (four: 4 ragged sequences of 4096 rows 397 -> 443 us, as parts' sums are
+// written and read; one: 5906 rows of 8 heads of 96 287 -> 551). A part has 128
+// columns or more (512: 1 x 399 rows of 14 heads of 128 over 2 42 -> 52 us, 2 x 148
+// of 16 of 80 over 4 24 -> 31), one of a tile of sinks 512, as the others' workgroups
+// run beside it (256: 18 x 4422 rows of a head of 128, a window of 15, 92 -> 100).
 constexpr int64_t kTileGroups = 512, kSinkGroups = 256;  // workgroups that parts make
 constexpr int64_t kKeyParts = 64;                        // of a tile at most
 constexpr int64_t kLeastColumns = 128, kLeastSinkColumns = 512;
