@@ -15,7 +15,9 @@
  *     consecutive elements within a head; rows and heads have a stride of
  *     their own in elements, so queries, keys and values may stand beside each
  *     other in one projection's rows. A stride of 0 lets one row or head of
- *     an input stand for all. No two heads of an output may overlap.
+ *     an input stand for all. No two heads of an output may overlap; an
+ *     output that begins where another matrix of the call does is refused
+ *     unless the call says that it may (then with the same strides).
  */
 #ifndef SMOL_ATTENTION_H
 #define SMOL_ATTENTION_H

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "smol.h"
 #include "smol_attend.h"
@@ -269,6 +270,17 @@ int check_workspace(const void *p, int64_t have, int64_t need)
     return SMOL_OK;
 }
 
+// Whether any of the written matrices stands where another of all does.
+int check_apart(std::initializer_list<const void *> written,
+                std::initializer_list<const void *> read)
+{
+    for (auto w = written.begin(); w != written.end(); ++w)
+        if (*w && (std::find(w + 1, written.end(), *w) != written.end() ||
+                   std::find(read.begin(), read.end(), *w) != read.end()))
+            return set_error(SMOL_ERR_INVALID_ARG, "an output stands where another matrix does");
+    return SMOL_OK;
+}
+
 int launch(const AttendArgs &a, int kernel, int type, int dim, int64_t grid, void *s)
 {
     const bool grad = kernel >= kAttendDelta;
@@ -323,7 +335,11 @@ extern "C" int smol_attend(const smol_attend_args *p, void *stream)
     if ((uintptr_t)p->lse % 4 || (uintptr_t)p->rest % elem_size(s.type))
         return set_error(SMOL_ERR_INVALID_ARG, "lse or rest is not aligned to its elements");
     const Split split = split_of(s);
-    if ((st = check_workspace(p->workspace, p->workspace_bytes, part_bytes(s, split))) != SMOL_OK)
+    if ((st = check_workspace(p->workspace, p->workspace_bytes, part_bytes(s, split))) !=
+            SMOL_OK ||
+        (st = check_apart({p->out.data, p->lse, p->rest},
+                          {p->q.data, s.keys ? p->k.data : nullptr,
+                           s.keys ? p->v.data : nullptr})) != SMOL_OK)
         return st;
     a.direct_keys = near_keys(a.k, kAttendKeys, s.dim, s.type) &&
                     near_keys(a.v, kAttendKeys, s.dim, s.type);
@@ -379,7 +395,13 @@ extern "C" int smol_attend_backward(const smol_attend_grad_args *p, void *stream
         return set_error(SMOL_ERR_INVALID_ARG, "lse is NULL or not aligned to its elements");
     if ((uintptr_t)p->rest % elem_size(s.type))
         return set_error(SMOL_ERR_INVALID_ARG, "rest is not aligned to its elements");
-    if ((st = check_workspace(p->workspace, p->workspace_bytes, grad_bytes(s))) != SMOL_OK)
+    const auto of = [](int32_t rows, const void *x) { return rows ? x : nullptr; };
+    if ((st = check_workspace(p->workspace, p->workspace_bytes, grad_bytes(s))) != SMOL_OK ||
+        (st = check_apart({of(s.queries, p->grad_q.data), of(s.keys, p->grad_k.data),
+                           of(s.keys, p->grad_v.data)},
+                          {of(s.queries, p->grad_out.data), of(s.queries, p->q.data),
+                           of(s.keys, p->k.data), of(s.keys, p->v.data),
+                           of(s.queries, p->out.data), p->rest, p->lse})) != SMOL_OK)
         return st;
     const KeyParts parts = key_parts_of(s);
     a.tiles = (int32_t)ceil_div(a.columns, kAttendColumns * kAttendWaves);

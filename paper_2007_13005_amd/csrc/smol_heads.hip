@@ -149,6 +149,15 @@ int check_heads(const char *name, const void *p, int64_t rows, int32_t heads, in
     return SMOL_OK;
 }
 
+// An output that stands where an input does has its strides.
+int check_in_place(const void *out, int64_t out_row, int64_t out_head, const void *in,
+                   int64_t in_row, int64_t in_head, int64_t rows, int32_t heads)
+{
+    if (out == in && ((rows > 1 && out_row != in_row) || (heads > 1 && out_head != in_head)))
+        return set_error(SMOL_ERR_INVALID_ARG, "strides of a call in place differ");
+    return SMOL_OK;
+}
+
 int check_sizes(int64_t rows, int32_t dim, int32_t rot, int32_t type, int32_t positions_type,
                 int32_t interleaved)
 {
@@ -219,7 +228,9 @@ int rotate(const smol_rotate_args *p, bool backward, void *stream)
         (st = check_heads("x", p->x, p->rows, p->heads, p->dim, p->x_row_stride,
                           p->x_head_stride, false, p->type)) != SMOL_OK ||
         (st = check_heads("out", p->out, p->rows, p->heads, p->dim, p->out_row_stride,
-                          p->out_head_stride, true, p->type)) != SMOL_OK)
+                          p->out_head_stride, true, p->type)) != SMOL_OK ||
+        (st = check_in_place(p->out, p->out_row_stride, p->out_head_stride, p->x,
+                             p->x_row_stride, p->x_head_stride, p->rows, p->heads)) != SMOL_OK)
         return st;
     HeadArgs a = {};
     HeadForm f = {};
@@ -366,6 +377,9 @@ extern "C" int smol_head_norm(const smol_head_norm_args *p, void *stream)
                               in.x_head_stride, false, s.type)) != SMOL_OK ||
             (st = check_heads(names[k][1], in.out, s.rows, in.heads, s.dim, in.out_row_stride,
                               in.out_head_stride, true, s.type)) != SMOL_OK ||
+            (st = check_in_place(in.out, in.out_row_stride, in.out_head_stride, in.x,
+                                 in.x_row_stride, in.x_head_stride, s.rows, in.heads)) !=
+                SMOL_OK ||
             (st = check_small_vector(names[k][2], in.weight, s.weight_type)) != SMOL_OK)
             return st;
         HeadSide &to = a.side[k];
@@ -380,6 +394,9 @@ extern "C" int smol_head_norm(const smol_head_norm_args *p, void *stream)
     }
     if (s.rows == 0 || p->q.heads + p->k.heads == 0)
         return SMOL_OK;
+    if (p->q.heads && p->k.heads &&
+        (p->q.out == p->k.out || p->q.out == p->k.x || p->k.out == p->q.x))
+        return set_error(SMOL_ERR_INVALID_ARG, "an output of q stands where one of k does");
     fill_shape(&a, &f, s);
     a.sign = 1.0f;
     plan(&a, &f, s.type);
@@ -435,6 +452,12 @@ extern "C" int smol_head_norm_backward(const smol_head_norm_grad_args *p, void *
             (st = check_heads(names[k][2], in.grad_x, s.rows, in.heads, s.dim,
                               in.grad_x_row_stride, in.grad_x_head_stride, true, s.type)) !=
                 SMOL_OK ||
+            (st = check_in_place(in.grad_x, in.grad_x_row_stride, in.grad_x_head_stride, in.x,
+                                 in.x_row_stride, in.x_head_stride, s.rows, in.heads)) !=
+                SMOL_OK ||
+            (st = check_in_place(in.grad_x, in.grad_x_row_stride, in.grad_x_head_stride,
+                                 in.grad_out, in.grad_out_row_stride, in.grad_out_head_stride,
+                                 s.rows, in.heads)) != SMOL_OK ||
             (st = check_small_vector(names[k][3], in.weight, s.weight_type)) != SMOL_OK)
             return st;
         HeadSide &to = a.side[k];
@@ -455,6 +478,12 @@ extern "C" int smol_head_norm_backward(const smol_head_norm_grad_args *p, void *
         return set_error(SMOL_ERR_INVALID_ARG,
                          "workspace must be 16-byte aligned and hold %lld bytes",
                          (long long)need);
+    const auto &q = p->q, &k = p->k;
+    if ((q.grad_weight && q.grad_weight == k.grad_weight) ||
+        (s.rows > 0 && q.heads && k.heads &&
+         (q.grad_x == k.grad_x || q.grad_x == k.x || q.grad_x == k.grad_out ||
+          k.grad_x == q.x || k.grad_x == q.grad_out)))
+        return set_error(SMOL_ERR_INVALID_ARG, "a gradient of q stands where one of k does");
     a.part = (float *)p->workspace;
     int e = hipSuccess;
     if (s.rows > 0 && p->q.heads + p->k.heads > 0) {

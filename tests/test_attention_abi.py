@@ -80,7 +80,8 @@ CALLS["smol_rotate_backward"] = CALLS["smol_rotate"]
 
 def call(name: str, **fields) -> int:
     fields = {k.replace("__", "."): v for k, v in fields.items()}
-    values = {k: v for k, _, v in CALLS[name][1]}
+    # every address its own
+    values = {k: v + (n << 24) if v == AT else v for n, (k, _, v) in enumerate(CALLS[name][1])}
     assert set(fields) <= set(values), set(fields) - set(values)
     values.update(fields)
     packed = struct.pack("".join(letter for _, letter, _ in CALLS[name][1]), *values.values())
@@ -171,6 +172,43 @@ BAD = {
     of_matrix("grad_v", True, 2, 16) + [(dict(lse=0), INVALID), (dict(lse=AT + 2), INVALID),
                                         (dict(rest=AT + 1), INVALID)],
 }
+
+
+SAME = {
+    "smol_head_norm": [("q.out", "k.out"), ("q.out", "k.x"), ("k.out", "q.x")],
+    "smol_head_norm_backward": [("q.grad_x", "k.grad_x"), ("q.grad_x", "k.x"),
+                                ("q.grad_x", "k.grad_out"), ("k.grad_x", "q.x"),
+                                ("k.grad_x", "q.grad_out"), ("q.grad_weight", "k.grad_weight")],
+    "smol_attend": [("out.data", f"{k}.data") for k in "qkv"] + [("lse", "q.data"),
+                                                                 ("rest", "out.data")],
+    "smol_attend_backward": [(f"grad_{a}.data", b) for a in "qkv" for b in (
+        "q.data", "k.data", "v.data", "out.data", "grad_out.data", "lse")] + [
+        ("grad_q.data", "grad_k.data"), ("grad_q.data", "grad_v.data"),
+        ("grad_k.data", "grad_v.data")],
+}
+
+
+@pytest.mark.parametrize("name", sorted(SAME))
+def test_outputs_stand_apart(name):
+    for written, other in SAME[name]:
+        assert call(name, **{written: AT, other: AT}) == INVALID, (name, written, other)
+        assert b"stands where" in smol.lib().smol_last_error(), (name, written, other)
+
+
+IN_PLACE = {
+    "smol_rotate": [("x", "out", "out")], "smol_rotate_backward": [("x", "out", "out")],
+    "smol_head_norm": [("q.x", "q.out", "q.out"), ("k.x", "k.out", "k.x")],
+    "smol_head_norm_backward": [("q.x", "q.grad_x", "q.x"), ("k.grad_out", "k.grad_x", "k.grad_x")],
+}
+
+
+@pytest.mark.parametrize("name", sorted(IN_PLACE))
+def test_in_place_means_the_same_strides(name):
+    for read, written, strides in IN_PLACE[name]:
+        for stride, value in (("row_stride", 320), ("head_stride", 2560)):
+            change = {read: AT, written: AT, f"{strides}_{stride}": value}
+            assert call(name, **change) == INVALID, (name, change)
+            assert b"in place" in smol.lib().smol_last_error(), (name, change)
 
 
 @pytest.mark.parametrize("name", sorted(BAD))
