@@ -38,7 +38,9 @@ struct AttendArgs {
     // these and of the other tiles (as many parts: the two divisors)
     int32_t sink_tiles, sink_part, tile_part;
     uint32_t batch, delta_groups;  // rows that workgroups form D of
-    uint32_t key_groups;           // workgroups of keys: the first
+    uint32_t key_units;            // workgroups of a pair's keys: its first
+    // pairs of a chunk, of the last one, and a chunk's workgroups
+    Divisor chunk, chunk_last, chunk_groups;
     Divisor group, pair_div, kv_heads, tile_div, sink_div, split_div;
     Divisor heads_div, queries_div;
 };

@@ -220,6 +220,25 @@ struct Sequence {
     }
 };
 
+// A workgroup's sequence and key head (a pair), and which of the pair's workgroups it
+// is. Pairs come in chunks whose workgroups run at the same time, so that what a
+// pair's share is read from memory once; within a chunk all pairs' first workgroups
+// come first, those of a pair a multiple of 8 apart and so on one XCD with one L2.
+struct Place {
+    uint32_t pair, unit;
+    __device__ __forceinline__ Place(const AttendArgs &a, uint32_t block)
+    {
+        const uint32_t n = divide(block, a.chunk_groups), p0 = n * a.chunk.d;
+        block -= n * a.chunk_groups.d;
+        const bool whole = p0 + a.chunk.d <= (uint32_t)a.pairs;
+        const Divisor pairs = {whole ? a.chunk.d : a.chunk_last.d,
+                               whole ? a.chunk.m : a.chunk_last.m,
+                               whole ? a.chunk.s : a.chunk_last.s};
+        unit = divide(block, pairs);
+        pair = p0 + block - unit * pairs.d;
+    }
+};
+
 __device__ __forceinline__ bool sees(int32_t j, int32_t last, int32_t first, int32_t sinks)
 {
     return j <= last && (j >= first || j < sinks);

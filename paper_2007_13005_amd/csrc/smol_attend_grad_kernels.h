@@ -88,15 +88,15 @@ struct GradQ {
     typedef LdsRows<T, N> Rows;
     static constexpr int kBytes = kKeys * Rows::kStride;
     static constexpr int kLds = 4 * kBytes;
-    static __device__ __forceinline__ void run(const AttendArgs &a, uint32_t group, char *lds);
+    static __device__ __forceinline__ void run(const AttendArgs &a, uint32_t pair, uint32_t turn,
+                                               char *lds);
 };
 
 template <typename T, int N>
-__device__ __forceinline__ void GradQ<T, N>::run(const AttendArgs &a, uint32_t group, char *lds)
+__device__ __forceinline__ void GradQ<T, N>::run(const AttendArgs &a, uint32_t pair, uint32_t turn,
+                                                 char *lds)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t turn = divide(group, a.pair_div);
-    const uint32_t pair = group - turn * a.pair_div.d;
     const uint32_t tile = a.causal ? a.tiles - 1 - turn : turn;
     const Sequence s(a, pair);
     const int32_t c0 = tile * (kAttendWaves * 32), mine = c0 + wave * 32;
@@ -256,11 +256,9 @@ struct KeySpan {
 // all later queries see them, so they have most columns, and parts of their own
 // size.
 struct KeyTask {
-    uint32_t pair, tile, part;
-    __device__ __forceinline__ KeyTask(const AttendArgs &a, uint32_t group)
+    uint32_t tile, part;
+    __device__ __forceinline__ KeyTask(const AttendArgs &a, uint32_t unit)
     {
-        const uint32_t unit = divide(group, a.pair_div);
-        pair = group - unit * a.pair_div.d;
         const uint32_t first = a.sink_tiles * a.sink_div.d;
         if (unit < first) {
             tile = divide(unit, a.sink_div);
@@ -294,17 +292,19 @@ struct GradK {
     };
     static constexpr int kValues = 4 * kBytes, kStats = kValues + kKeys * Rows::kStride;
     static constexpr int kLds = kStats + sizeof(Stats);
-    static __device__ __forceinline__ void run(const AttendArgs &a, uint32_t block, char *lds);
+    static __device__ __forceinline__ void run(const AttendArgs &a, uint32_t pair, uint32_t unit,
+                                               char *lds);
 };
 
 template <typename T, int N>
-__device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t block, char *lds)
+__device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t pair, uint32_t unit,
+                                                 char *lds)
 {
     char *values = lds + kValues;
     Stats &stats = *(Stats *)(lds + kStats);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const KeyTask task(a, block);
-    const Sequence s(a, task.pair);
+    const KeyTask task(a, unit);
+    const Sequence s(a, pair);
     const int32_t j0 = task.tile * kKeys, mine = j0 + wave * 32, j = mine + (lane & 31);
     const int32_t group = (int32_t)a.group.d, head0 = s.kv * group;
     const KeySpan span(a, s, j0, j0 + kKeys - 1);
@@ -546,7 +546,9 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t b
     const bool none = j >= s.k_length;
     const float fk = a.scale * kCarried<T>, fv = kCarried<T>;
     if (!whole) {
-        float *p = a.part + ((int64_t)block * 2 * kKeys + wave * 32 + (lane & 31)) * (N * 32);
+        const Place at(args_again(), blockIdx.x);  // (in fewer registers than kept)
+        const int64_t place = (int64_t)at.unit * a.pairs + at.pair;
+        float *p = a.part + (place * 2 * kKeys + wave * 32 + (lane & 31)) * (N * 32);
         write_row<float, N>(p, nullptr, dk, fk, none, N * 32, lane);
         write_row<float, N>(p + kKeys * (N * 32), nullptr, dv, fv, none, N * 32, lane);
         return;
@@ -570,11 +572,11 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     typedef GradQ<T, N> Queries;
     __shared__ __attribute__((aligned(
         512))) char lds[Keys::kLds > Queries::kLds ? Keys::kLds : Queries::kLds];
-    const uint32_t block = blockIdx.x;
-    if (block < a.key_groups)
-        Keys::run(a, block, lds);
+    const Place at(a, blockIdx.x);
+    if (at.unit < a.key_units)
+        Keys::run(a, at.pair, at.unit, lds);
     else
-        Queries::run(a, block - a.key_groups, lds);
+        Queries::run(a, at.pair, at.unit - a.key_units, lds);
 }
 
 // Joins the parts of the keys' gradients, in order: four keys a workgroup, four

@@ -155,10 +155,10 @@ struct Task {
     uint32_t pair, tile, split;
     __device__ __forceinline__ Task(const AttendArgs &a)
     {
-        const uint32_t rest = divide(blockIdx.x, a.pair_div);
-        pair = blockIdx.x - rest * a.pair_div.d;
-        split = divide(rest, a.tile_div);
-        tile = rest - split * a.tile_div.d;
+        const Place at(a, blockIdx.x);
+        pair = at.pair;
+        split = divide(at.unit, a.tile_div);
+        tile = at.unit - split * a.tile_div.d;
         if (a.causal)
             tile = a.tiles - 1 - tile;
     }
@@ -168,9 +168,9 @@ struct Task {
 //
 // Bound by the matrix instructions with the exponentials beside them: each 32 x 32
 // scores need d / 8 instructions for both products, and 16 exponentials a lane. So a
-// wave's tile of 64 keys is two halves, and one half's
-// exponentials stand between the other's products; operands are read from LDS a few
-// instructions ahead; the next tile is on its way to LDS while this one is used.
+// wave's tile of 64 keys is two halves, and one half's exponentials stand between the
+// other's products; operands are read from LDS a few instructions ahead; the next
+// tile is on its way to LDS while this one is used.
 // 8192 tokens, 32 heads of 128 over 8, a window of 2048, bf16: 268 us, 900 TFLOP/s of
 // the scores that are seen (products alone 138, with the softmax 209, with LDS reads
 // 233). Three buffers of tiles instead of two left too little LDS: 64 images of 197

@@ -296,6 +296,8 @@ SHAPES = [
     (1, 12, 40, 1, 1, 104, True, 100, 4),   # a window past all keys
     (1, 2, 5000, 4, 1, 72, True, 0, 0),     # the most parts of keys
     (2, 70, 1100, 2, 1, 96, False, 0, 0),
+    (60, 140, 90, 15, 5, 16, False, 0, 0),  # pairs in three chunks
+    (150, 33, 70, 8, 8, 8, False, 0, 0),
 ]
 
 
