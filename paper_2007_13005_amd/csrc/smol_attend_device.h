@@ -281,7 +281,10 @@ struct Sight {
         return j0 <= last_max && (j1 >= first_min || j0 < a.sinks);
     }
     // x[e] for keys j0 + 8 (e / 4) + 4 (lane / 32) + e % 4, e = 0 .. 15: `hidden` where the
-    // lane's column does not see the key.
+    // lane's column does not see the key. Ends: tiles that no column's first key cuts
+    // get code of their own, a third of the instructions (gradients of 64 images of 197
+    // rows 84 -> 81 us; the forward pass has no registers for it).
+    template <bool Ends>
     __device__ __forceinline__ void hide(const AttendArgs &a, f32x16 &x, int32_t j0, int lane,
                                          float hidden) const
     {
@@ -290,6 +293,12 @@ struct Sight {
             return;
         const int32_t base = fresh(j0 + 4 * (lane >> 5));
         const int32_t to = last - base, from = begin ? first - base : -64, sinks = a.sinks - base;
+        if (Ends && !begin) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                x[e] = 8 * (e >> 2) + (e & 3) <= to ? x[e] : hidden;
+            return;
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int32_t j = 8 * (e >> 2) + (e & 3);

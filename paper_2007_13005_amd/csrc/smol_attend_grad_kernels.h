@@ -159,7 +159,7 @@ __device__ __forceinline__ void GradQ<T, N>::run(const AttendArgs &a, uint32_t p
         vec<T, 8> d[4];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            sight.hide(a, x[h], j0 + 32 * h, lane, -INFINITY);
+            sight.hide<true>(a, x[h], j0 + 32 * h, lane, -INFINITY);
         const auto weigh = [&](int h, int k) {
 #pragma unroll
             for (int e = 16 * k / kHalf; e < 16 * (k + 1) / kHalf; ++e)

@@ -49,7 +49,7 @@ struct Columns {
     __device__ __forceinline__ bool look(const AttendArgs &a, f32x16 &x, int32_t j0, int lane,
                                          float *f)
     {
-        sight.hide(a, x, j0, lane, -INFINITY);
+        sight.hide<false>(a, x, j0, lane, -INFINITY);
         float top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 16; ++e)
