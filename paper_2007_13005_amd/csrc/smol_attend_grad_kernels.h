@@ -561,9 +561,9 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t p
 
 // Workgroups of keys, then those of queries, which are shorter: either's last run
 // beside the other's (queries first: 431 us for 397). Bound by the matrix
-// instructions and what they wait for: the ragged sequences take 380 us, seven
+// instructions and what they wait for: the ragged sequences take 373 us, seven
 // products at a library's rate would take 208. 64 images of 197 rows of 12
-// heads of 64 in fp16, 77 us: 197 rows fill 77 % of two tiles of 128.
+// heads of 64 in fp16, 74 us: 197 rows fill 77 % of two tiles of 128.
 template <typename T, int N>
 __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     attend_grad_kernel(AttendArgs a)
