@@ -349,6 +349,7 @@ PARTS = [
     (1, 700, 700, 8, 2, 64, False, 0, 0),
     (1, 515, 300, 6, 2, 72, True, 100, 130),  # queries before the first key
     (2, 333, 401, 5, 1, 128, True, 64, 3),    # columns of a query across tiles
+    (9, 700, 900, 4, 2, 32, False, 0, 0),     # pairs in chunks of 8, 8 and 2
 ]
 
 
