@@ -115,11 +115,12 @@ int64_t part_bytes(const smol_attend_shape &s, const Split &p)
 // unit (four: 4 ragged sequences of 4096 rows 397 -> 443 us, as parts' sums are
 // written and read; one: 5906 rows of 8 heads of 96 287 -> 551). A part has 128
 // columns or more (512: 1 x 399 rows of 14 heads of 128 over 2 42 -> 52 us, 2 x 148
-// of 16 of 80 over 4 24 -> 31), one of a tile of sinks 512, as the others' workgroups
-// run beside it (256: 18 x 4422 rows of a head of 128, a window of 15, 92 -> 100).
+// of 16 of 80 over 4 24 -> 31), one of a tile of sinks 256 (512: 3 x 271 rows of 32
+// heads of 128 over 8, a window of 10, 32 -> 38; 18 x 4422 rows of a head, a window of
+// 15, where other workgroups run beside them, 90 -> 88).
 constexpr int64_t kTileGroups = 512, kSinkGroups = 256;  // workgroups that parts make
 constexpr int64_t kKeyParts = 64;                        // of a tile at most
-constexpr int64_t kLeastColumns = 128, kLeastSinkColumns = 512;
+constexpr int64_t kLeastColumns = 128, kLeastSinkColumns = 256;
 
 // The parts in which the gradients of keys are formed: a tile of 128 keys takes
 // the columns of all queries that see it, or a part of them.
