@@ -265,7 +265,18 @@ typedef struct smol_attend_grad_args {
 
 int smol_attend_backward(const smol_attend_grad_args *a, void *stream);
 
-/* Bytes of workspace the backward call needs (0 for an invalid shape). */
+/* smol_attend_backward_kept: the same, with lse and rest where a program keeps
+ * them, at strides of their own (of sequences, rows and heads, in elements; 0 lets
+ * one stand for all) instead of dense. */
+typedef struct smol_attend_kept {
+    int64_t lse_batch_stride, lse_row_stride, lse_head_stride;
+    int64_t rest_batch_stride, rest_row_stride, rest_head_stride; /* unused: rest NULL */
+} smol_attend_kept;
+
+int smol_attend_backward_kept(const smol_attend_grad_args *a, const smol_attend_kept *kept,
+                              void *stream);
+
+/* Bytes of workspace a backward call needs (0 for an invalid shape). */
 int64_t smol_attend_backward_workspace_bytes(const smol_attend_shape *shape);
 
 #ifdef __cplusplus

@@ -44,7 +44,7 @@ _native = None
 # in the order in which the native module takes them
 _FUNCTIONS = ("smol_rotate", "smol_rotate_backward", "smol_head_norm", "smol_head_norm_backward",
               "smol_head_norm_workspace_bytes", "smol_attend", "smol_attend_workspace_bytes",
-              "smol_attend_backward", "smol_attend_backward_workspace_bytes")
+              "smol_attend_backward_kept", "smol_attend_backward_workspace_bytes")
 
 
 def _load():
@@ -232,8 +232,9 @@ def attend_backward(grad_out, q, k, v, out, lse, rest=None, scale: float | None 
                     stream=None):
     """Gradients of ``attend`` from that of ``out``: returns (grad_q, grad_k,
     grad_v), of the matrices' type. ``out``, ``lse`` and ``rest`` are the forward
-    call's (``rest`` may be None), the other arguments the same as there. Rows past
-    the lengths get zeros (``smol_attend_backward``)."""
+    call's (``rest`` may be None; they may lie at any strides, heads before rows for
+    instance, or dense in another shape), the other arguments the same as there. Rows
+    past the lengths get zeros (``smol_attend_backward_kept``)."""
     native = _native or _load()
     if grad_q is None:
         grad_q = _torch.empty(q.shape, dtype=q.dtype, device=q.device)

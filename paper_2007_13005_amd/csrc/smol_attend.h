@@ -18,10 +18,10 @@ struct HeadRows {
 struct AttendArgs {
     HeadRows q, k, v, out, dout;  // out is written by the forward pass, read by the backward
     HeadRows dq, dk, dv;          // written
-    const void *rest_in;
+    HeadRows rest_in, lse_in;     // read by the backward pass (rest_in.p null: zeros)
     void *rest;
-    float *lse;    // batch x queries x heads
-    float *delta;  // the same (backward)
+    float *lse;      // batch x queries x heads
+    float *lse_delta;  // of each of these (backward): lse in base 2, and D
     float *part;   // sums of parts of the keys (forward, splits > 1), of the columns
                    // (gradients of keys)
     const int32_t *q_lengths, *k_lengths;

@@ -163,7 +163,7 @@ KeyParts key_parts_of(const smol_attend_shape &s)
 
 int64_t delta_bytes(const smol_attend_shape &s)
 {
-    return ((int64_t)s.queries * s.heads * s.batch * 4 + 15) / 16 * 16;
+    return ((int64_t)s.queries * s.heads * s.batch * 8 + 15) / 16 * 16;
 }
 
 // Whatever the mask: the parts that there can be.
@@ -383,12 +383,12 @@ extern "C" int smol_attend(const smol_attend_args *p, void *stream)
     return SMOL_OK;
 }
 
-extern "C" int smol_attend_backward(const smol_attend_grad_args *p, void *stream)
+namespace smol {
+namespace {
+
+// kept: the strides of lse and rest, or null: dense.
+int attend_backward(const smol_attend_grad_args *p, const smol_attend_kept *kept, void *stream)
 {
-    using namespace smol;
-    clear_error();
-    if (!p)
-        return set_error(SMOL_ERR_INVALID_ARG, "args is NULL");
     const smol_attend_shape &s = p->shape;
     int st = check_shape(s);
     if (st != SMOL_OK)
@@ -411,10 +411,18 @@ extern "C" int smol_attend_backward(const smol_attend_grad_args *p, void *stream
         (st = of_keys(&a.dk, "grad_k", p->grad_k, true)) != SMOL_OK ||
         (st = of_keys(&a.dv, "grad_v", p->grad_v, true)) != SMOL_OK)
         return st;
-    if (s.queries > 0 && (!p->lse || (uintptr_t)p->lse % 4))
-        return set_error(SMOL_ERR_INVALID_ARG, "lse is NULL or not aligned to its elements");
-    if ((uintptr_t)p->rest % elem_size(s.type))
-        return set_error(SMOL_ERR_INVALID_ARG, "rest is not aligned to its elements");
+    const smol_attend_kept dense = {(int64_t)s.queries * s.heads, s.heads, 1,
+                                    (int64_t)s.queries * s.heads * s.dim,
+                                    (int64_t)s.heads * s.dim, s.dim};
+    const smol_attend_kept &at = kept ? *kept : dense;
+    const smol_attend_rows lse = {p->lse, at.lse_batch_stride, at.lse_row_stride,
+                                  at.lse_head_stride};
+    const smol_attend_rows rest = {p->rest, at.rest_batch_stride, at.rest_row_stride,
+                                   at.rest_head_stride};
+    if ((st = take(&a.lse_in, "lse", lse, s.batch, s.queries, s.heads, 1, SMOL_ELEM_F32,
+                   false)) != SMOL_OK ||
+        (p->rest && (st = of_queries(&a.rest_in, "rest", rest, false)) != SMOL_OK))
+        return st;
     const auto of = [](int32_t rows, const void *x) { return rows ? x : nullptr; };
     if ((st = check_workspace(p->workspace, p->workspace_bytes, grad_bytes(s))) != SMOL_OK ||
         (st = check_apart({of(s.queries, p->grad_q.data), of(s.keys, p->grad_k.data),
@@ -433,9 +441,7 @@ extern "C" int smol_attend_backward(const smol_attend_grad_args *p, void *stream
     a.direct_keys = near_keys(a.k, 128, s.dim, s.type) && near_keys(a.v, 128, s.dim, s.type);
     a.direct_rows = near_rows(a.q, 33, a.group.d, s.type) &&
                     near_rows(a.dout, 33, a.group.d, s.type);
-    a.lse = (float *)p->lse;
-    a.rest_in = p->rest;
-    a.delta = (float *)p->workspace;
+    a.lse_delta = (float *)p->workspace;
     a.part = (float *)((char *)p->workspace + delta_bytes(s));
     a.sink_tiles = parts.sink_tiles;
     a.sink_part = parts.sink_part;
@@ -468,4 +474,26 @@ extern "C" int smol_attend_backward(const smol_attend_grad_args *p, void *stream
         return set_error(SMOL_ERR_HIP, "attention backward launch: %s",
                          hipGetErrorString((hipError_t)e));
     return SMOL_OK;
+}
+
+}  // namespace
+}  // namespace smol
+
+extern "C" int smol_attend_backward(const smol_attend_grad_args *p, void *stream)
+{
+    using namespace smol;
+    clear_error();
+    if (!p)
+        return set_error(SMOL_ERR_INVALID_ARG, "args is NULL");
+    return attend_backward(p, nullptr, stream);
+}
+
+extern "C" int smol_attend_backward_kept(const smol_attend_grad_args *p,
+                                         const smol_attend_kept *kept, void *stream)
+{
+    using namespace smol;
+    clear_error();
+    if (!p || !kept)
+        return set_error(SMOL_ERR_INVALID_ARG, "args or kept is NULL");
+    return attend_backward(p, kept, stream);
 }

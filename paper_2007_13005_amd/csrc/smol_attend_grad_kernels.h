@@ -46,8 +46,8 @@ struct PairOf {
     }
 };
 
-// D of every row of queries that exists: a group of lanes a row, eight values a
-// lane. Bound by memory (the ragged sequences above: 129 MB in 29 us).
+// D of every row of queries that exists, beside its lse (which may lie at strides of
+// its own): a group of lanes a row, eight values a lane. Bound by memory (the ragged sequences above: 129 MB in 29 us).
 template <typename T, int N>
 __global__ void __launch_bounds__(64 * kAttendWaves) attend_delta_kernel(AttendArgs a)
 {
@@ -58,15 +58,16 @@ __global__ void __launch_bounds__(64 * kAttendWaves) attend_delta_kernel(AttendA
         const uint32_t row = divide(r, a.heads_div), b = divide(row, a.queries_div);
         const int32_t head = r - row * a.heads_div.d, i = row - b * a.queries_div.d;
         const bool some = b < a.batch;
+        const bool exists = some && (!a.q_lengths || i < a.q_lengths[b]);
         float delta = 0.0f;
-        if (some && d < a.dim && (!a.q_lengths || i < a.q_lengths[b])) {
+        if (exists && d < a.dim) {
             const auto at = [&](const HeadRows &m) {
                 return (const T *)m.p + b * m.batch + i * m.row + head * m.head + d;
             };
             vec<float, 8> y = to_f32<8, T>(load<T, 8>(at(a.out)));
             const vec<float, 8> dy = to_f32<8, T>(load<T, 8>(at(a.dout)));
-            if (a.rest_in)
-                y += to_f32<8, T>(load<T, 8>((const T *)a.rest_in + (int64_t)r * a.dim + d));
+            if (a.rest_in.p)
+                y += to_f32<8, T>(load<T, 8>(at(a.rest_in)));
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 delta = fmaf(dy[e], y[e], delta);
@@ -74,9 +75,18 @@ __global__ void __launch_bounds__(64 * kAttendWaves) attend_delta_kernel(AttendA
 #pragma unroll
         for (int step = 1; step < kLanes; step <<= 1)
             delta += __shfl_xor(delta, step);
-        if (some && d == 0)
-            a.delta[r] = delta;
+        if (some && d == 0 && exists) {
+            const float lse = *((const float *)a.lse_in.p + b * a.lse_in.batch +
+                                i * a.lse_in.row + head * a.lse_in.head);
+            *((float2 *)a.lse_delta + r) = make_float2(lse * kLog2e, delta);
+        }
     }
+}
+
+// A row's lse in base 2, and its D.
+__device__ __forceinline__ float2 lse_delta(const AttendArgs &a, int64_t row)
+{
+    return *((const float2 *)a.lse_delta + row);
 }
 
 // Gradients of queries: four waves of 32 columns over shared tiles of 64 keys. Both
@@ -111,8 +121,8 @@ __device__ __forceinline__ void GradQ<T, N>::run(const AttendArgs &a, uint32_t p
     const T *dyp = s.rows<T>(a.dout, c.head) + c.i * a.dout.row;
     row_operands<T, N>(qp, a.dim, lane, q);
     row_operands<T, N>(dyp, a.dim, lane, dy);
-    const float lse2 = sight.last < 0 ? 0.0f : a.lse[at] * kLog2e, minus_lse = kCarry<T> - lse2;
-    const float delta = sight.last < 0 ? 0.0f : a.delta[at];
+    const float2 stat = sight.last < 0 ? make_float2(0.0f, 0.0f) : lse_delta(a, at);
+    const float lse2 = stat.x, minus_lse = kCarry<T> - lse2, delta = stat.y;
     f32x16 sum[N];
 #pragma unroll
     for (int n = 0; n < N; ++n)
@@ -397,8 +407,9 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t p
             m_lse = m_delta = 0.0f;  // what the scores' and the products' sums start from
             if (m_last >= 0) {
                 const int64_t row = stat0 + (int64_t)i * a.heads + c - i * group;
-                m_lse = (kCarry<T> - a.lse[row] * kLog2e) * (1.0f / a.scale_log2);
-                m_delta = -a.delta[row];
+                const float2 stat = lse_delta(a, row);
+                m_lse = (kCarry<T> - stat.x) * (1.0f / a.scale_log2);
+                m_delta = -stat.y;
             }
         }
     };
@@ -531,7 +542,8 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t p
             const Spread qs = Spread::of(s.rows<T>(a.q, c.head) + c.i * a.q.row, a.dim, lane);
             const Spread ds =
                 Spread::of(s.rows<T>(a.dout, c.head) + c.i * a.dout.row, a.dim, lane);
-            const PairOf w(a, qs, ds, ks, vs, a.lse[row] * kLog2e, a.delta[row]);
+            const float2 stat = lse_delta(a, row);
+            const PairOf w(a, qs, ds, ks, vs, stat.x, stat.y);
             gk.x = fmaf(w.d, qs.x, gk.x);
             gk.y = fmaf(w.d, qs.y, gk.y);
             gv.x = fmaf(w.p, ds.x, gv.x);

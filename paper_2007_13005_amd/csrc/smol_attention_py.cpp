@@ -20,7 +20,7 @@ struct Library {
     decltype(&smol_head_norm_workspace_bytes) norm_bytes;
     decltype(&smol_attend) attend;
     decltype(&smol_attend_workspace_bytes) attend_bytes;
-    decltype(&smol_attend_backward) attend_backward;
+    decltype(&smol_attend_backward_kept) attend_backward;
     decltype(&smol_attend_backward_workspace_bytes) attend_backward_bytes;
 } lib;
 
@@ -341,6 +341,25 @@ M rows_like(const at::Tensor &t, const at::Tensor &like, const char *name)
     return m;
 }
 
+// What the forward call wrote for each query and head, on its way back: as many
+// elements densely, or the sizes of `like`'s first dimensions (and rest's values,
+// dense) at any strides.
+void strides_of(const at::Tensor &t, const at::Tensor &like, int64_t dims, at::ScalarType type,
+                const char *name, int64_t *batch, int64_t *row, int64_t *head)
+{
+    const int64_t values = dims == 4 ? like.size(3) : 1;
+    const int64_t count = like.size(0) * like.size(1) * like.size(2) * values;
+    same_type(t, type, name);
+    const bool dense = t.is_contiguous() && t.numel() == count;
+    if (!dense && (t.dim() != dims || t.sizes() != like.sizes().slice(0, dims) ||
+                   (values > 1 && t.stride(3) != 1)))
+        wrong("%s must have q's %s, or %lld elements densely", name,
+              dims == 4 ? "sizes with dense heads" : "batch, rows and heads", (long long)count);
+    *head = dense ? values : t.stride(2);
+    *row = dense ? like.size(2) * values : t.stride(1);
+    *batch = dense ? like.size(1) * like.size(2) * values : t.stride(0);
+}
+
 // q, k, v, scale, causal, window, sinks, q_lengths, k_lengths, out, lse, rest,
 // workspace, stream
 PyObject *attend(PyObject *const *o)
@@ -406,8 +425,12 @@ PyObject *attend_backward(PyObject *const *o)
     a.grad_q = rows_like<smol_attend_out>(dq, q, "grad_q");
     a.grad_k = rows_like<smol_attend_out>(dk, k, "grad_k");
     a.grad_v = rows_like<smol_attend_out>(dv, k, "grad_v");
-    vector(&lse, q.size(0) * q.size(1) * q.size(2), at::kFloat, "lse");
-    vector(rest, q.numel(), q.scalar_type(), "rest");
+    smol_attend_kept kept = {};
+    strides_of(lse, q, 3, at::kFloat, "lse", &kept.lse_batch_stride, &kept.lse_row_stride,
+               &kept.lse_head_stride);
+    if (rest)
+        strides_of(*rest, q, 4, q.scalar_type(), "rest", &kept.rest_batch_stride,
+                   &kept.rest_row_stride, &kept.rest_head_stride);
     const at::Tensor &room = *all.take(o[16], "workspace");
     workspace(room, lib.attend_backward_bytes(&a.shape));
     all.check_device();
@@ -423,7 +446,7 @@ PyObject *attend_backward(PyObject *const *o)
     a.out.data = ptr(&out);
     a.rest = ptr(rest);
     a.lse = (const float *)ptr(&lse);
-    return launch(o[17], all, [&](void *s) { return lib.attend_backward(&a, s); });
+    return launch(o[17], all, [&](void *s) { return lib.attend_backward(&a, &kept, s); });
 }
 
 // q, k

@@ -198,6 +198,7 @@ SIGNATURES = {
                                                         ctypes.c_int32, ctypes.c_int32]),
     "smol_attend": (ctypes.c_int, [_vp, _vp]),
     "smol_attend_backward": (ctypes.c_int, [_vp, _vp]),
+    "smol_attend_backward_kept": (ctypes.c_int, [_vp, _vp, _vp]),
     "smol_attend_workspace_bytes": (ctypes.c_int64, [_vp]),
     "smol_attend_backward_workspace_bytes": (ctypes.c_int64, [_vp]),
     "smol_stream_probe": (ctypes.c_int, [_vp, ctypes.c_uint64, _vp, ctypes.c_uint64,
