@@ -284,7 +284,6 @@ def prepare(case, seed):
     s["mask"] = {"scale": s["scale"], "causal": case["causal"], "window": case["window"],
                  "sinks": case["sinks"], "q_lengths": s["q_lengths"], "k_lengths": s["k_lengths"]}
     if op == "attend_grad":
-        s["lse"], s["rest"] = s["lse"].contiguous(), s["rest"].contiguous()
         s["grads"] = like(s["q"]), like(s["k"]), like(s["v"])
         s["workspace"] = room(attention.attend_backward_workspace_bytes(s["q"], s["k"]))
     else:
