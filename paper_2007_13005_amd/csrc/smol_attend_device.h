@@ -502,6 +502,13 @@ __device__ __forceinline__ float dot(const Spread &a, const Spread &b)
 {
     return wave_sum(a.x * b.x + a.y * b.y);
 }
+// A pair's weight: not 0, as an infinity counts however small its weight; NaN where
+// the score, or what it is relative to, is (which a maximum would drop).
+__device__ __forceinline__ float weight_of(float exponent)
+{
+    const float w = exp2_of(exponent);
+    return w < 1.0e-37f ? 1.0e-37f : w;
+}
 // Whether all values of a sum are NaN, which no further term changes.
 __device__ __forceinline__ bool settled(const Spread &s, int32_t dim, int lane)
 {

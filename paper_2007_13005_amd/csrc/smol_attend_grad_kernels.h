@@ -40,8 +40,7 @@ struct PairOf {
     __device__ __forceinline__ PairOf(const AttendArgs &a, const Spread &q, const Spread &dy,
                                       const Spread &k, const Spread &v, float lse2, float delta)
     {
-        // not 0: an infinity counts however small its weight
-        p = fmaxf(exp2_of(fmaf(dot(q, k), a.scale_log2, -lse2)), 1.0e-37f);
+        p = weight_of(fmaf(dot(q, k), a.scale_log2, -lse2));
         d = p * (dot(dy, v) - delta);
     }
 };

@@ -102,9 +102,7 @@ struct Columns {
                         continue;
                     const Spread k = Spread::of(s.rows<T>(a.k, s.kv) + j * a.k.row, a.dim, lane);
                     const Spread v = Spread::of(s.rows<T>(a.v, s.kv) + j * a.v.row, a.dim, lane);
-                    // not 0: an infinity counts however small its weight
-                    const float w =
-                        fmaxf(exp2_of(fmaf(dot(x, k), a.scale_log2, -top)), 1.0e-37f);
+                    const float w = weight_of(fmaf(dot(x, k), a.scale_log2, -top));
                     y.x = fmaf(w, v.x, y.x);
                     y.y = fmaf(w, v.y, y.y);
                     if (settled(y, a.dim, lane))

@@ -1,0 +1,126 @@
+"""Attention and its gradients where inputs are not finite: NaN and infinities reach
+exactly what sees them. Against the 64-bit definitions of tests/attention_util.py."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2007_13005_amd import attention
+from tests import attention_util as ref
+from tests.gpu_util import note
+from tests.test_gpu_attention import BF16, F16, F32, INF, NAN, dev, inputs, mask
+from tests.tokens_util import close
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [F32, F16, BF16]
+# batch, queries, keys, heads, kv_heads, dim, causal, window, sinks
+SHAPES = [
+    (1, 150, 150, 2, 1, 64, True, 0, 0),
+    (2, 140, 150, 6, 2, 40, True, 30, 2),   # columns of a query across tiles
+    (1, 90, 130, 3, 3, 128, False, 0, 0),
+    (1, 700, 700, 8, 2, 24, True, 0, 0),    # gradients of keys in parts
+    (1, 3, 700, 4, 2, 72, True, 100, 5),    # few columns, keys in parts
+    (2, 1, 90, 8, 2, 32, True, 0, 0),
+]
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("what", ["query", "gradient", "key"])
+def test_nan_reaches_all_that_sees_it(shape, dtype, what):
+    """A NaN in a query, in its output's gradient, or in a key, alone: the weights p =
+    exp(s - lse), or d, of every pair of a spoiled row are NaN, so the gradients of all
+    keys that the row sees are; nothing else is."""
+    note(f"attend nan {shape} {dtype} {what}")
+    lq, lk = shape[1:3]
+    see = ref.visible(lq, lk, lq, lk, *shape[6:])
+    q, k, v, dy = inputs(shape, dtype, 29)
+    i, j = lq // 2, int(see[lq // 2].nonzero()[0])
+    spoiled = torch.arange(lq) == i
+    if what == "query":
+        q[:, i, :, 3] = NAN
+    elif what == "gradient":
+        dy[:, i] = NAN
+    else:
+        k[:, j, :, 5] = NAN
+        spoiled = see[:, j]
+    out, lse = attention.attend(dev(q), dev(k), dev(v), **mask(shape))
+    if what != "gradient":
+        assert torch.equal(torch.isnan(lse.cpu()), spoiled[None, :, None].expand(lse.shape))
+        assert bool(torch.isnan(out.cpu()[:, spoiled]).all())
+        assert bool(torch.isfinite(out.cpu()[:, ~spoiled]).all())
+    dq, dk, dv = (x.cpu() for x in attention.attend_backward(
+        dev(dy), dev(q), dev(k), dev(v), out, lse, **mask(shape)))
+    touched = see[spoiled].any(0)
+    assert bool(torch.isnan(dq[:, spoiled]).all())
+    assert bool(torch.isfinite(dq[:, ~spoiled]).all())
+    for name, x in (("k", dk), ("v", dv)):
+        assert bool(torch.isnan(x[:, touched]).all()), f"grad {name} lost a NaN"
+        assert bool(torch.isfinite(x[:, ~touched]).all()), f"grad {name} got a NaN"
+
+
+def spoil(x, at):
+    """x with the values of `at`, {(row, dim): value}, in all heads."""
+    bad = x.clone()
+    for (row, d), value in at.items():
+        bad[:, row, :, d] = value
+    return bad
+
+
+def reach(see, at, rows, dim):
+    """(rows, dim): the sum over what is seen of the values of `at`, zeros elsewhere."""
+    total = torch.zeros((rows, dim), dtype=torch.float64)
+    for (j, d), value in at.items():
+        total[:, d] += torch.where(see[:, j], value, 0.0)
+    return total
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_values_that_are_not_finite(shape, dtype):
+    """Single NaN and infinities among the values: the rows that see them have them, in
+    their column alone, infinities of both signs a NaN, however small the weight."""
+    note(f"attend values {shape} {dtype}")
+    lq, lk, dim = shape[1], shape[2], shape[5]
+    see = ref.visible(lq, lk, lq, lk, *shape[6:])
+    q, k, v, _ = inputs(shape, dtype, 31)
+    # one key that no query likes: a weight below 2^-200
+    k[:, lk // 3] = 0.0
+    k[:, lk // 3, :, 0] = -200.0
+    q[..., 0] = 0.6 * dim ** 0.5 + 6.0
+    at = {(lk // 3, 1): INF, (lk - 1, 0): NAN, (lk - 2, dim - 1): -INF, (lk // 2, 4): INF,
+          (lk // 2 + 1, 4): -INF, (lk // 2, 7): -INF, (lk - lq, 6): INF}
+    (want, bound), (wl, bl) = ref.attend(q, k, v, **mask(shape))
+    want = want + reach(see, at, lq, dim)[None, :, None, :]
+    out, lse = attention.attend(dev(q), dev(k), dev(spoil(v, at)), **mask(shape))
+    close(out, want, bound, "out")
+    close(lse, wl, bl, "lse")
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradients_that_are_not_finite(shape, dtype):
+    """Single NaN and infinities in the rows' gradients: grad_v has them in their column
+    alone, the keys that such a row sees have no finite grad_k, the row no finite
+    grad_q, and the others what they have without."""
+    note(f"attend gradients {shape} {dtype}")
+    lq, lk, dim = shape[1], shape[2], shape[5]
+    see = ref.visible(lq, lk, lq, lk, *shape[6:])
+    q, k, v, dy = inputs(shape, dtype, 37)
+    rest = torch.empty_like(q, device="cuda")
+    out, lse = attention.attend(dev(q), dev(k), dev(v), rest=rest, **mask(shape))
+    at = {(lq // 2, 1): INF, (lq - 1, 0): NAN, (lq // 2, 4): -INF, (lq // 3, 4): INF}
+    spoiled = torch.zeros(lq, dtype=torch.bool)
+    spoiled[[i for i, _ in at]] = True
+    (wq, bq), (wk, bk), (wv, bv) = ref.attend_backward(
+        dy, q, k, v, out.cpu(), lse.cpu(), rest.cpu(), **mask(shape))
+    wv = wv + reach(see.t(), at, lk, dim)[None, :, None, :]
+    dq, dk, dv = (x.cpu() for x in attention.attend_backward(
+        dev(spoil(dy, at)), dev(q), dev(k), dev(v), out, lse, rest, **mask(shape)))
+    touched = see[spoiled].any(0)
+    close(dv, wv, bv, "grad v")
+    close(dq[:, ~spoiled], wq[:, ~spoiled], bq[:, ~spoiled], "grad q")
+    close(dk[:, ~touched], wk[:, ~touched], bk[:, ~touched], "grad k")
+    assert not bool(torch.isfinite(dq[:, spoiled]).any())
+    assert not bool(torch.isfinite(dk[:, touched]).any())
