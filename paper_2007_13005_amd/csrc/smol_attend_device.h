@@ -456,6 +456,81 @@ __device__ __forceinline__ bool any_not_finite(const f32x16 (&x)[N])
     return all != all;
 }
 
+// Whether any of the workgroup's waves says so (each the same in all its lanes), by way
+// of four words of LDS that none reads any more.
+__device__ __forceinline__ bool any_wave(int *told, bool so, int wave, int lane)
+{
+    if (lane == 0)
+        told[wave] = so;
+    __syncthreads();
+    int any = 0;
+#pragma unroll
+    for (int w = 0; w < kAttendWaves; ++w)
+        any |= told[w];
+    return __builtin_amdgcn_readfirstlane(any);
+}
+
+// Which of 32 rows of a tile in LDS (at its first) hold a value that is not finite:
+// bit r for row r.
+template <typename T, int N>
+__device__ __forceinline__ uint32_t rows_not_finite(const char *tile, int lane)
+{
+    typedef LdsRows<T, N> Rows;
+    static_assert(Rows::kChunks % 2 == 0, "half a row a lane");
+    const char *p = tile + (lane & 31) * Rows::kStride + (lane >> 5) * (Rows::kStride / 2);
+    float s = 0.0f;
+#pragma unroll
+    for (int c = 0; c < Rows::kChunks / 2; ++c) {
+        const typename Rows::Chunk v = *(const typename Rows::Chunk *)(p + 16 * c);
+#pragma unroll
+        for (int e = 0; e < Rows::kEach; ++e)
+            s = fmaf((float)v[e], 0.0f, s);
+    }
+    const uint64_t which = __ballot(s != s);
+    return (uint32_t)(which | which >> 32);
+}
+
+// v with zeros where it is not finite.
+template <typename T>
+__device__ __forceinline__ vec<T, 8> finite_of(vec<T, 8> v)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v[e] = fabsf((float)v[e]) < INFINITY ? v[e] : (T)0.0f;
+    return v;
+}
+
+// Adds to a result [values x columns] what `rows` of a tile's 32 hold that is not
+// finite, to the columns that see the row (sees(r), of the lane's column): as it is,
+// or as NaN.
+template <bool AsNan, typename T, int N, typename Sees>
+__device__ __forceinline__ void add_not_finite(f32x16 (&sum)[N], const char *tile, uint32_t rows,
+                                               int lane, Sees sees)
+{
+    typedef LdsRows<T, N> Rows;
+#pragma unroll 1
+    while (rows) {
+        const int r = __builtin_ctz(rows);
+        rows &= rows - 1;
+        const bool some = sees(r);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int at = (32 * n + 8 * g + 4 * (lane >> 5)) * (int)sizeof(T);
+                const vec<T, 4> v =
+                    *(const vec<T, 4> *)(tile + Rows::place(r, at >> 4) + (at & 15));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = (float)v[e];
+                    if (some && !(fabsf(x) < INFINITY))
+                        sum[n][4 * g + e] += AsNan ? x - x : x;
+                }
+                in_order();
+            }
+    }
+}
+
 // Writes a result [values x rows]: the lane's row at p, times f, and what rounding
 // takes from it at rest (or null); zeros for a row that has no pair (its sums may
 // hold 0 times a NaN). dim is a multiple of 8, so both halves of the wave write.

@@ -9,9 +9,10 @@
 //
 // What a query does not see takes no part: its score is set to minus infinity
 // before the maximum. A weight of 0 times a NaN or an infinity among the values
-// would still spoil the sums (of a tile that other queries see); so a column
-// whose sums are not finite in the end, though its weights are, is summed
-// again key by key, over what it sees alone.
+// would still spoil the sums (of a tile that other queries see). So where a
+// column's sums are not finite in the end, though its weights are, the waves that
+// share its tiles sum once more, with zeros for such values in the products, and add
+// the values themselves to the columns that see them.
 #ifndef SMOL_ATTEND_KERNELS_H
 #define SMOL_ATTEND_KERNELS_H
 
@@ -36,6 +37,10 @@ struct Columns {
         const Column c(a, s, c0 + (lane & 31));
         row_operands<T, N>(s.rows<T>(a.q, c.head) + c.i * a.q.row, a.dim, lane, q);
         sight.start(a, s, c0, c);
+        clear();
+    }
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
         for (int n = 0; n < N; ++n)
             sum[n] = (f32x16)0.0f;
@@ -76,46 +81,51 @@ struct Columns {
                 l += x[e];
             }
     }
-    // Columns whose sums alone are not finite, again: over keys j0 .. j1 of each
-    // tile that next gives (false: none left), what the column sees.
-    template <typename Next>
-    __device__ __forceinline__ void mend(const AttendArgs &a, const Sequence &s, int32_t c0,
-                                         int lane, Next next)
+    // Whether a column's sums alone are not finite, or were spoiled by what it does not
+    // see: over the wave, the same in each lane.
+    __device__ __forceinline__ bool spoiled() const
     {
-        const bool bad = any_not_finite(sum) && fabsf(l) < INFINITY && sight.last >= 0;
-        uint64_t which = __ballot(bad);
-        which = (which | which >> 32) & 0xffffffffu;
-        while (which) {
-            const int col = __builtin_ctzll(which);
-            which &= which - 1;
-            const int32_t to = __builtin_amdgcn_readlane(sight.last, col);
-            const int32_t from = __builtin_amdgcn_readlane(sight.first, col);
-            const float top = __builtin_bit_cast(
-                float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), col));
-            const Column c(a, s, c0 + col);
-            const Spread x = Spread::of(s.rows<T>(a.q, c.head) + c.i * a.q.row, a.dim, lane);
-            Spread y = {0.0f, 0.0f};
-            int32_t j0, j1;
-            for (int32_t n = 0; next(n, &j0, &j1); ++n)
-                for (int32_t j = j0; j <= j1 && j <= to; ++j) {
-                    if (!sees(j, to, from, a.sinks))
-                        continue;
-                    const Spread k = Spread::of(s.rows<T>(a.k, s.kv) + j * a.k.row, a.dim, lane);
-                    const Spread v = Spread::of(s.rows<T>(a.v, s.kv) + j * a.v.row, a.dim, lane);
-                    const float w = weight_of(fmaf(dot(x, k), a.scale_log2, -top));
-                    y.x = fmaf(w, v.x, y.x);
-                    y.y = fmaf(w, v.y, y.y);
-                    if (settled(y, a.dim, lane))
-                        break;
-                }
-            set_column(sum, y, col, lane);
+        const float all = both_halves(l, [](float u, float v) { return u + v; });
+        return __any(any_not_finite(sum) && fabsf(all) < INFINITY && sight.last >= 0);
+    }
+    // Scores, weights and sums of 32 keys from j0 on, whose values stand at `values` in
+    // LDS; keys(k) gives the operands of their scores. What is not finite among the
+    // values takes no part in the products, and is added where it is seen.
+    template <typename Keys>
+    __device__ __forceinline__ void carefully(const AttendArgs &a, Keys keys, const char *values,
+                                              int32_t j0, int lane)
+    {
+        typedef LdsRows<T, N> Rows;
+        lane = fresh(lane);  // (no address of these is kept through the loops)
+        const int value_at = Rows::column_at(lane);
+        f32x16 x = (f32x16)0.0f;
+        float f;
+#pragma unroll
+        for (int k = 0; k < 2 * N; ++k)
+            multiply<T>(x, keys(k), q[k]);
+        in_order();
+        look(a, x, j0, lane, &f);
+        weigh(a, x, 0, 16);
+        in_order();
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const vec<T, 8> w = operand<T>(x, g);
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                multiply<T>(sum[n], finite_of<T>(Rows::column(values, value_at, 16 * g, n)), w);
+                in_order();
+            }
         }
+        add_not_finite<false, T, N>(
+            sum, values, rows_not_finite<T, N>(values, lane), lane,
+            [&](int r) { return sees(j0 + r, sight.last, sight.first, a.sinks); });
     }
     // Rows of out, rest and lse; or, of a part of the keys, sums, m and l.
     __device__ __forceinline__ void finish(const AttendArgs &a, const Sequence &s, int32_t c0,
                                            uint32_t pair, uint32_t split, int lane)
     {
         l = both_halves(l, [](float u, float v) { return u + v; });
+        lane = fresh(lane);
         const int32_t at = c0 + (lane & 31);
         if (at >= a.columns)
             return;
@@ -287,13 +297,29 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 4 ? 1 : N <= 2
         }
     }
     const AttendArgs &late = args_again();
-    cols.mend(late, s, mine, lane, [&](int32_t n, int32_t *j0, int32_t *j1) {
-        if (lo + n >= hi)
-            return false;
-        *j0 = walk.tile(lo + n) * kKeys;
-        *j1 = *j0 + kKeys - 1;
-        return true;
-    });
+    // Told in the buffer that the last tile is not in: four bytes of LDS more than two
+    // buffers, 64 KB for heads of 128, cost a tenth (4096 tokens, 16 heads of 128 over
+    // 4, bf16, 98 us -> 110).
+    if (any_wave((int *)lds[(hi - lo) & 1], cols.spoiled(), wave, lane)) {
+        __syncthreads();  // before tiles take its place
+        cols.clear();
+        fetch(lo);
+#pragma unroll 1
+        for (int32_t n = lo; n < hi; ++n) {
+            loads_done();
+            __syncthreads();
+            if (n + 1 < hi)
+                fetch(n + 1);
+            const char *tile = lds[(n - lo) & 1];
+            const int32_t j0 = walk.tile(n) * kKeys;
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h)
+                if (cols.sight.any(late, j0 + 32 * h, j0 + 32 * h + 31))
+                    cols.carefully(
+                        late, [&](int k) { return Rows::row(tile, Rows::row_at(fresh(lane)), 32 * h, k); },
+                        tile + kBytes + 32 * h * Rows::kStride, j0 + 32 * h, lane);
+        }
+    }
     cols.finish(late, s, mine, task.pair, task.split, lane);
 }
 
@@ -364,13 +390,19 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
         }
     }
     const AttendArgs &late = args_again();
-    cols.mend(late, s, c0, lane, [&](int32_t n, int32_t *j0, int32_t *j1) {
-        if (own + n * kAttendWaves >= hi)
-            return false;
-        *j0 = walk.tile(own + n * kAttendWaves) * kKeys;
-        *j1 = *j0 + kKeys - 1;
-        return true;
-    });
+    if (cols.spoiled()) {
+        cols.clear();
+        fetch(own, 0);
+#pragma unroll 1
+        for (int32_t n = own; n < hi; n += kAttendWaves) {
+            loads_done();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            cols.carefully(late, [&](int t) { return k[t]; }, values, walk.tile(n) * kKeys, lane);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // before the tile is replaced
+            if (n + kAttendWaves < hi)
+                fetch(n + kAttendWaves, 0);
+        }
+    }
     loads_done();
     // the waves' sums at one maximum, then waves 2 and 3 into 0 and 1, 1 into 0:
     // of those that had a tile

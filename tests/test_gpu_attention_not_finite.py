@@ -124,3 +124,50 @@ def test_gradients_that_are_not_finite(shape, dtype):
     close(dk[:, ~touched], wk[:, ~touched], bk[:, ~touched], "grad k")
     assert not bool(torch.isfinite(dq[:, spoiled]).any())
     assert not bool(torch.isfinite(dk[:, touched]).any())
+
+
+def least_time(call) -> float:
+    """Of five calls, in milliseconds."""
+    begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    times = []
+    for _ in range(6):
+        begin.record()
+        call()
+        end.record()
+        end.synchronize()
+        times.append(begin.elapsed_time(end))
+    return min(times[1:])
+
+
+def costs(dtype, spoiled):
+    """Times of a causal prompt's forward and backward pass, of clean inputs and of ones
+    that `spoiled` changes in place."""
+    shape = (1, 1024, 1024, 8, 2, 64, True, 0, 0)
+    times = []
+    for change in (None, spoiled):
+        q, k, v, dy = (dev(x) for x in inputs(shape, dtype, 47))
+        if change:
+            change(q, k, v, dy)
+        out, lse = attention.attend(q, k, v)
+        grads = [torch.empty_like(x) for x in (q, k, v)]
+        room = torch.empty(attention.attend_backward_workspace_bytes(q, k), dtype=torch.uint8,
+                           device="cuda")
+        times.append((least_time(lambda: attention.attend(q, k, v, out=out, lse=lse)),
+                      least_time(lambda: attention.attend_backward(
+                          dy, q, k, v, out, lse, grad_q=grads[0], grad_k=grads[1],
+                          grad_v=grads[2], workspace=room))))
+    return times
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("value, row", [(NAN, 60), (INF, 1000), (-INF, 500)])
+def test_a_value_that_is_not_finite_costs_little(value, row, dtype):
+    """Rows that are summed again are summed by tiles: a call takes a few times a clean
+    one's time (pair by pair it took hundreds of times that)."""
+    note(f"attend time, {value} among the values {dtype}")
+
+    def change(q, k, v, dy):
+        v[0, row, 0, 5] = value
+
+    clean, spoiled = costs(dtype, change)
+    assert spoiled[0] < 20 * clean[0], (clean, spoiled)
