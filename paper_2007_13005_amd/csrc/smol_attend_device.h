@@ -197,8 +197,9 @@ struct Sequence {
     {
         b = (int32_t)divide(pair, a.kv_heads);
         kv = (int32_t)(pair - b * a.kv_heads.d);
-        q_length = a.q_lengths ? a.q_lengths[b] : a.queries;
-        k_length = a.k_lengths ? a.k_lengths[b] : a.keys;
+        // (the same in all lanes, which the compiler need not see through args_again)
+        q_length = __builtin_amdgcn_readfirstlane(a.q_lengths ? a.q_lengths[b] : a.queries);
+        k_length = __builtin_amdgcn_readfirstlane(a.k_lengths ? a.k_lengths[b] : a.keys);
         q_length = q_length < 0 ? 0 : q_length < a.queries ? q_length : a.queries;
         k_length = k_length < 0 ? 0 : k_length < a.keys ? k_length : a.keys;
         shift = k_length - q_length;
@@ -490,24 +491,38 @@ __device__ __forceinline__ uint32_t rows_not_finite(const char *tile, int lane)
     return (uint32_t)(which | which >> 32);
 }
 
-// v with zeros where it is not finite.
+// v with zeros where it is not finite; some: whether any lane's v was not, of those
+// that were asked.
 template <typename T>
-__device__ __forceinline__ vec<T, 8> finite_of(vec<T, 8> v)
+__device__ __forceinline__ vec<T, 8> finite_of(vec<T, 8> v, bool &some)
 {
+    // an exponent of ones carries into the sign's bit
+    constexpr bool half = std::is_same<T, f16>::value, single = sizeof(T) == 4;
+    constexpr uint32_t ones = single ? 0x7f800000u : half ? 0x7c007c00u : 0x7f807f80u;
+    constexpr uint32_t one = single ? 0x00800000u : half ? 0x04000400u : 0x00800080u;
+    typedef uint32_t Words __attribute__((ext_vector_type(2 * sizeof(T))));
+    const Words w = __builtin_bit_cast(Words, v);
+    uint32_t any = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        v[e] = fabsf((float)v[e]) < INFINITY ? v[e] : (T)0.0f;
+    for (int k = 0; k < 2 * (int)sizeof(T); ++k)
+        any |= (w[k] & ones) + one;
+    if (__any((any & 0x80008000u) != 0)) {
+        some = true;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = fabsf((float)v[e]) < INFINITY ? v[e] : (T)0.0f;
+    }
     return v;
 }
 
-// Adds to a result [values x columns] what `rows` of a tile's 32 hold that is not
-// finite, to the columns that see the row (sees(r), of the lane's column): as it is,
-// or as NaN.
+// Adds to a result [values x columns] what a tile's 32 rows hold that is not finite, to
+// the columns that see the row (sees(r), of the lane's column): as it is, or as NaN.
 template <bool AsNan, typename T, int N, typename Sees>
-__device__ __forceinline__ void add_not_finite(f32x16 (&sum)[N], const char *tile, uint32_t rows,
-                                               int lane, Sees sees)
+__device__ __forceinline__ void add_not_finite(f32x16 (&sum)[N], const char *tile, int lane,
+                                               Sees sees)
 {
     typedef LdsRows<T, N> Rows;
+    uint32_t rows = rows_not_finite<T, N>(tile, lane);
 #pragma unroll 1
     while (rows) {
         const int r = __builtin_ctz(rows);
@@ -522,9 +537,8 @@ __device__ __forceinline__ void add_not_finite(f32x16 (&sum)[N], const char *til
                     *(const vec<T, 4> *)(tile + Rows::place(r, at >> 4) + (at & 15));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float x = (float)v[e];
-                    if (some && !(fabsf(x) < INFINITY))
-                        sum[n][4 * g + e] += AsNan ? x - x : x;
+                    const float x = some ? (float)v[e] : 0.0f;
+                    sum[n][4 * g + e] += AsNan ? x - x : fabsf(x) < INFINITY ? 0.0f : x;
                 }
                 in_order();
             }
@@ -567,46 +581,7 @@ __device__ __forceinline__ void write_row(T *p, T *rest, f32x16 (&sum)[N], float
 // A row of up to 128 values over the wave: values lane and lane + 64.
 struct Spread {
     float x, y;
-    template <typename T>
-    static __device__ __forceinline__ Spread of(const T *p, int32_t dim, int lane)
-    {
-        return {lane < dim ? (float)p[lane] : 0.0f, lane + 64 < dim ? (float)p[lane + 64] : 0.0f};
-    }
 };
-__device__ __forceinline__ float dot(const Spread &a, const Spread &b)
-{
-    return wave_sum(a.x * b.x + a.y * b.y);
-}
-// A pair's weight: not 0, as an infinity counts however small its weight; NaN where
-// the score, or what it is relative to, is (which a maximum would drop).
-__device__ __forceinline__ float weight_of(float exponent)
-{
-    const float w = exp2_of(exponent);
-    return w < 1.0e-37f ? 1.0e-37f : w;
-}
-// Whether all values of a sum are NaN, which no further term changes.
-__device__ __forceinline__ bool settled(const Spread &s, int32_t dim, int lane)
-{
-    return !__any((lane < dim && s.x == s.x) || (lane + 64 < dim && s.y == s.y));
-}
-// The value at `d` of a spread row, any d a lane.
-__device__ __forceinline__ float value_at(const Spread &s, int d)
-{
-    const float x = __shfl(s.x, d & 63), y = __shfl(s.y, d & 63);
-    return d < 64 ? x : y;
-}
-// Sets the registers of the lanes of column `column` to a spread row.
-template <int N>
-__device__ __forceinline__ void set_column(f32x16 (&x)[N], const Spread &s, int column, int lane)
-{
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float v = value_at(s, 32 * n + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3));
-            x[n][e] = (lane & 31) == column ? v : x[n][e];
-        }
-}
 
 }  // namespace
 }  // namespace smol

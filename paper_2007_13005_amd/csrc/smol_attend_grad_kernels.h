@@ -14,12 +14,16 @@
 // us for 401, 5906 rows of 8 heads of 96 350 for 290.
 //
 // p and d are rounded to the type as operands. fp16 has few exponents: there
-// both are carried times 2^6 (a weight of 2^-20 is then still a normal number);
-// d past 2^10 overflows, and its row is summed again as below.
+// both are carried times 2^6 (a weight of 2^-20 is then still a normal number).
 //
 // What a query does not see has a score of minus infinity, so p and d are zero.
-// Where it holds a NaN or an infinity they may not be: sums that are not finite in
-// the end are formed again over what is seen alone (as in smol_attend_kernels.h).
+// Where it holds a NaN or an infinity they may not be, and d past 2^10 overflows as
+// carried. So a workgroup some of whose sums are not finite in the end, though lse
+// and D are, forms them once more: with zeros for p and d of pairs that are not seen
+// and for what is not finite in the products' other operands, which is added where it
+// is seen; and with d carried by less where it grows past fp16, as a running maximum
+// would. 2048 rows, 16 heads of 128 over 4, causal, fp16: 146 us, with a NaN in a query
+// 209, with d past 2^10 everywhere 364.
 #ifndef SMOL_ATTEND_GRAD_KERNELS_H
 #define SMOL_ATTEND_GRAD_KERNELS_H
 
@@ -34,19 +38,35 @@ constexpr float kCarry = std::is_same<T, f16>::value ? 6.0f : 0.0f;  // log2
 template <typename T>
 constexpr float kCarried = std::is_same<T, f16>::value ? 1.0f / 64.0f : 1.0f;
 
-// The weight of one pair and its d, over the wave.
-struct PairOf {
-    float p, d;
-    __device__ __forceinline__ PairOf(const AttendArgs &a, const Spread &q, const Spread &dy,
-                                      const Spread &k, const Spread &v, float lse2, float delta)
-    {
-        p = weight_of(fmaf(dot(q, k), a.scale_log2, -lse2));
-        d = p * (dot(dy, v) - delta);
+// fp16: by what the lane's d are carried beside p's 2^6, a power of two so that the
+// largest of them stays below 2^15. Sums change with it.
+template <typename T, int N>
+__device__ __forceinline__ void carry_less(f32x16 &d, f32x16 (&sum)[N], float &carry)
+{
+    if constexpr (std::is_same<T, f16>::value) {
+        float top = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            top = fmaxf(top, fabsf(d[e]));
+        top = both_halves(top, [](float u, float v) { return fmaxf(u, v); });
+        if (__any(top * carry >= 0x1p15f && top < INFINITY)) {
+            // top is below 2^exponent, at least half of it
+            const float to = top < INFINITY
+                                 ? fminf(carry, ldexpf(1.0f, 15 - __builtin_amdgcn_frexp_expf(top)))
+                                 : carry;
+            const float f = to / carry;
+            carry = to;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+                sum[n] *= f;
+        }
+        d *= carry;
     }
-};
+}
 
 // D of every row of queries that exists, beside its lse (which may lie at strides of
-// its own): a group of lanes a row, eight values a lane. Bound by memory (the ragged sequences above: 129 MB in 29 us).
+// its own): a group of lanes a row, eight values a lane. Bound by memory (the ragged
+// sequences above: 129 MB in 29 us).
 template <typename T, int N>
 __global__ void __launch_bounds__(64 * kAttendWaves) attend_delta_kernel(AttendArgs a)
 {
@@ -121,7 +141,7 @@ __device__ __forceinline__ void GradQ<T, N>::run(const AttendArgs &a, uint32_t p
     row_operands<T, N>(qp, a.dim, lane, q);
     row_operands<T, N>(dyp, a.dim, lane, dy);
     const float2 stat = sight.last < 0 ? make_float2(0.0f, 0.0f) : lse_delta(a, at);
-    const float lse2 = stat.x, minus_lse = kCarry<T> - lse2, delta = stat.y;
+    const float minus_lse = kCarry<T> - stat.x, delta = stat.y;
     f32x16 sum[N];
 #pragma unroll
     for (int n = 0; n < N; ++n)
@@ -207,39 +227,66 @@ __device__ __forceinline__ void GradQ<T, N>::run(const AttendArgs &a, uint32_t p
             }
         }
     }
-    const bool bad = any_not_finite(sum) && sight.last >= 0 && fabsf(lse2) < INFINITY &&
+    // once more, with care
+    float carry = 1.0f;
+    const bool bad = any_not_finite(sum) && sight.last >= 0 && fabsf(minus_lse) < INFINITY &&
                      fabsf(delta) < INFINITY;
-    uint64_t which = __ballot(bad);
-    which = (which | which >> 32) & 0xffffffffu;
-    while (which) {
-        const int col = __builtin_ctzll(which);
-        which &= which - 1;
-        const int32_t to = __builtin_amdgcn_readlane(sight.last, col);
-        const int32_t from = __builtin_amdgcn_readlane(sight.first, col);
-        const float l2 = __shfl(lse2, col), dl = __shfl(delta, col);
-        const Column cc(a, s, mine + col);
-        const Spread qs = Spread::of(s.rows<T>(a.q, cc.head) + cc.i * a.q.row, a.dim, lane);
-        const Spread ds = Spread::of(s.rows<T>(a.dout, cc.head) + cc.i * a.dout.row, a.dim, lane);
-        Spread y = {0.0f, 0.0f};
-        for (int32_t n = 0; n < walk.count && !settled(y, a.dim, lane); ++n) {
-            const int32_t j0 = walk.tile(n) * kKeys;
-            for (int32_t j = j0; j < j0 + kKeys && j <= to; ++j) {
-                if (!sees(j, to, from, a.sinks))
+    // (told in the buffer that the last tile is not in)
+    if (any_wave((int *)(lds + (walk.count & 1) * (2 * kBytes)), __any(bad), wave, lane)) {
+        __syncthreads();  // before tiles take its place
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            sum[n] = (f32x16)0.0f;
+        fetch(0);
+#pragma unroll 1
+        for (int32_t n = 0; n < walk.count; ++n) {
+            loads_done();
+            __syncthreads();
+            if (n + 1 < walk.count)
+                fetch(n + 1);
+            const int l = fresh(lane), row_at = Rows::row_at(l), column_at = Rows::column_at(l);
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                const int32_t j0 = walk.tile(n) * kKeys + 32 * h;
+                if (!sight.any(a, j0, j0 + 31))
                     continue;
-                const Spread ks = Spread::of(kp + j * a.k.row, a.dim, lane);
-                const Spread vs = Spread::of(vp + j * a.v.row, a.dim, lane);
-                const PairOf w(a, qs, ds, ks, vs, l2, dl);
-                y.x = fmaf(w.d, ks.x, y.x);
-                y.y = fmaf(w.d, ks.y, y.y);
+                const char *keys = lds + (n & 1) * (2 * kBytes) + 32 * h * Rows::kStride;
+                f32x16 x = (f32x16)0.0f, y = (f32x16)0.0f;
+#pragma unroll
+                for (int k = 0; k < 2 * N; ++k) {
+                    multiply<T>(x, Rows::row(keys, row_at, 0, k), q[k]);
+                    multiply<T>(y, Rows::row(keys + kBytes, row_at, 0, k), dy[k]);
+                    in_order();
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    x[e] = exp2_of(fmaf(x[e], a.scale_log2, minus_lse)) * (y[e] - delta);
+                sight.hide<true>(a, x, j0, l, 0.0f);
+                carry_less<T, N>(x, sum, carry);
+                in_order();
+                bool some = false;
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const vec<T, 8> d = operand<T>(x, g);
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        multiply<T>(
+                            sum[k], finite_of<T>(Rows::column(keys, column_at, 16 * g, k), some),
+                            d);
+                        in_order();
+                    }
+                }
+                // a key that is not finite: its weight is zero, or lse is not finite
+                if (some)
+                    add_not_finite<true, T, N>(sum, keys, l, [&](int r) {
+                        return sees(j0 + r, sight.last, sight.first, a.sinks);
+                    });
             }
         }
-        y.x *= 1.0f / kCarried<T>;
-        y.y *= 1.0f / kCarried<T>;
-        set_column(sum, y, col, lane);
     }
     if (c.exists)
         write_row<T, N>((T *)s.rows<T>(a.dq, c.head) + c.i * a.dq.row, nullptr, sum,
-                        a.scale * kCarried<T>, sight.last < 0, a.dim, lane);
+                        a.scale * kCarried<T> / carry, sight.last < 0, a.dim, lane);
 }
 
 // The queries that see any of keys j0 .. j1, and their columns.
@@ -412,6 +459,14 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t p
             }
         }
     };
+    const auto tell = [&](int buffer) {
+        if (threadIdx.x < kCols) {
+            stats.lses[buffer][threadIdx.x] = m_lse;
+            stats.deltas[buffer][threadIdx.x] = m_delta;
+            stats.lasts[buffer][threadIdx.x] = m_last;
+            stats.firsts[buffer][threadIdx.x] = m_first;
+        }
+    };
     if (c_begin < c_end) {
         place(c_begin);
         fetch(c_begin, 0);
@@ -419,12 +474,7 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t p
     const int row_at0 = Rows::row_at(lane), column_at0 = Rows::column_at(lane);
     int buffer = 0;
     for (int32_t c0 = c_begin; c0 < c_end; c0 += kCols, buffer ^= 1) {
-        if (threadIdx.x < kCols) {
-            stats.lses[buffer][threadIdx.x] = m_lse;
-            stats.deltas[buffer][threadIdx.x] = m_delta;
-            stats.lasts[buffer][threadIdx.x] = m_last;
-            stats.firsts[buffer][threadIdx.x] = m_first;
-        }
+        tell(buffer);
         // the tile is there, for all waves; the other buffer's tile has been used by all
         loads_done();
         __syncthreads();
@@ -523,39 +573,74 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t p
             }
         }
     }
+    // once more, with care
+    float carry = 1.0f;
+    const AttendArgs &late = args_again();
     const bool bad = (any_not_finite(dk) || any_not_finite(dv)) && j < s.k_length;
-    uint64_t which = __ballot(bad);
-    which = (which | which >> 32) & 0xffffffffu;
-    while (which) {
-        const int col = __builtin_ctzll(which);
-        which &= which - 1;
-        const int32_t key = mine + col;
-        const Spread ks = Spread::of(kp + key * a.k.row, a.dim, lane);
-        const Spread vs = Spread::of(vp + key * a.v.row, a.dim, lane);
-        Spread gk = {0.0f, 0.0f}, gv = {0.0f, 0.0f};
-        for (int32_t at = c_begin; at < c_end; ++at) {
-            const Column c(a, s, at);
-            if (!sees(key, s.last(a, c.i), s.first(a, c.i), a.sinks))
-                continue;
-            const int64_t row = ((int64_t)s.b * a.queries + c.i) * a.heads + c.head;
-            const Spread qs = Spread::of(s.rows<T>(a.q, c.head) + c.i * a.q.row, a.dim, lane);
-            const Spread ds =
-                Spread::of(s.rows<T>(a.dout, c.head) + c.i * a.dout.row, a.dim, lane);
-            const float2 stat = lse_delta(a, row);
-            const PairOf w(a, qs, ds, ks, vs, stat.x, stat.y);
-            gk.x = fmaf(w.d, qs.x, gk.x);
-            gk.y = fmaf(w.d, qs.y, gk.y);
-            gv.x = fmaf(w.p, ds.x, gv.x);
-            gv.y = fmaf(w.p, ds.y, gv.y);
-            if (settled(gk, a.dim, lane) && settled(gv, a.dim, lane))
-                break;
+    // (told in the buffer that the last tile is not in)
+    if (any_wave((int *)(lds + buffer * (2 * kBytes)), __any(bad), wave, lane)) {
+        __syncthreads();  // before tiles take its place
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            dk[n] = dv[n] = (f32x16)0.0f;
+        fetch(c_begin, 0);
+        buffer = 0;
+#pragma unroll 1
+        for (int32_t c0 = c_begin; c0 < c_end; c0 += kCols, buffer ^= 1) {
+            tell(buffer);
+            loads_done();
+            __syncthreads();
+            if (c0 + kCols < c_end)
+                fetch(c0 + kCols, buffer ^ 1);
+            const int l = fresh(lane), row_at = Rows::row_at(l), column_at = Rows::column_at(l);
+            const char *rows = lds + buffer * (2 * kBytes), *grads = rows + kBytes;
+            f32x16 x, y;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int r = 8 * (e >> 2) + 4 * (l >> 5) + (e & 3);
+                x[e] = stats.lses[buffer][r];
+                y[e] = stats.deltas[buffer][r];
+            }
+#pragma unroll
+            for (int k = 0; k < 2 * N; ++k) {
+                multiply<T>(x, Rows::row(rows, row_at, 0, k), k_rows[k]);
+                multiply<T>(y, Rows::row(grads, row_at, 0, k),
+                            Rows::row(values, row_at + wave * (32 * Rows::kStride), 0, k));
+                in_order();
+            }
+            const auto seen = [&](int r) {
+                return sees(j, stats.lasts[buffer][r], stats.firsts[buffer][r], late.sinks);
+            };
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const bool some = seen(8 * (e >> 2) + 4 * (l >> 5) + (e & 3));
+                x[e] = some ? exp2_of(x[e] * late.scale_log2) : 0.0f;
+                y[e] = some ? x[e] * y[e] : 0.0f;
+            }
+            carry_less<T, N>(y, dk, carry);
+            in_order();
+            bool some_grads = false, some_rows = false;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const vec<T, 8> p = operand<T>(x, g), d = operand<T>(y, g);
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const vec<T, 8> of_grads = Rows::column(grads, column_at, 16 * g, k);
+                    const vec<T, 8> of_rows = Rows::column(rows, column_at, 16 * g, k);
+                    multiply<T>(dv[k], finite_of<T>(of_grads, some_grads), p);
+                    multiply<T>(dk[k], finite_of<T>(of_rows, some_rows), d);
+                    in_order();
+                }
+            }
+            // (a query that is not finite has no finite weight)
+            if (some_grads)
+                add_not_finite<false, T, N>(dv, grads, l, seen);
+            if (some_rows)
+                add_not_finite<true, T, N>(dk, rows, l, seen);
         }
-        constexpr float up = 1.0f / kCarried<T>;
-        set_column(dk, Spread{gk.x * up, gk.y * up}, col, lane);
-        set_column(dv, Spread{gv.x * up, gv.y * up}, col, lane);
     }
     const bool none = j >= s.k_length;
-    const float fk = a.scale * kCarried<T>, fv = kCarried<T>;
+    const float fk = a.scale * kCarried<T> / carry, fv = kCarried<T>;
     if (!whole) {
         const Place at(args_again(), blockIdx.x);  // (in fewer registers than kept)
         const int64_t place = (int64_t)at.unit * a.pairs + at.pair;
@@ -574,7 +659,8 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t p
 // beside the other's (queries first: 431 us for 397). Bound by the matrix
 // instructions and what they wait for: the ragged sequences take 373 us, seven
 // products at a library's rate would take 208. 64 images of 197 rows of 12
-// heads of 64 in fp16, 74 us: 197 rows fill 77 % of two tiles of 128.
+// heads of 64 in fp16, 74 us: 197 rows fill 77 % of two tiles of 128. (Either reads the
+// arguments for itself: read for both at the start they do not fit the registers.)
 template <typename T, int N>
 __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     attend_grad_kernel(AttendArgs a)
@@ -587,7 +673,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 2 ? 2 : 1)
     if (at.unit < a.key_units)
         Keys::run(a, at.pair, at.unit, lds);
     else
-        Queries::run(a, at.pair, at.unit - a.key_units, lds);
+        Queries::run(args_again(), at.pair, at.unit - a.key_units, lds);
 }
 
 // Joins the parts of the keys' gradients, in order: four keys a workgroup, four

@@ -107,18 +107,21 @@ struct Columns {
         look(a, x, j0, lane, &f);
         weigh(a, x, 0, 16);
         in_order();
+        bool some = false;
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             const vec<T, 8> w = operand<T>(x, g);
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                multiply<T>(sum[n], finite_of<T>(Rows::column(values, value_at, 16 * g, n)), w);
+                multiply<T>(sum[n], finite_of<T>(Rows::column(values, value_at, 16 * g, n), some),
+                            w);
                 in_order();
             }
         }
-        add_not_finite<false, T, N>(
-            sum, values, rows_not_finite<T, N>(values, lane), lane,
-            [&](int r) { return sees(j0 + r, sight.last, sight.first, a.sinks); });
+        if (some)
+            add_not_finite<false, T, N>(sum, values, lane, [&](int r) {
+                return sees(j0 + r, sight.last, sight.first, a.sinks);
+            });
     }
     // Rows of out, rest and lse; or, of a part of the keys, sums, m and l.
     __device__ __forceinline__ void finish(const AttendArgs &a, const Sequence &s, int32_t c0,

@@ -126,6 +126,60 @@ def test_gradients_that_are_not_finite(shape, dtype):
     assert not bool(torch.isfinite(dk[:, touched]).any())
 
 
+def test_keys_of_minus_infinity_have_no_weight():
+    """A visible key whose score is minus infinity: rows and gradients as without it."""
+    note("attend gradients, -inf")
+    for dtype in TYPES:
+        q, k, v, dy = inputs((1, 70, 70, 1, 1, 16, True, 0, 0), dtype, 2)
+        q[..., 0] = 1.0
+        k[..., 0] = 0.0
+        k[:, 20:23, :, 0] = -INF
+        keep = [j for j in range(70) if not 20 <= j < 23]
+        out, lse = attention.attend(dev(q), dev(k), dev(v))
+        see = ref.visible(70, 70, 70, 70, True, 0, 0)
+        assert bool(torch.isfinite(out).all())
+        dq, dk, dv = (x.cpu() for x in attention.attend_backward(dev(dy), dev(q), dev(k), dev(v),
+                                                                 out, lse))
+        # the key's infinite value times a d of zero
+        some = see[:, 20:23].any(1)
+        assert bool(torch.isfinite(dq[..., 1:]).all())
+        assert bool(torch.isfinite(dq[:, ~some]).all())
+        assert bool(torch.isfinite(dk[:, keep]).all()) and bool(torch.isfinite(dv[:, keep]).all())
+        assert bool((dk[:, 20:23] == 0).all()) and bool((dv[:, 20:23] == 0).all())
+
+
+@pytest.mark.parametrize("shape", SHAPES + [(1, 515, 300, 6, 2, 72, True, 100, 130),
+                                            (1, 300, 300, 1, 1, 96, False, 0, 0)])
+@pytest.mark.parametrize("top, wide", [(6000.0, 1.0), (24000.0, 1.0), (60000.0, 1.0),
+                                       (60000.0, 4.0)])
+@pytest.mark.parametrize("every", [1, 40])
+def test_large_gradients_in_fp16(shape, top, wide, every):
+    """|d| between 2^10, where d carried times 2^6 passes fp16, and 2^17.5: within the
+    bound of smaller ones. A d that would pass is carried so that the largest of its
+    row (key) is at least 2^14: half a step of fp16's smallest is then largest *
+    2^-39."""
+    note(f"attend large gradients {shape} {top} {wide} {every}")
+    q, k, v, dy = inputs(shape, F16, 41)
+    q, k, v, dy = q * 0.25, k * 0.25, v * wide, dy * 0.01
+    dy[:, ::every] = (dy[:, ::every].float() * (top / 0.03)).clamp(-60000, 60000).half()
+    k[:, ::7] *= 8.0
+    q[:, ::3] *= 8.0
+    rest = torch.empty_like(q, device="cuda")
+    kw = dict(mask(shape), scale=0.02)  # gradients of queries and keys stay within fp16
+    out, lse = attention.attend(dev(q), dev(k), dev(v), rest=rest, **kw)
+    wants = ref.attend_backward(dy, q, k, v, out.cpu(), lse.cpu(), rest.cpu(), **kw)
+    grads = attention.attend_backward(dev(dy), dev(q), dev(k), dev(v), out, lse, rest, **kw)
+    # |d| <= |dy| |v| + |dy| |out + rest| <= 2 |dy| max |v|, of each pair
+    lq, lk = shape[1:3]
+    most = 2.0 * float(dy.double().norm(dim=-1).max()) * float(v.double().norm(dim=-1).max())
+    step = most * 2.0 ** -39 * 0.02
+    room = (lk * float(k.double().abs().max()), lq * shape[3] // shape[4] *
+            float(q.double().abs().max()), 0.0)
+    for got, (a, e), name, n in zip(grads, wants, "qkv", room):
+        assert float(a.abs().max()) < 65000.0
+        close(got, a, e + step * n, f"grad {name}")
+
+
 def least_time(call) -> float:
     """Of five calls, in milliseconds."""
     begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
@@ -171,3 +225,22 @@ def test_a_value_that_is_not_finite_costs_little(value, row, dtype):
 
     clean, spoiled = costs(dtype, change)
     assert spoiled[0] < 20 * clean[0], (clean, spoiled)
+
+
+SPOIL = {
+    "value": lambda q, k, v, dy: v[0, 60, 0].fill_(NAN),
+    "query": lambda q, k, v, dy: q[0, 500, 0, 3:4].fill_(NAN),
+    "key": lambda q, k, v, dy: k[0, 60, 0, 3:4].fill_(INF),
+    "gradient": lambda q, k, v, dy: dy[0, 1000, 0, 3:4].fill_(-INF),
+    "large gradients": lambda q, k, v, dy: (dy.mul_(10000.0), q.mul_(4.0)),
+}
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("what", sorted(SPOIL))
+def test_a_gradient_that_is_not_finite_costs_little(what, dtype):
+    """The same for the backward pass, and for finite gradients that fp16 does not hold as
+    they are carried."""
+    note(f"attend time, gradients, {what} {dtype}")
+    clean, spoiled = costs(dtype, SPOIL[what])
+    assert spoiled[1] < 20 * clean[1], (clean, spoiled)
