@@ -5,7 +5,12 @@
 // base 2: weights 2^(s - m) are rounded to the type and multiplied with the
 // values in fp32; a maximum that grows scales what was summed before. m is a
 // whole number and may stay up to 8 behind the maximum (weights up to 256), so
-// most tiles scale nothing, and scaling rounds nothing.
+// most tiles scale nothing, and scaling sums rounds nothing.
+//
+// fp16 has few exponents: there m is 7 less, so weights are carried times 2^7 (up to
+// 2^15), in l too. A weight below 2^-32 of the largest is then zero, so that n keys
+// lose at most n 2^-32 of a row's weight (2^-25 without: a key of e^18 times the weight
+// of each of 8192 others left them none of their 2^-13).
 //
 // What a query does not see takes no part: its score is set to minus infinity
 // before the maximum. A weight of 0 times a NaN or an infinity among the values
@@ -22,6 +27,10 @@ namespace smol {
 namespace {
 
 constexpr float kBehind = 8.0f;
+
+// log2 of what weights are carried by.
+template <typename T>
+constexpr float kWeightCarry = std::is_same<T, f16>::value ? 7.0f : 0.0f;
 
 // One wave's 32 columns: scores, weights and sums.
 template <typename T, int N>
@@ -50,7 +59,7 @@ struct Columns {
     // Scores x of 32 keys from j0 on (register rows): what is not seen leaves, and
     // the maximum follows. True (and f) where what was summed, and weights formed
     // before, are to be scaled by f. The maximum is kept as a whole number, so f is a
-    // power of two and scaling rounds nothing.
+    // power of two and scaling rounds nothing but fp16 weights that come below 2^-14.
     __device__ __forceinline__ bool look(const AttendArgs &a, f32x16 &x, int32_t j0, int lane,
                                          float *f)
     {
@@ -60,9 +69,9 @@ struct Columns {
         for (int e = 0; e < 16; ++e)
             top = fmaxf(top, x[e]);
         top = both_halves(top, [](float u, float v) { return fmaxf(u, v); }) * a.scale_log2;
-        if (!__any(top > m + kBehind))
+        if (!__any(top > m + (kBehind + kWeightCarry<T>)))
             return false;
-        const float to = fmaxf(m, ceilf(top));
+        const float to = fmaxf(m, ceilf(top) - kWeightCarry<T>);
         *f = exp2_of(m - to);
         m = to;
         l *= *f;
@@ -319,7 +328,10 @@ __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 4 ? 1 : N <= 2
             for (int h = 0; h < 2; ++h)
                 if (cols.sight.any(late, j0 + 32 * h, j0 + 32 * h + 31))
                     cols.carefully(
-                        late, [&](int k) { return Rows::row(tile, Rows::row_at(fresh(lane)), 32 * h, k); },
+                        late,
+                        [&](int k) {
+                            return Rows::row(tile, Rows::row_at(fresh(lane)), 32 * h, k);
+                        },
                         tile + kBytes + 32 * h * Rows::kStride, j0 + 32 * h, lane);
         }
     }

@@ -77,7 +77,8 @@ def test_binding_takes_any_strides():
             attention.attend_backward(**dict(args, **good))
     for bad in (dict(lse=lse[:1]), dict(lse=lse.double()), dict(lse=lse.transpose(1, 2)[:, 1:]),
                 dict(lse=torch.zeros((b, n, 1, h)).transpose(1, 3)[..., 0].transpose(1, 2)[:, :2]),
-                dict(rest=rest[:, :2]), dict(rest=rest.half()), dict(rest=rest.transpose(1, 2)[:, 1:]),
+                dict(rest=rest[:, :2]), dict(rest=rest.half()),
+                dict(rest=rest.transpose(1, 2)[:, 1:]),
                 dict(rest=torch.zeros((b, n, d, h)).transpose(2, 3))):
         with pytest.raises(ValueError, match="lse|rest") as e:
             attention.attend_backward(**dict(args, **bad))

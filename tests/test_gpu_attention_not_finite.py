@@ -180,6 +180,30 @@ def test_large_gradients_in_fp16(shape, top, wide, every):
         close(got, a, e + step * n, f"grad {name}")
 
 
+@pytest.mark.parametrize("queries", [1, 70])
+def test_many_small_weights_in_fp16(queries):
+    """Keys of which each has 2^-26 of a query's weight, 2^13 of them together 2^-13,
+    beside one key whose value is zero: a weight's rounding is half a step of 2^-24
+    below 2^-14, and weights are carried times 2^7 relative to a whole maximum that is
+    8 behind at most: each is off by 2^-25 * 2^-7 * 2 of the largest."""
+    note(f"attend small weights {queries}")
+    n, d, b = 1 << 13, 32, 300  # (as many sequences as make a cache whole, not in parts)
+    q = torch.zeros((1, queries, 1, d), dtype=F16)
+    k = torch.zeros((1, n + 1, 1, d), dtype=F16)
+    v = torch.full((1, n + 1, 1, d), 500.0, dtype=F16)
+    q[..., 0] = 1.0
+    k[:, 0, :, 0] = 18.0  # e^18 = 2^25.97
+    v[:, 0] = 0.0
+    (want, bound), _ = ref.attend(q.float(), k.float(), v.float(), scale=1.0, causal=False)
+    assert 0.05 < float(want.min()) < 0.1
+    each = 2.0 ** -31 * n * 500.0
+    for order in (slice(None), torch.arange(n, -1, -1)):
+        args = (dev(t).expand(b, -1, -1, -1) for t in (q, k[:, order], v[:, order]))
+        out, _ = attention.attend(*args, scale=1.0, causal=False)
+        assert bool((out == out[:1]).all())
+        close(out[:1], want, bound + 2.0 ** -11 * want.abs() + each, "out")
+
+
 def least_time(call) -> float:
     """Of five calls, in milliseconds."""
     begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
