@@ -443,18 +443,19 @@ struct RowMover {
 };
 
 // Whether any of a result's N tiles has a value that is not finite: the only ones
-// that 0 times does not make 0.
+// that 0 times does not make 0. (Or, with another factor, one that times this passes
+// fp32.)
 template <int N>
-__device__ __forceinline__ bool any_not_finite(const f32x16 (&x)[N])
+__device__ __forceinline__ bool any_not_finite(const f32x16 (&x)[N], float times = 0.0f)
 {
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-            s[e & 3] = fmaf(x[n][e], 0.0f, s[e & 3]);
+            s[e & 3] = fmaf(x[n][e], times, s[e & 3]);
     const float all = (s[0] + s[1]) + (s[2] + s[3]);
-    return all != all;
+    return !(fabsf(all) < INFINITY);
 }
 
 // Whether any of the workgroup's waves says so (each the same in all its lanes), by way

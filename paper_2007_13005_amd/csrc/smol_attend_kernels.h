@@ -32,6 +32,20 @@ constexpr float kBehind = 8.0f;
 template <typename T>
 constexpr float kWeightCarry = std::is_same<T, f16>::value ? 7.0f : 0.0f;
 
+// The same where sums are formed again, which may be because they neared fp32's end: the
+// maximum is never behind and weights are 2^-24 at most, so that as many of them as
+// there can be, times the largest value, stay within it (fp16's sums cannot pass it).
+template <typename T>
+constexpr float kCarefulCarry = std::is_same<T, f16>::value ? 7.0f : -24.0f;
+
+// lse in base e, of a maximum m and sum l of weights. l of weights carried far down is
+// taken up first, so that the logarithm's integer is added exactly.
+__device__ __forceinline__ float lse_of(float m, float l)
+{
+    const bool down = l < 0x1p-6f;
+    return ((down ? m - 24.0f : m) + __builtin_amdgcn_logf(down ? l * 0x1p24f : l)) * kLn2;
+}
+
 // One wave's 32 columns: scores, weights and sums.
 template <typename T, int N>
 struct Columns {
@@ -60,18 +74,20 @@ struct Columns {
     // the maximum follows. True (and f) where what was summed, and weights formed
     // before, are to be scaled by f. The maximum is kept as a whole number, so f is a
     // power of two and scaling rounds nothing but fp16 weights that come below 2^-14.
+    template <bool Careful = false>
     __device__ __forceinline__ bool look(const AttendArgs &a, f32x16 &x, int32_t j0, int lane,
                                          float *f)
     {
+        constexpr float carry = Careful ? kCarefulCarry<T> : kWeightCarry<T>;
         sight.hide<false>(a, x, j0, lane, -INFINITY);
         float top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 16; ++e)
             top = fmaxf(top, x[e]);
         top = both_halves(top, [](float u, float v) { return fmaxf(u, v); }) * a.scale_log2;
-        if (!__any(top > m + (kBehind + kWeightCarry<T>)))
+        if (!__any(top > m + (Careful ? carry : kBehind + carry)))
             return false;
-        const float to = fmaxf(m, ceilf(top) - kWeightCarry<T>);
+        const float to = fmaxf(m, ceilf(top) - carry);
         *f = exp2_of(m - to);
         m = to;
         l *= *f;
@@ -90,12 +106,13 @@ struct Columns {
                 l += x[e];
             }
     }
-    // Whether a column's sums alone are not finite, or were spoiled by what it does not
-    // see: over the wave, the same in each lane.
+    // Whether a column's sums alone are not finite, spoiled by what it does not see
+    // perhaps, or past 2^112 and so perhaps not in what joins waves and parts (256 of
+    // them): over the wave, the same in each lane.
     __device__ __forceinline__ bool spoiled() const
     {
         const float all = both_halves(l, [](float u, float v) { return u + v; });
-        return __any(any_not_finite(sum) && fabsf(all) < INFINITY && sight.last >= 0);
+        return __any(any_not_finite(sum, 0x1p16f) && fabsf(all) < INFINITY && sight.last >= 0);
     }
     // Scores, weights and sums of 32 keys from j0 on, whose values stand at `values` in
     // LDS; keys(k) gives the operands of their scores. What is not finite among the
@@ -113,7 +130,7 @@ struct Columns {
         for (int k = 0; k < 2 * N; ++k)
             multiply<T>(x, keys(k), q[k]);
         in_order();
-        look(a, x, j0, lane, &f);
+        look<true>(a, x, j0, lane, &f);
         weigh(a, x, 0, 16);
         in_order();
         bool some = false;
@@ -164,7 +181,7 @@ struct Columns {
         write_row<T, N>(out, a.rest ? (T *)a.rest + row * a.dim : nullptr, sum, 1.0f / l,
                         sight.last < 0, a.dim, lane);
         if (a.lse && lane < 32)
-            a.lse[row] = sight.last < 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+            a.lse[row] = sight.last < 0 ? -INFINITY : lse_of(m, l);
     }
 };
 
@@ -541,7 +558,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves) attend_join_kernel(AttendAr
     if (N > 2)
         write(lane + 64, y.y);
     if (a.lse && lane == 0)
-        a.lse[row] = none ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
+        a.lse[row] = none ? -INFINITY : lse_of(top, total);
 }
 
 template <typename T>

@@ -2,6 +2,8 @@
 exactly what sees them. Against the 64-bit definitions of tests/attention_util.py."""
 from __future__ import annotations
 
+import math
+
 import pytest
 import torch
 
@@ -202,6 +204,44 @@ def test_many_small_weights_in_fp16(queries):
         out, _ = attention.attend(*args, scale=1.0, causal=False)
         assert bool((out == out[:1]).all())
         close(out[:1], want, bound + 2.0 ** -11 * want.abs() + each, "out")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", [(1, 70, 300, 2, 1, 32, True, 0, 0),
+                                   (1, 1, 900, 4, 1, 64, True, 0, 0),
+                                   (1, 200, 200, 1, 1, 128, False, 0, 0)])
+def test_values_near_the_types_largest(shape, dtype):
+    """Rows are means of the values, so finite values have finite rows: values of 2^126
+    and scores that grow along the keys."""
+    note(f"attend largest values {shape} {dtype}")
+    q, k, v, _ = inputs(shape, dtype, 43)
+    lk = shape[2]
+    q[..., 0] = 1.0
+    k[..., 0] = (torch.arange(lk) * 0.125).view(1, lk, 1).to(dtype)
+    v = torch.sign(v) * 2.0 ** 126
+    (want, bound), (wl, bl) = ref.attend(q, k, v, scale=1.0, **mask(shape))
+    out, lse = attention.attend(dev(q), dev(k), dev(v.to(dtype)), scale=1.0, **mask(shape))
+    close(out, want, bound, "out")
+    close(lse, wl, bl, "lse")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("power", [126, 122, 120, 118, 116, 112, 108])
+def test_equal_weights_of_large_values(power, dtype):
+    """The same with equal weights, whose sums pass fp32 within a tile, where waves' or
+    parts' sums join, or not at all."""
+    note(f"attend equal weights {power} {dtype}")
+    for queries, keys, heads in ((1, 128, 4), (1, 3000, 2), (1, 20000, 8), (150, 700, 2)):
+        q = torch.zeros((1, queries, heads, 16), dtype=dtype)
+        k = torch.zeros((1, keys, 1, 16), dtype=dtype)
+        v = torch.full((1, keys, 1, 16), 2.0 ** power, dtype=dtype)
+        v[..., 1::2] *= -1.0
+        out, lse = attention.attend(dev(q), dev(k), dev(v), causal=False)
+        want = v[:, :1].double().expand(1, queries, heads, 16)
+        # count + 16 roundings of the sums and the quotient
+        close(out, want, (keys + 16) * 2.0 ** -24 * want.abs(), f"{keys}")
+        total = torch.full(lse.shape, math.log(keys), dtype=torch.float64)
+        close(lse, total, 64 * 2.0 ** -24 * (1 + total), f"lse {keys}")
 
 
 def least_time(call) -> float:
