@@ -15,6 +15,7 @@ workspaces are allocated where they are not given; a loop keeps its own.
 from __future__ import annotations
 
 import ctypes
+import math
 
 from . import smol
 from .smol import SmolError  # noqa: F401
@@ -149,7 +150,7 @@ def _head_norm_bytes(native, q, k) -> int:
     if q.dim() < 2 or (k is not None and k.dim() < 2):
         raise ValueError("q and k must have dimensions (..., heads, dim)")
     heads, dim = q.shape[-2:]
-    return native.head_norm_bytes(q.numel() // max(1, heads * dim), heads,
+    return native.head_norm_bytes(math.prod(q.shape[:-2]), heads,
                                   0 if k is None else k.shape[-2], dim)
 
 
