@@ -278,7 +278,7 @@ __device__ __forceinline__ void GradQ<T, N>::run(const AttendArgs &a, uint32_t p
                 }
                 // a key that is not finite: its weight is zero, or lse is not finite
                 if (some)
-                    add_not_finite<true, T, N>(sum, keys, l, [&](int r) {
+                    add_not_finite<true, T, N>(sum, keys, a.dim, sight.last >= 0, l, [&](int r) {
                         return sees(j0 + r, sight.last, sight.first, a.sinks);
                     });
             }
@@ -592,6 +592,9 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t p
             __syncthreads();
             if (c0 + kCols < c_end)
                 fetch(c0 + kCols, buffer ^ 1);
+            const int32_t end = c0 + kCols < c_end ? c0 + kCols : c_end;
+            if (mine > s.last(late, (int32_t)divide(end - 1, late.group)))
+                continue;
             const int l = fresh(lane), row_at = Rows::row_at(l), column_at = Rows::column_at(l);
             const char *rows = lds + buffer * (2 * kBytes), *grads = rows + kBytes;
             f32x16 x, y;
@@ -634,9 +637,9 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t p
             }
             // (a query that is not finite has no finite weight)
             if (some_grads)
-                add_not_finite<false, T, N>(dv, grads, l, seen);
+                add_not_finite<false, T, N>(dv, grads, late.dim, j < s.k_length, l, seen);
             if (some_rows)
-                add_not_finite<true, T, N>(dk, rows, l, seen);
+                add_not_finite<true, T, N>(dk, rows, late.dim, j < s.k_length, l, seen);
         }
     }
     const bool none = j >= s.k_length;

@@ -145,7 +145,7 @@ struct Columns {
             }
         }
         if (some)
-            add_not_finite<false, T, N>(sum, values, lane, [&](int r) {
+            add_not_finite<false, T, N>(sum, values, a.dim, sight.last >= 0, lane, [&](int r) {
                 return sees(j0 + r, sight.last, sight.first, a.sinks);
             });
     }
