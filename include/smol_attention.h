@@ -104,7 +104,9 @@ int smol_rotate_backward(const smol_rotate_args *a, void *stream);
  *
  *   r = 1 / sqrt((1/dim) sum_c x[c]^2 + eps),   out = rotation(x r weight)
  *
- * Squares are formed in fp32: values past 2^63 / sqrt(dim) overflow.
+ * Squares are formed in fp32: values past 2^63 / sqrt(dim) overflow, and those
+ * below 2^-75 count as zeros (with eps 0, a head of such values alone is not
+ * finite).
  * ------------------------------------------------------------------------ */
 
 /* The queries or the keys. heads may be 0: this side is then absent. */
@@ -189,9 +191,14 @@ int64_t smol_head_norm_workspace_bytes(int64_t rows, int32_t q_heads, int32_t k_
  *
  * A query that sees no key, or does not exist, has out 0 and lse minus
  * infinity. What a query does not see takes no part, whatever it holds: NaN
- * and infinities there are harmless. A NaN or infinite score that it sees
- * makes its row NaN. The weights exp(s - m), m near the row's maximum, are
- * rounded to the type before the product with v, as matrix operands are.
+ * and infinities there are harmless. Of the scores that it sees, a NaN or plus
+ * infinity makes its row and lse NaN; minus infinity has no weight, and a row of
+ * nothing else is NaN with lse minus infinity. NaN and infinities among the
+ * values that it sees are in their columns of its row, however small their
+ * weight; finite values give finite rows. The weights exp(s - m), m near the
+ * row's maximum, are rounded to the type before the product with v, as matrix
+ * operands are (fp16: those below 2^-32 of the largest are then zero). A call
+ * some of whose sums are not finite forms them twice, in a few times its time.
  *
  * Single tokens, prompts and pieces of prompts are the same call: new tokens
  * are the last `queries` rows of a cache whose first k_length rows are filled.
@@ -251,8 +258,11 @@ int64_t smol_attend_workspace_bytes(const smol_attend_shape *shape);
  *   grad_v[j] = sum_i p[i][j] grad_out[i]       (over all heads that read j)
  *   grad_q[i] = scale sum_j d[i][j] k[j],   grad_k[j] = scale sum_i d[i][j] q[i]
  *
- * p and d are rounded to the type before these products. Rows that do not
- * exist get zeros. */
+ * p and d are rounded to the type before these products (fp16: times powers of
+ * two, so that p down to 2^-30 and d of any size are held; a call some of whose d
+ * pass 2^10 forms sums twice in 2 to 3 times its time, as one with a NaN or an
+ * infinity does). A query that is NaN, or whose lse is, makes the gradients of
+ * all keys that it sees NaN. Rows that do not exist get zeros. */
 typedef struct smol_attend_grad_args {
     smol_attend_shape shape;
     smol_attend_rows grad_out, q, k, v, out;
