@@ -66,7 +66,7 @@ __device__ __forceinline__ void carry_less(f32x16 &d, f32x16 (&sum)[N], float &c
 
 // D of every row of queries that exists, beside its lse (which may lie at strides of
 // its own): a group of lanes a row, eight values a lane. Bound by memory (the ragged
-// sequences above: 129 MB in 29 us).
+// sequences above: 138 MB in 31 us).
 template <typename T, int N>
 __global__ void __launch_bounds__(64 * kAttendWaves) attend_delta_kernel(AttendArgs a)
 {
@@ -660,7 +660,7 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t p
 
 // Workgroups of keys, then those of queries, which are shorter: either's last run
 // beside the other's (queries first: 431 us for 397). Bound by the matrix
-// instructions and what they wait for: the ragged sequences take 373 us, seven
+// instructions and what they wait for: the ragged sequences take 377 us, seven
 // products at a library's rate would take 208. 64 images of 197 rows of 12
 // heads of 64 in fp16, 74 us: 197 rows fill 77 % of two tiles of 128. (Either reads the
 // arguments for itself: read for both at the start they do not fit the registers.)
