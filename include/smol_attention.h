@@ -193,12 +193,12 @@ int64_t smol_head_norm_workspace_bytes(int64_t rows, int32_t q_heads, int32_t k_
  * infinity. What a query does not see takes no part, whatever it holds: NaN
  * and infinities there are harmless. Of the scores that it sees, a NaN or plus
  * infinity makes its row and lse NaN; minus infinity has no weight, and a row of
- * nothing else is NaN with lse minus infinity. NaN and infinities among the
- * values that it sees are in their columns of its row, however small their
- * weight; finite values give finite rows. The weights exp(s - m), m near the
- * row's maximum, are rounded to the type before the product with v, as matrix
- * operands are (fp16: those below 2^-32 of the largest are then zero). A call
- * some of whose sums are not finite forms them twice, in a few times its time.
+ * nothing else is NaN with lse minus infinity. A NaN or an infinity among the
+ * values that it sees is in its row, however small the weight; finite values up
+ * to 2^127 give finite rows. The weights exp(s - m), m near the row's maximum,
+ * are rounded to the type before the product with v, as matrix operands are
+ * (fp16: those below 2^-32 of the largest are then zero). A call some of whose
+ * sums are not finite forms them twice, in a few times its time.
  *
  * Single tokens, prompts and pieces of prompts are the same call: new tokens
  * are the last `queries` rows of a cache whose first k_length rows are filled.

@@ -210,9 +210,9 @@ struct Task {
 // tile is on its way to LDS while this one is used.
 // 8192 tokens, 32 heads of 128 over 8, a window of 2048, bf16: 272 to 282 us by the card,
 // 855 to 886 TFLOP/s of the scores that are seen (products alone 138, with the softmax
-// 209, with LDS reads 233). Three buffers of tiles instead of two left too little LDS: 64 images of 197
-// rows and 16 heads of 64 took 42 us for 38. Up to 64 values a head four waves a SIMD
-// fit (these images 38 -> 36 us, and 33 since pairs come in chunks).
+// 209, with LDS reads 233). Three buffers of tiles instead of two left too little LDS: 64
+// images of 197 rows and 16 heads of 64 took 42 us for 38. Up to 64 values a head four
+// waves a SIMD fit (these images 38 -> 36 us, and 33 since pairs come in chunks).
 template <typename T, int N>
 __global__ void __launch_bounds__(64 * kAttendWaves, sizeof(T) == 4 ? 1 : N <= 2 ? 4 : 2)
     attend_kernel(AttendArgs a)
