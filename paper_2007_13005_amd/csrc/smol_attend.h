@@ -33,7 +33,7 @@ struct AttendArgs {
     int32_t tiles;         // of the columns
     int32_t pairs;         // batch * kv_heads
     int32_t splits;
-    float scale, scale_log2;  // the second times log2 e
+    float scale, scale_log2, per_scale_log2;  // times log2 e; 1 / that
     // gradients of keys: tiles of keys that hold sinks, and columns of a part of
     // these and of the other tiles (as many parts: the two divisors)
     int32_t sink_tiles, sink_part, tile_part;

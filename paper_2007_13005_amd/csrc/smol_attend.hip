@@ -239,6 +239,7 @@ AttendArgs args_of(const smol_attend_shape &s)
     a.pairs = s.batch * s.kv_heads;
     a.scale = s.scale;
     a.scale_log2 = (float)(s.scale * 1.44269504088896340736);
+    a.per_scale_log2 = 1.0f / a.scale_log2;
     a.group = make_divisor(group);
     a.pair_div = make_divisor(a.pairs);
     a.kv_heads = make_divisor(s.kv_heads);

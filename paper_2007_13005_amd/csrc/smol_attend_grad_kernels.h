@@ -227,66 +227,72 @@ __device__ __forceinline__ void GradQ<T, N>::run(const AttendArgs &a, uint32_t p
             }
         }
     }
-    // once more, with care
+    // written, and formed and written once more if need be (as in
+    // smol_attend_kernels.h)
     float carry = 1.0f;
     const bool bad = any_not_finite(sum) && sight.last >= 0 && fabsf(minus_lse) < INFINITY &&
                      fabsf(delta) < INFINITY;
+    const auto write = [&](const AttendArgs &late) {
+        if (c.exists)
+            write_row<T, N>((T *)s.rows<T>(late.dq, c.head) + c.i * late.dq.row, nullptr, sum,
+                            late.scale * kCarried<T> / carry, sight.last < 0, late.dim, lane);
+    };
+    write(args_again());
     // (told in the buffer that the last tile is not in)
-    if (any_wave((int *)(lds + (walk.count & 1) * (2 * kBytes)), __any(bad), wave, lane)) {
-        __syncthreads();  // before tiles take its place
+    if (!any_wave((int *)(lds + (walk.count & 1) * (2 * kBytes)), __any(bad), wave, lane))
+        return;
+    const AttendArgs &late = args_again();
+    __syncthreads();  // before tiles take its place
 #pragma unroll
-        for (int n = 0; n < N; ++n)
-            sum[n] = (f32x16)0.0f;
-        fetch(0);
+    for (int n = 0; n < N; ++n)
+        sum[n] = (f32x16)0.0f;
+    fetch(0);
 #pragma unroll 1
-        for (int32_t n = 0; n < walk.count; ++n) {
-            loads_done();
-            __syncthreads();
-            if (n + 1 < walk.count)
-                fetch(n + 1);
-            const int l = fresh(lane), row_at = Rows::row_at(l), column_at = Rows::column_at(l);
+    for (int32_t n = 0; n < walk.count; ++n) {
+        loads_done();
+        __syncthreads();
+        if (n + 1 < walk.count)
+            fetch(n + 1);
+        const int l = fresh(lane), row_at = Rows::row_at(l), column_at = Rows::column_at(l);
 #pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                const int32_t j0 = walk.tile(n) * kKeys + 32 * h;
-                if (!sight.any(a, j0, j0 + 31))
-                    continue;
-                const char *keys = lds + (n & 1) * (2 * kBytes) + 32 * h * Rows::kStride;
-                f32x16 x = (f32x16)0.0f, y = (f32x16)0.0f;
+        for (int h = 0; h < 2; ++h) {
+            const int32_t j0 = walk.tile(n) * kKeys + 32 * h;
+            if (!sight.any(late, j0, j0 + 31))
+                continue;
+            const char *keys = lds + (n & 1) * (2 * kBytes) + 32 * h * Rows::kStride;
+            f32x16 x = (f32x16)0.0f, y = (f32x16)0.0f;
 #pragma unroll
-                for (int k = 0; k < 2 * N; ++k) {
-                    multiply<T>(x, Rows::row(keys, row_at, 0, k), q[k]);
-                    multiply<T>(y, Rows::row(keys + kBytes, row_at, 0, k), dy[k]);
+            for (int k = 0; k < 2 * N; ++k) {
+                multiply<T>(x, Rows::row(keys, row_at, 0, k), q[k]);
+                multiply<T>(y, Rows::row(keys + kBytes, row_at, 0, k), dy[k]);
+                in_order();
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                x[e] = exp2_of(fmaf(x[e], late.scale_log2, minus_lse)) * (y[e] - delta);
+            sight.hide<true>(late, x, j0, l, 0.0f);
+            carry_less<T, N>(x, sum, carry);
+            in_order();
+            bool some = false;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const vec<T, 8> d = operand<T>(x, g);
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    multiply<T>(
+                        sum[k], finite_of<T>(Rows::column(keys, column_at, 16 * g, k), some),
+                        d);
                     in_order();
                 }
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    x[e] = exp2_of(fmaf(x[e], a.scale_log2, minus_lse)) * (y[e] - delta);
-                sight.hide<true>(a, x, j0, l, 0.0f);
-                carry_less<T, N>(x, sum, carry);
-                in_order();
-                bool some = false;
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const vec<T, 8> d = operand<T>(x, g);
-#pragma unroll
-                    for (int k = 0; k < N; ++k) {
-                        multiply<T>(
-                            sum[k], finite_of<T>(Rows::column(keys, column_at, 16 * g, k), some),
-                            d);
-                        in_order();
-                    }
-                }
-                // a key that is not finite: its weight is zero, or lse is not finite
-                if (some)
-                    add_not_finite<true, T, N>(sum, keys, a.dim, sight.last >= 0, l, [&](int r) {
-                        return sees(j0 + r, sight.last, sight.first, a.sinks);
-                    });
             }
+            // a key that is not finite: its weight is zero, or lse is not finite
+            if (some)
+                add_not_finite<true, T, N>(sum, keys, late.dim, sight.last >= 0, l, [&](int r) {
+                    return sees(j0 + r, sight.last, sight.first, late.sinks);
+                });
         }
     }
-    if (c.exists)
-        write_row<T, N>((T *)s.rows<T>(a.dq, c.head) + c.i * a.dq.row, nullptr, sum,
-                        a.scale * kCarried<T> / carry, sight.last < 0, a.dim, lane);
+    write(args_again());
 }
 
 // The queries that see any of keys j0 .. j1, and their columns.
@@ -388,7 +394,7 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t p
     }
     const T *qp = s.rows<T>(a.q, head0), *dp = s.rows<T>(a.dout, head0);
     const int64_t stat0 = (int64_t)s.b * a.queries * a.heads + head0;
-    // of the first 32 threads one column's numbers
+    // of the first 32 lanes one column's numbers
     float m_lse = 0.0f, m_delta = 0.0f;
     int32_t m_last = -1, m_first = 0;
     // offsets of the thread's chunks from the tile's first query: the same for all
@@ -446,25 +452,25 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t p
                 *(Chunk *)(here + kBytes) = w;
             }
         }
-        if (threadIdx.x < kCols) {
-            const int32_t c = c0 + threadIdx.x, i = (int32_t)divide(c, a.group);
+        if (wave == 0 && lane < kCols) {
+            const int32_t c = c0 + fresh(lane), i = (int32_t)divide(c, a.group);
             m_last = c < c_end ? s.last(a, i) : -1;
             m_first = s.first(a, i);
             m_lse = m_delta = 0.0f;  // what the scores' and the products' sums start from
             if (m_last >= 0) {
                 const int64_t row = stat0 + (int64_t)i * a.heads + c - i * group;
                 const float2 stat = lse_delta(a, row);
-                m_lse = (kCarry<T> - stat.x) * (1.0f / a.scale_log2);
+                m_lse = (kCarry<T> - stat.x) * a.per_scale_log2;
                 m_delta = -stat.y;
             }
         }
     };
     const auto tell = [&](int buffer) {
-        if (threadIdx.x < kCols) {
-            stats.lses[buffer][threadIdx.x] = m_lse;
-            stats.deltas[buffer][threadIdx.x] = m_delta;
-            stats.lasts[buffer][threadIdx.x] = m_last;
-            stats.firsts[buffer][threadIdx.x] = m_first;
+        if (wave == 0 && lane < kCols) {
+            stats.lses[buffer][lane] = m_lse;
+            stats.deltas[buffer][lane] = m_delta;
+            stats.lasts[buffer][lane] = m_last;
+            stats.firsts[buffer][lane] = m_first;
         }
     };
     if (c_begin < c_end) {
@@ -573,89 +579,95 @@ __device__ __forceinline__ void GradK<T, N>::run(const AttendArgs &a, uint32_t p
             }
         }
     }
-    // once more, with care
+    // written, and formed and written once more if need be
     float carry = 1.0f;
-    const AttendArgs &late = args_again();
-    const bool bad = (any_not_finite(dk) || any_not_finite(dv)) && j < s.k_length;
+    const bool none = j >= s.k_length;
+    const bool bad = (any_not_finite(dk) || any_not_finite(dv)) && !none;
+    const auto write = [&](const AttendArgs &late) {
+        const int l = fresh(lane);
+        const int32_t j1 = fresh(j);
+        const float fk = late.scale * kCarried<T> / carry, fv = kCarried<T>;
+        if (!whole) {
+            const Place at(late, blockIdx.x);
+            const int64_t place = (int64_t)at.unit * late.pairs + at.pair;
+            float *p = late.part + (place * 2 * kKeys + wave * 32 + (l & 31)) * (N * 32);
+            write_row<float, N>(p, nullptr, dk, fk, none, N * 32, l);
+            write_row<float, N>(p + kKeys * (N * 32), nullptr, dv, fv, none, N * 32, l);
+        } else if (j1 < late.keys) {
+            write_row<T, N>((T *)s.rows<T>(late.dk, s.kv) + j1 * late.dk.row, nullptr, dk, fk,
+                            none, late.dim, l);
+            write_row<T, N>((T *)s.rows<T>(late.dv, s.kv) + j1 * late.dv.row, nullptr, dv, fv,
+                            none, late.dim, l);
+        }
+    };
+    write(args_again());
     // (told in the buffer that the last tile is not in)
-    if (any_wave((int *)(lds + buffer * (2 * kBytes)), __any(bad), wave, lane)) {
-        __syncthreads();  // before tiles take its place
+    if (!any_wave((int *)(lds + buffer * (2 * kBytes)), __any(bad), wave, lane))
+        return;
+    const AttendArgs &late = args_again();
+    __syncthreads();  // before tiles take its place
 #pragma unroll
-        for (int n = 0; n < N; ++n)
-            dk[n] = dv[n] = (f32x16)0.0f;
-        fetch(c_begin, 0);
-        buffer = 0;
+    for (int n = 0; n < N; ++n)
+        dk[n] = dv[n] = (f32x16)0.0f;
+    fetch(c_begin, 0);
+    buffer = 0;
 #pragma unroll 1
-        for (int32_t c0 = c_begin; c0 < c_end; c0 += kCols, buffer ^= 1) {
-            tell(buffer);
-            loads_done();
-            __syncthreads();
-            if (c0 + kCols < c_end)
-                fetch(c0 + kCols, buffer ^ 1);
-            const int32_t end = c0 + kCols < c_end ? c0 + kCols : c_end;
-            if (mine > s.last(late, (int32_t)divide(end - 1, late.group)))
-                continue;
-            const int l = fresh(lane), row_at = Rows::row_at(l), column_at = Rows::column_at(l);
-            const char *rows = lds + buffer * (2 * kBytes), *grads = rows + kBytes;
-            f32x16 x, y;
+    for (int32_t c0 = c_begin; c0 < c_end; c0 += kCols, buffer ^= 1) {
+        tell(buffer);
+        loads_done();
+        __syncthreads();
+        if (c0 + kCols < c_end)
+            fetch(c0 + kCols, buffer ^ 1);
+        const int32_t end = c0 + kCols < c_end ? c0 + kCols : c_end;
+        if (mine > s.last(late, (int32_t)divide(end - 1, late.group)))
+            continue;
+        const int l = fresh(lane), row_at = Rows::row_at(l), column_at = Rows::column_at(l);
+        const char *rows = lds + buffer * (2 * kBytes), *grads = rows + kBytes;
+        f32x16 x, y;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int r = 8 * (e >> 2) + 4 * (l >> 5) + (e & 3);
-                x[e] = stats.lses[buffer][r];
-                y[e] = stats.deltas[buffer][r];
-            }
+        for (int e = 0; e < 16; ++e) {
+            const int r = 8 * (e >> 2) + 4 * (l >> 5) + (e & 3);
+            x[e] = stats.lses[buffer][r];
+            y[e] = stats.deltas[buffer][r];
+        }
 #pragma unroll
-            for (int k = 0; k < 2 * N; ++k) {
-                multiply<T>(x, Rows::row(rows, row_at, 0, k), k_rows[k]);
-                multiply<T>(y, Rows::row(grads, row_at, 0, k),
-                            Rows::row(values, row_at + wave * (32 * Rows::kStride), 0, k));
+        for (int k = 0; k < 2 * N; ++k) {
+            multiply<T>(x, Rows::row(rows, row_at, 0, k), k_rows[k]);
+            multiply<T>(y, Rows::row(grads, row_at, 0, k),
+                        Rows::row(values, row_at + wave * (32 * Rows::kStride), 0, k));
+            in_order();
+        }
+        const auto seen = [&](int r) {
+            return sees(j, stats.lasts[buffer][r], stats.firsts[buffer][r], late.sinks);
+        };
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const bool some = seen(8 * (e >> 2) + 4 * (l >> 5) + (e & 3));
+            x[e] = some ? exp2_of(x[e] * late.scale_log2) : 0.0f;
+            y[e] = some ? x[e] * y[e] : 0.0f;
+        }
+        carry_less<T, N>(y, dk, carry);
+        in_order();
+        bool some_grads = false, some_rows = false;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const vec<T, 8> p = operand<T>(x, g), d = operand<T>(y, g);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const vec<T, 8> of_grads = Rows::column(grads, column_at, 16 * g, k);
+                const vec<T, 8> of_rows = Rows::column(rows, column_at, 16 * g, k);
+                multiply<T>(dv[k], finite_of<T>(of_grads, some_grads), p);
+                multiply<T>(dk[k], finite_of<T>(of_rows, some_rows), d);
                 in_order();
             }
-            const auto seen = [&](int r) {
-                return sees(j, stats.lasts[buffer][r], stats.firsts[buffer][r], late.sinks);
-            };
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const bool some = seen(8 * (e >> 2) + 4 * (l >> 5) + (e & 3));
-                x[e] = some ? exp2_of(x[e] * late.scale_log2) : 0.0f;
-                y[e] = some ? x[e] * y[e] : 0.0f;
-            }
-            carry_less<T, N>(y, dk, carry);
-            in_order();
-            bool some_grads = false, some_rows = false;
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const vec<T, 8> p = operand<T>(x, g), d = operand<T>(y, g);
-#pragma unroll
-                for (int k = 0; k < N; ++k) {
-                    const vec<T, 8> of_grads = Rows::column(grads, column_at, 16 * g, k);
-                    const vec<T, 8> of_rows = Rows::column(rows, column_at, 16 * g, k);
-                    multiply<T>(dv[k], finite_of<T>(of_grads, some_grads), p);
-                    multiply<T>(dk[k], finite_of<T>(of_rows, some_rows), d);
-                    in_order();
-                }
-            }
-            // (a query that is not finite has no finite weight)
-            if (some_grads)
-                add_not_finite<false, T, N>(dv, grads, late.dim, j < s.k_length, l, seen);
-            if (some_rows)
-                add_not_finite<true, T, N>(dk, rows, late.dim, j < s.k_length, l, seen);
         }
+        // (a query that is not finite has no finite weight)
+        if (some_grads)
+            add_not_finite<false, T, N>(dv, grads, late.dim, j < s.k_length, l, seen);
+        if (some_rows)
+            add_not_finite<true, T, N>(dk, rows, late.dim, j < s.k_length, l, seen);
     }
-    const bool none = j >= s.k_length;
-    const float fk = a.scale * kCarried<T> / carry, fv = kCarried<T>;
-    if (!whole) {
-        const Place at(args_again(), blockIdx.x);  // (in fewer registers than kept)
-        const int64_t place = (int64_t)at.unit * a.pairs + at.pair;
-        float *p = a.part + (place * 2 * kKeys + wave * 32 + (lane & 31)) * (N * 32);
-        write_row<float, N>(p, nullptr, dk, fk, none, N * 32, lane);
-        write_row<float, N>(p + kKeys * (N * 32), nullptr, dv, fv, none, N * 32, lane);
-        return;
-    }
-    if (j >= a.keys)
-        return;
-    write_row<T, N>((T *)s.rows<T>(a.dk, s.kv) + j * a.dk.row, nullptr, dk, fk, none, a.dim, lane);
-    write_row<T, N>((T *)s.rows<T>(a.dv, s.kv) + j * a.dv.row, nullptr, dv, fv, none, a.dim, lane);
+    write(args_again());
 }
 
 // Workgroups of keys, then those of queries, which are shorter: either's last run
